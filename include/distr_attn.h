@@ -219,6 +219,112 @@ int distr_attn_hyperplanes(uint64_t seed, int n_planes, int Br, float *host_out)
 int distr_attn_fwd_noalloc(const void *q, const void *k, const void *v, void *o, const da_params *p);
 size_t distr_attn_noalloc_max_bytes(void);
 
+/*
+ * Around attention: what makes its queries and keys, and a cache that keeps keys and values in pages.
+ *
+ * Norm and rotation of a row x of d channels at position t, in 32 bits, rounded once:
+ *   n = x / sqrt(mean(x^2) + eps) * weight                       (norm = 1; else n = x)
+ *   (a, b) -> (a cos - b sin, a sin + b cos)                      for every pair of the first rot_dim channels
+ * with cos and sin of table row t, entry j for pair j: channels (j, j + rot_dim / 2) where rope is DA_ROPE_HALVES, (2 j, 2 j + 1)
+ * where it is DA_ROPE_NEIGHBOURS. A position outside the table makes the row's rotated channels NaN.
+ */
+typedef enum { DA_ROPE_NONE = 0, DA_ROPE_HALVES = 1, DA_ROPE_NEIGHBOURS = 2 } da_rope;
+
+typedef struct {
+  int norm;              /* 0 / 1                                                                        */
+  float eps;             /* >= 0, finite                                                                 */
+  const void *q_weight;  /* device [d], or [H][d] with weight_heads; null: ones                            */
+  const void *k_weight;  /* device [d], or [Hkv][d] with weight_heads; null: ones                          */
+  int weight_dtype;      /* da_dtype of the weights                                                      */
+  int weight_heads;      /* 0: one weight for all heads, 1: a weight for each head                       */
+  int rope;              /* da_rope                                                                      */
+  int rot_dim;           /* rotated channels, a multiple of 16, at most d (with rope)                    */
+  int n_pos;             /* rows of the tables                                                           */
+  const float *cos_table; /* device [n_pos][rot_dim / 2], 16-byte aligned                                */
+  const float *sin_table;
+} da_rotary;
+
+/* Queries q and keys k as [B][heads][N][d] by strides, in elements: of a batch, a head and a row (d is contiguous). */
+typedef struct {
+  int B, H, Hkv, N, d;   /* d in {64, 128}; Hkv 0: queries alone                                          */
+  int dtype;             /* da_dtype of the tensors                                                      */
+  int64_t q_stride[3], k_stride[3];          /* of q, k (backward: and of dq, dk); multiples of 16 bytes   */
+  int64_t q_out_stride[3], k_out_stride[3];  /* of q_out, k_out (backward: of dq_out, dk_out)              */
+  da_rotary rotary;
+  const int32_t *positions;  /* device [B][N]; null: row n of every batch is at position n                */
+  void *stream;          /* as in da_params                                                              */
+  void *workspace;       /* backward with weight gradients: as in da_params, distr_attn_qk_bwd_workspace_bytes() */
+  size_t workspace_bytes;
+} da_qk;
+
+/*
+ * Norms of queries and keys for each head, with the position rotation in the same pass. k and k_out null with Hkv = 0.
+ * q_out may be q and k_out may be k where their strides are the same (in place); other overlap is not allowed, and
+ * neither may rows of one output overlap. Pointers 16-byte aligned.
+ */
+int distr_attn_qk_norm_rope(const void *q, const void *k, void *q_out, void *k_out, const da_qk *p);
+
+/*
+ * Its gradient. q, k: the forward's inputs (read with norm = 1 alone, null else allowed); dq_out, dk_out: gradients of the loss with
+ * respect to its outputs. Written: dq, dk, in the types and strides of q and k (dq may be dq_out where the strides are the
+ * same, dk likewise), and, where not null, dq_weight ([d] or [H][d]) and dk_weight ([d] or [Hkv][d]), float: the sums over
+ * all rows that a weight scales (norm = 1 alone). No atomics: results are the same on every run. With a weight gradient the call
+ * needs distr_attn_qk_bwd_workspace_bytes(p) of scratch, found as in da_params.
+ */
+int distr_attn_qk_norm_rope_bwd(const void *q, const void *k, const void *dq_out, const void *dk_out, void *dq, void *dk,
+                                float *dq_weight, float *dk_weight, const da_qk *p);
+size_t distr_attn_qk_bwd_workspace_bytes(const da_qk *p);
+
+/*
+ * A batch of sequences whose keys and values lie in pages, and their new tokens.
+ *
+ * k_pages and v_pages are [n_pages][Hkv][page_size][d] by strides. Sequence s has kv_len[s] tokens, the new ones among
+ * them; token i of it lies in page page_table[s][i / page_size], row i % page_size. The new tokens of all sequences are
+ * the rows of q, k, v and o, one sequence after the other: rows q_start[s] .. q_start[s + 1] - 1 are the last ones of sequence
+ * s. Rows before q_start[0] and from q_start[n_seq] on belong to none and are left as they are. The three index arrays are read on the
+ * device, at the time of the call's kernels (a captured call sees what they hold at each replay): what they hold is not
+ * checked by the call, but no access leaves the buffers whatever it is. Lengths count up to max_pages * page_size; pages
+ * outside the cache hold nothing: a token whose page is none of 0 .. n_pages - 1 is not stored, and keys of such a page are
+ * not seen.
+ */
+typedef struct {
+  int H, Hkv, d;         /* d in {64, 128}; H a multiple of Hkv                                           */
+  int dtype;             /* da_dtype of all tensors                                                      */
+  int n_seq, n_tokens;   /* sequences; rows of q, k, v and o                                             */
+  int n_pages, page_size, max_pages;  /* page_size a multiple of 16; max_pages: columns of page_table     */
+  int64_t page_stride, head_stride, row_stride;  /* of k_pages and v_pages, in elements, multiples of 16 bytes; row_stride >= d */
+  const int32_t *page_table;  /* device [n_seq][max_pages]                                               */
+  const int32_t *kv_len;      /* device [n_seq]                                                          */
+  const int32_t *q_start;     /* device [n_seq + 1], ascending, within 0 .. n_tokens                      */
+  int64_t q_stride[2], k_stride[2], v_stride[2]; /* of a token and a head of q, k, v; multiples of 16 bytes */
+  da_rotary rotary;      /* append: norm (k_weight) and rotation of the new keys on their way              */
+  const int32_t *positions;   /* append: device [n_tokens], where a token's rotation is not that of its place in its sequence */
+  int causal;            /* 1: a new token sees the keys up to its own; 0: all kv_len[s]                  */
+  float softmax_scale;   /* as in da_params                                                              */
+  float *lse_out;        /* optional device [n_tokens][H]: log-sum-exp of every row (-infinity where it sees no key) */
+  void *stream;          /* as in da_params                                                              */
+  void *workspace;       /* attention: distr_attn_paged_workspace_bytes(), 256-byte aligned, for the partial sums of keys that are dealt
+                            out: with less of it they go to fewer workgroups, with too little stay together; NULL: a
+                            library-owned buffer as in da_params, or, where there is none to have, keys stay together */
+  size_t workspace_bytes;
+} da_paged;
+
+/*
+ * Stores the new tokens' keys and values (k, v: [n_tokens][Hkv][d] by strides) in the cache, the keys normed and rotated on the way if
+ * p->rotary says so. What lies in the cache otherwise is left as it is. Places that two tokens share (a page in two
+ * sequences' tables, both with new tokens on it) receive either of them.
+ */
+int distr_attn_cache_append(const void *k, const void *v, void *k_pages, void *v_pages, const da_paged *p);
+
+/*
+ * Exact attention of the new tokens over the cache, which holds their own keys and values already:
+ * o[t][h] = softmax(scale * q[t][h] K^T) V over the keys that token t sees, K and V those of head h / (H / Hkv). q is
+ * [n_tokens][H][d] by strides, o contiguous. A row that sees no key is 0. bf16: matrix cores, P rounded to bf16, sums in float; float tensors: float
+ * arithmetic. How the keys are dealt out depends on the lengths of the whole batch, and with it the order of a row's sums.
+ */
+int distr_attn_paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *o, const da_paged *p);
+size_t distr_attn_paged_workspace_bytes(const da_paged *p);
+
 /* Stream used when da_params.stream is NULL and by the short-form entry points (process-wide). */
 int distr_attn_set_stream(void *hip_stream);
 

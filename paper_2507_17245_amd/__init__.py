@@ -20,6 +20,8 @@ EXPORTS = (
     "distr_attn_bwd_ex", "distr_attn_exact_bwd_ex",
     "distr_attn_lsh_group", "distr_attn_key_prepass", "distr_attn_kt_bytes",
     "distr_attn_workspace_bytes", "distr_attn_bwd_workspace_bytes", "distr_attn_hyperplanes",
+    "distr_attn_qk_norm_rope", "distr_attn_qk_norm_rope_bwd", "distr_attn_qk_bwd_workspace_bytes",
+    "distr_attn_cache_append", "distr_attn_paged_fwd", "distr_attn_paged_workspace_bytes",
     "distr_attn_set_stream", "distr_attn_release", "distr_attn_last_error", "distr_attn_version",
 )
 
@@ -35,6 +37,40 @@ class DaParams(ctypes.Structure):
         ("workspace_bytes", ctypes.c_size_t), ("perm_out", ctypes.c_void_p),
         ("hash_out", ctypes.c_void_p), ("perm_in", ctypes.c_void_p), ("kt_in", ctypes.c_void_p),
         ("Nk", ctypes.c_int), ("side", ctypes.c_int), ("lse_out", ctypes.c_void_p),
+    ]
+
+
+class DaRotary(ctypes.Structure):
+    """Mirror of da_rotary."""
+    _fields_ = [
+        ("norm", ctypes.c_int), ("eps", ctypes.c_float), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+        ("weight_dtype", ctypes.c_int), ("weight_heads", ctypes.c_int), ("rope", ctypes.c_int), ("rot_dim", ctypes.c_int),
+        ("n_pos", ctypes.c_int), ("cos_table", ctypes.c_void_p), ("sin_table", ctypes.c_void_p),
+    ]
+
+
+class DaQk(ctypes.Structure):
+    """Mirror of da_qk."""
+    _fields_ = [
+        ("B", ctypes.c_int), ("H", ctypes.c_int), ("Hkv", ctypes.c_int), ("N", ctypes.c_int), ("d", ctypes.c_int),
+        ("dtype", ctypes.c_int), ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+        ("q_out_stride", ctypes.c_int64 * 3), ("k_out_stride", ctypes.c_int64 * 3), ("rotary", DaRotary),
+        ("positions", ctypes.c_void_p), ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class DaPaged(ctypes.Structure):
+    """Mirror of da_paged."""
+    _fields_ = [
+        ("H", ctypes.c_int), ("Hkv", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int),
+        ("n_seq", ctypes.c_int), ("n_tokens", ctypes.c_int), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int),
+        ("max_pages", ctypes.c_int), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64), ("page_table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+        ("q_start", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2),
+        ("v_stride", ctypes.c_int64 * 2), ("rotary", DaRotary), ("positions", ctypes.c_void_p), ("causal", ctypes.c_int),
+        ("softmax_scale", ctypes.c_float), ("lse_out", ctypes.c_void_p), ("stream", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
     ]
 
 
@@ -66,6 +102,13 @@ def lib():
         L.distr_attn_key_prepass.argtypes = [vp, vp, ctypes.POINTER(DaParams)]
         for name in ("distr_attn_workspace_bytes", "distr_attn_bwd_workspace_bytes", "distr_attn_kt_bytes"):
             getattr(L, name).argtypes = [ctypes.POINTER(DaParams)]
+            getattr(L, name).restype = ctypes.c_size_t
+        L.distr_attn_qk_norm_rope.argtypes = [vp] * 4 + [ctypes.POINTER(DaQk)]
+        L.distr_attn_qk_norm_rope_bwd.argtypes = [vp] * 8 + [ctypes.POINTER(DaQk)]
+        for name in ("distr_attn_cache_append", "distr_attn_paged_fwd"):
+            getattr(L, name).argtypes = [vp] * 4 + [ctypes.POINTER(DaPaged)]
+        for name, params in (("distr_attn_qk_bwd_workspace_bytes", DaQk), ("distr_attn_paged_workspace_bytes", DaPaged)):
+            getattr(L, name).argtypes = [ctypes.POINTER(params)]
             getattr(L, name).restype = ctypes.c_size_t
         L.distr_attn_hyperplanes.argtypes = [u64, ci, ci, ctypes.POINTER(ctypes.c_float)]
         L.distr_attn_set_stream.argtypes = [vp]
@@ -300,3 +343,232 @@ def distr_attn_release():
 
 def distr_attn_version():
     return lib().distr_attn_version().decode()
+
+
+# ---- around attention: norms and rotation of queries and keys, a cache in pages --------------------------
+
+ROPE = {"none": 0, "halves": 1, "neighbours": 2}
+
+
+def _strides(t, what):
+    """Strides of all dimensions but the last, which has to be contiguous; those of a single entry do not matter."""
+    if t.stride(-1) != 1:
+        raise ValueError(f"the channels of {what} must be contiguous")
+    return [s if n > 1 else 0 for n, s in zip(t.shape[:-1], t.stride()[:-1])]
+
+
+def _layout(t):
+    return (t.shape, t.stride(), t.dtype, t.device)
+
+
+def _check_layout(t, like, what):
+    if (t.shape, t.stride(), t.dtype, t.device) != like:
+        raise ValueError(f"params were made for a {what} of another shape, stride, dtype or device")
+
+
+def _check_device(device, *tensors):
+    """All on `device`, the current one (whose stream the call takes)."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError("tensors must be on the GPU")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("tensors must be on one device")
+
+
+def _check_index(t, shape, what):
+    import torch
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int32 of shape {tuple(shape)}")
+
+
+def _fill_rotary(r, d, heads, norm, eps, weights, rope, cos, sin):
+    """weights: (of the queries, of the keys), for `heads` of them."""
+    import torch
+    if rope not in ROPE:
+        raise ValueError(f"rope must be one of {sorted(ROPE)}")
+    r.norm, r.eps = int(bool(norm)), eps
+    given = [(w, h, n) for w, h, n in zip(weights, heads, ("q_weight", "k_weight")) if w is not None]
+    if given and not norm:
+        raise ValueError("weights without norm")
+    if len({(w.dtype, w.dim()) for w, _, _ in given}) > 1:
+        raise ValueError("q_weight and k_weight must share dtype and form")
+    for w, h, name in given:
+        if tuple(w.shape) not in ((d,), (h, d)) or not w.is_contiguous():
+            raise ValueError(f"{name} must be contiguous, [{d}] or [{h}, {d}]")
+        r.weight_dtype, r.weight_heads = _dtype_code(w), int(w.dim() == 2)
+    r.q_weight, r.k_weight = (w.data_ptr() if w is not None else None for w in weights)
+    r.rope = ROPE[rope]
+    if r.rope:
+        for t, name in ((cos, "cos"), (sin, "sin")):
+            if t is None or t.dim() != 2 or t.dtype != torch.float32 or not t.is_contiguous() or t.shape != cos.shape:
+                raise ValueError(f"{name} must be contiguous float32 [positions, rotated channels / 2]")
+        r.n_pos, r.rot_dim = cos.shape[0], 2 * cos.shape[1]
+        r.cos_table, r.sin_table = cos.data_ptr(), sin.data_ptr()
+
+
+def _fill_workspace(p, workspace):
+    _check_buffer(workspace, "workspace", 0)
+    if workspace is not None:
+        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    p.stream = _current_stream().value
+
+
+def make_qk_params(q, k, q_out, k_out, norm=False, eps=1e-6, q_weight=None, k_weight=None, rope="none", cos=None, sin=None,
+                   positions=None, workspace=None):
+    """Parameters of distr_attn_qk_norm_rope and its backward for tensors of these layouts: q, q_out [B, H, N, d], k, k_out
+    [B, Hkv, N, d] (None: queries alone), any strides with contiguous channels (views of one projection, [B, N, heads, d]
+    transposed, outputs in place). norm: RMS norm of each row with eps and the weights ([d], or [heads, d]; None: ones). rope: "none",
+    "halves" (pairs of channels j and j + rotated / 2) or "neighbours" (2 j and 2 j + 1), cos and sin float32
+    [positions, rotated channels / 2]; positions int32 [B, N], None: 0 .. N - 1 in every batch. workspace: scratch of the
+    backward's weight gradients (None: the library's)."""
+    if q.dim() != 4 or q_out.shape != q.shape:
+        raise ValueError("q and q_out must be [B, H, N, d]")
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out go together")
+    B, H, N, d = q.shape
+    if k is not None and (k.dim() != 4 or k_out.shape != k.shape or (k.shape[0], k.shape[2], k.shape[3]) != (B, N, d)):
+        raise ValueError("k and k_out must be [B, Hkv, N, d]")
+    if any(t is not None and t.dtype != q.dtype for t in (q_out, k, k_out)):
+        raise TypeError("q, k, q_out, k_out must share a dtype")
+    _check_device(q.device, q_out, k, k_out, q_weight, k_weight, cos, sin, positions, workspace)
+    p = DaQk()
+    p.B, p.H, p.Hkv, p.N, p.d, p.dtype = B, H, 0 if k is None else k.shape[1], N, d, _dtype_code(q)
+    p.q_stride[:], p.q_out_stride[:] = _strides(q, "q"), _strides(q_out, "q_out")
+    if k is not None:
+        p.k_stride[:], p.k_out_stride[:] = _strides(k, "k"), _strides(k_out, "k_out")
+    _fill_rotary(p.rotary, d, (H, p.Hkv), norm, eps, (q_weight, k_weight), rope, cos, sin)
+    if positions is not None:
+        _check_index(positions, (B, N), "positions")
+        p.positions = positions.data_ptr()
+    _fill_workspace(p, workspace)
+    p.layouts = {"q": _layout(q), "q_out": _layout(q_out), "k": k if k is None else _layout(k), "k_out": k if k is None else _layout(k_out)}
+    p.weights = {"q": q_weight, "k": k_weight}
+    p.held = (cos, sin, positions, workspace)
+    return p
+
+
+def _check_qk(params, tensors):
+    for t, name in tensors:
+        if params.layouts[name] is None or t is None:
+            if params.layouts[name] is not t:
+                raise ValueError("params were made with keys, or without")
+            continue
+        _check_layout(t, params.layouts[name], name)
+
+
+def distr_attn_qk_norm_rope(q, k, q_out, k_out, params):
+    """q_out, k_out = rotation(norm(q)), rotation(norm(k)), in one launch. -> (q_out, k_out)"""
+    _check_qk(params, ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")))
+    _check(lib().distr_attn_qk_norm_rope(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), ctypes.byref(params)))
+    return q_out, k_out
+
+
+def distr_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, params, dq_weight=None, dk_weight=None):
+    """Gradient of distr_attn_qk_norm_rope: dq, dk (laid out like q, k) from dq_out, dk_out (like q_out, k_out) and the forward's
+    inputs; dq_weight, dk_weight float32 in the weights' shapes ([d] where there is none), or None. -> (dq, dk)"""
+    import torch
+    _check_qk(params, ((q, "q"), (k, "k"), (dq_out, "q_out"), (dk_out, "k_out"), (dq, "q"), (dk, "k")))
+    for t, of in ((dq_weight, "q"), (dk_weight, "k")):
+        if t is None:
+            continue
+        if of == "k" and params.Hkv == 0:
+            raise ValueError("dk_weight without keys")
+        w = params.weights[of]
+        shape = (params.H if of == "q" else params.Hkv, params.d) if params.rotary.weight_heads else (params.d,)
+        if t.dtype != torch.float32 or tuple(t.shape) != (tuple(w.shape) if w is not None else shape) or not t.is_contiguous() or t.device != dq.device:
+            raise ValueError(f"d{of}_weight must be contiguous float32 of the weight's shape")
+    _check(lib().distr_attn_qk_norm_rope_bwd(_ptr(q), _ptr(k), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight),
+                                             ctypes.byref(params)))
+    return dq, dk
+
+
+def distr_attn_qk_bwd_workspace_bytes(params):
+    return int(lib().distr_attn_qk_bwd_workspace_bytes(ctypes.byref(params)))
+
+
+def make_paged_params(k_pages, v_pages, page_table, kv_len, q_start, q=None, k=None, v=None, causal=True, softmax_scale=0.0,
+                      lse_out=None, norm=False, eps=1e-6, k_weight=None, rope="none", cos=None, sin=None, positions=None, workspace=None):
+    """Parameters of distr_attn_cache_append (k, v given) and distr_attn_paged_fwd (q given) for a batch of sequences in one
+    cache. k_pages, v_pages: [pages, Hkv, page size, d], any strides with contiguous channels (a transposed view where
+    the tokens lie outside the heads). page_table int32 [sequences, pages of the longest], kv_len int32 [sequences]: tokens with the new
+    ones, q_start int32 [sequences + 1]: the new tokens of sequence s are rows q_start[s] .. q_start[s + 1] - 1 of q
+    [tokens, H, d] and of k, v [tokens, Hkv, d]. The three are read on the device by each call: a program writes
+    the next step's into them and calls again. norm, rope and the rest: of the keys on their way into the cache, as in make_qk_params (positions
+    int32 [tokens]; None: a token's place in its sequence). lse_out: float32 [tokens, H]. workspace: of
+    distr_attn_paged_workspace_bytes, which a captured call needs for the keys of a row to be dealt out to several workgroups."""
+    import torch
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or _strides(k_pages, "k_pages") != _strides(v_pages, "v_pages"):
+        raise ValueError("k_pages and v_pages must be [pages, Hkv, page size, d] of the same strides")
+    n_pages, Hkv, page_size, d = k_pages.shape
+    new = [t for t in (q, k, v) if t is not None]
+    if not new or (k is None) != (v is None):
+        raise ValueError("q, or k and v, must be given")
+    if any(t.dim() != 3 or t.shape[2] != d or t.shape[0] != new[0].shape[0] for t in new) or any(t.shape[1] != Hkv for t in (k, v) if t is not None):
+        raise ValueError("q must be [tokens, H, d]; k, v [tokens, Hkv, d]")
+    if any(t.dtype != k_pages.dtype for t in (v_pages, *new)):
+        raise TypeError("q, k, v and the pages must share a dtype")
+    if page_table.dim() != 2 or kv_len.dim() != 1:
+        raise ValueError("page_table must be [sequences, pages], kv_len [sequences]")
+    _check_device(k_pages.device, v_pages, page_table, kv_len, q_start, *new, lse_out, k_weight, cos, sin, positions, workspace)
+    n_seq, n_tokens = kv_len.shape[0], new[0].shape[0]
+    _check_index(page_table, (n_seq, page_table.shape[1]), "page_table")
+    _check_index(kv_len, (n_seq,), "kv_len")
+    _check_index(q_start, (n_seq + 1,), "q_start")
+    p = DaPaged()
+    p.H, p.Hkv, p.d, p.dtype = q.shape[1] if q is not None else Hkv, Hkv, d, _dtype_code(k_pages)
+    p.n_seq, p.n_tokens = n_seq, n_tokens
+    p.n_pages, p.page_size, p.max_pages = n_pages, page_size, page_table.shape[1]
+    p.page_stride, p.head_stride, p.row_stride = _strides(k_pages, "k_pages")
+    p.page_table, p.kv_len, p.q_start = page_table.data_ptr(), kv_len.data_ptr(), q_start.data_ptr()
+    for t, field in ((q, p.q_stride), (k, p.k_stride), (v, p.v_stride)):
+        if t is not None:
+            field[:] = _strides(t, "q, k, v")
+    _fill_rotary(p.rotary, d, (p.H, Hkv), norm, eps, (None, k_weight), rope, cos, sin)
+    if positions is not None:
+        _check_index(positions, (n_tokens,), "positions")
+        p.positions = positions.data_ptr()
+    p.causal, p.softmax_scale = int(bool(causal)), softmax_scale
+    if lse_out is not None:
+        if lse_out.dtype != torch.float32 or q is None or tuple(lse_out.shape) != tuple(q.shape[:2]) or not lse_out.is_contiguous():
+            raise ValueError("lse_out must be contiguous float32 [tokens, H]")
+        p.lse_out = lse_out.data_ptr()
+    _fill_workspace(p, workspace)
+    p.layouts = {"pages": _layout(k_pages), "q": q if q is None else _layout(q), "k": k if k is None else _layout(k), "v": v if v is None else _layout(v)}
+    p.held = (page_table, kv_len, q_start, lse_out, k_weight, cos, sin, positions, workspace)
+    return p
+
+
+def _check_pages(k_pages, v_pages, params):
+    like = params.layouts["pages"]
+    if _layout(k_pages) != like or _layout(v_pages) != like:
+        raise ValueError("params were made for pages of another shape, stride, dtype or device")
+
+
+def distr_attn_cache_append(k, v, k_pages, v_pages, params):
+    """The new tokens' keys (normed and rotated on the way if params say so) and values into the cache. -> (k_pages, v_pages)"""
+    if params.layouts["k"] is None:
+        raise ValueError("params were made without k and v")
+    _check_layout(k, params.layouts["k"], "k")
+    _check_layout(v, params.layouts["v"], "v")
+    _check_pages(k_pages, v_pages, params)
+    _check(lib().distr_attn_cache_append(_ptr(k), _ptr(v), _ptr(k_pages), _ptr(v_pages), ctypes.byref(params)))
+    return k_pages, v_pages
+
+
+def distr_attn_paged_fwd(q, k_pages, v_pages, o, params):
+    """Exact attention of the new tokens over the cache, their own keys in it: o [tokens, H, d], contiguous."""
+    if params.layouts["q"] is None:
+        raise ValueError("params were made without q")
+    _check_layout(q, params.layouts["q"], "q")
+    if o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or not o.is_contiguous():
+        raise ValueError("o must be contiguous, of q's shape and dtype, on its device")
+    _check_pages(k_pages, v_pages, params)
+    _check(lib().distr_attn_paged_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(o), ctypes.byref(params)))
+    return o
+
+
+def distr_attn_paged_workspace_bytes(params):
+    return int(lib().distr_attn_paged_workspace_bytes(ctypes.byref(params)))

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "da_common.h"
+#include "paged.h"
 #include "share_pool.h"
 
 namespace {
@@ -468,6 +469,121 @@ int attention_bwd(const void* q, const void* k, const void* v, const void* o, co
                       "backward launch", r.stream);
 }
 
+// ---- around attention: norms and rotation, paged cache ------------------------------------------------
+
+hipStream_t stream_of(void* stream) { return (hipStream_t)(stream ? stream : g_stream.load()); }
+
+int check_shape(int d, int dtype) {
+  if (dtype != DA_BF16 && dtype != DA_F32) return fail(DA_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (d <= 0) return fail(DA_ERR_INVALID_ARG, "d must be positive");
+  if (d != 64 && d != 128) return fail(DA_ERR_UNSUPPORTED, "d = %d: kernels are built for d in {64, 128}", d);
+  return DA_OK;
+}
+
+int check_rotary(const da_rotary& r, int d) {
+  if (r.norm != 0 && r.norm != 1) return fail(DA_ERR_INVALID_ARG, "norm must be 0 or 1");
+  if (r.norm) {
+    if (!(r.eps >= 0.0f) || !std::isfinite(r.eps)) return fail(DA_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (r.weight_dtype != DA_BF16 && r.weight_dtype != DA_F32) return fail(DA_ERR_INVALID_ARG, "unknown weight dtype %d", r.weight_dtype);
+    if (r.weight_heads != 0 && r.weight_heads != 1) return fail(DA_ERR_INVALID_ARG, "weight_heads must be 0 or 1");
+    if (!aligned16(r.q_weight) || !aligned16(r.k_weight)) return fail(DA_ERR_INVALID_ARG, "weights must be 16-byte aligned");
+  }
+  if (r.rope != DA_ROPE_NONE && r.rope != DA_ROPE_HALVES && r.rope != DA_ROPE_NEIGHBOURS) return fail(DA_ERR_INVALID_ARG, "unknown rope %d", r.rope);
+  if (r.rope != DA_ROPE_NONE) {
+    if (r.rot_dim < 16 || r.rot_dim > d || r.rot_dim % 16 != 0)
+      return fail(DA_ERR_INVALID_ARG, "rot_dim = %d: a multiple of 16 up to d = %d", r.rot_dim, d);
+    if (r.n_pos <= 0) return fail(DA_ERR_INVALID_ARG, "n_pos must be positive");
+    if (!r.cos_table || !r.sin_table || !aligned16(r.cos_table) || !aligned16(r.sin_table))
+      return fail(DA_ERR_INVALID_ARG, "cos_table and sin_table must be non-null and 16-byte aligned");
+  }
+  return DA_OK;
+}
+
+// `sizes` of the dimensions that the strides belong to. Rows that are written must not lie in each other.
+int check_strides(const int64_t* stride, const int* sizes, int n, int d, int dtype, bool written, const char* what) {
+  const int unit = dtype == DA_BF16 ? 8 : 4;
+  for (int i = 0; i < n; ++i) {
+    if (sizes[i] <= 1) continue;   // (never taken)
+    if (stride[i] < 0 || stride[i] % unit != 0 || stride[i] > (int64_t)1 << 40)
+      return fail(DA_ERR_INVALID_ARG, "strides of %s must be multiples of 16 bytes, not negative", what);
+    if (written && stride[i] < d) return fail(DA_ERR_INVALID_ARG, "strides of %s, which is written, must be at least d", what);
+  }
+  return DA_OK;
+}
+
+int check_qk(const da_qk* p, bool backward) {
+  if (!p) return fail(DA_ERR_INVALID_ARG, "params is null");
+  int rc = check_shape(p->d, p->dtype);
+  if (rc) return rc;
+  if (p->B <= 0 || p->H <= 0 || p->Hkv < 0 || p->N <= 0) return fail(DA_ERR_INVALID_ARG, "B, H, N must be positive, Hkv not negative");
+  rc = check_rotary(p->rotary, p->d);
+  if (rc) return rc;
+  if ((long long)p->B * p->N > 0x7fffffffLL / 64 || ((long long)p->B * p->N + 31) / 32 * (p->H + (long long)p->Hkv) > 0x7fffffffLL)
+    return fail(DA_ERR_UNSUPPORTED, "too many rows");
+  const int nq[] = {p->B, p->H, p->N}, nk[] = {p->B, p->Hkv, p->N};
+  rc = check_strides(p->q_stride, nq, 3, p->d, p->dtype, backward, "q");
+  if (!rc) rc = check_strides(p->q_out_stride, nq, 3, p->d, p->dtype, !backward, "q_out");
+  if (!rc && p->Hkv) rc = check_strides(p->k_stride, nk, 3, p->d, p->dtype, backward, "k");
+  if (!rc && p->Hkv) rc = check_strides(p->k_out_stride, nk, 3, p->d, p->dtype, !backward, "k_out");
+  if (!rc && ((uintptr_t)p->positions & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+  return rc;
+}
+
+da::QkProblem qk_problem(const da_qk* p) {
+  da::QkProblem r = {};
+  r.B = p->B;
+  r.N = p->N;
+  r.d = p->d;
+  r.dtype = p->dtype;
+  r.heads[0] = p->H;
+  r.heads[1] = p->Hkv;
+  for (int i = 0; i < 3; ++i) {
+    r.in_stride[0][i] = p->q_stride[i];
+    r.in_stride[1][i] = p->k_stride[i];
+    r.out_stride[0][i] = p->q_out_stride[i];
+    r.out_stride[1][i] = p->k_out_stride[i];
+  }
+  r.weight[0] = p->rotary.norm ? p->rotary.q_weight : nullptr;
+  r.weight[1] = p->rotary.norm ? p->rotary.k_weight : nullptr;
+  r.rotary = p->rotary;
+  r.positions = p->positions;
+  return r;
+}
+
+// A tensor that is written in the place of one that is read: by the same strides, or not at all.
+int check_in_place(const void* in, const void* out, const int64_t* in_stride, const int64_t* out_stride, const int* sizes, const char* what) {
+  if (in != out) return DA_OK;
+  for (int i = 0; i < 3; ++i)
+    if (sizes[i] > 1 && in_stride[i] != out_stride[i]) return fail(DA_ERR_INVALID_ARG, "%s in place needs the same strides", what);
+  return DA_OK;
+}
+
+int check_paged(const da_paged* p) {
+  if (!p) return fail(DA_ERR_INVALID_ARG, "params is null");
+  int rc = check_shape(p->d, p->dtype);
+  if (rc) return rc;
+  if (p->H <= 0 || p->Hkv <= 0 || p->n_seq <= 0 || p->n_tokens < 0) return fail(DA_ERR_INVALID_ARG, "H, Hkv, n_seq must be positive, n_tokens not negative");
+  if (p->H % p->Hkv != 0) return fail(DA_ERR_INVALID_ARG, "H (%d) is not a multiple of Hkv (%d)", p->H, p->Hkv);
+  if (p->n_pages <= 0 || p->page_size <= 0 || p->max_pages <= 0) return fail(DA_ERR_INVALID_ARG, "n_pages, page_size, max_pages must be positive");
+  if (p->page_size % 16 != 0) return fail(DA_ERR_UNSUPPORTED, "page_size = %d: pages of a multiple of 16 tokens", p->page_size);
+  if ((long long)p->max_pages * p->page_size > 1LL << 30) return fail(DA_ERR_UNSUPPORTED, "more than 2^30 tokens in a row of page_table");
+  const int sizes[] = {p->n_pages, p->Hkv, p->page_size};
+  const int64_t strides[] = {p->page_stride, p->head_stride, p->row_stride};
+  rc = check_strides(strides, sizes, 3, p->d, p->dtype, true, "k_pages and v_pages");
+  if (rc) return rc;
+  if (p->row_stride > 1 << 25) return fail(DA_ERR_UNSUPPORTED, "row_stride of more than 2^25 elements");
+  if (!p->page_table || !p->kv_len || !p->q_start) return fail(DA_ERR_INVALID_ARG, "page_table, kv_len, q_start must be non-null");
+  if ((((uintptr_t)p->page_table | (uintptr_t)p->kv_len | (uintptr_t)p->q_start) & 3u) != 0)
+    return fail(DA_ERR_INVALID_ARG, "page_table, kv_len, q_start must be 4-byte aligned");
+  const int keys = 32, rows = 32;   // the smallest tile and unit of the kernels
+  const double units = (double)p->n_tokens * (p->H / p->Hkv) / rows + p->n_seq;
+  if (units * ((double)p->max_pages * p->page_size / keys + 1) > 4e9 || units * p->Hkv > 2e9 || (double)p->n_tokens * p->H > 2e9)
+    return fail(DA_ERR_UNSUPPORTED, "too many rows and keys for one call");
+  return DA_OK;
+}
+
+float paged_scale(const da_paged* p) { return p->softmax_scale == 0.0f ? 1.0f / std::sqrt((float)p->d) : p->softmax_scale; }
+
 da_params short_form(int B, int H, int Hkv, int N, int d, int Br, int Bc, int n_groups, uint64_t seed, int causal) {
   da_params p = {};
   p.B = B; p.H = H; p.Hkv = Hkv; p.N = N; p.d = d; p.Br = Br; p.Bc = Bc;
@@ -567,6 +683,121 @@ int distr_attn_hyperplanes(uint64_t seed, int n_planes, int Br, float* host_out)
     for (int r = 0; r < Br; ++r)
       host_out[(size_t)p * Br + r] = da::hyperplane_entry(seed, (uint32_t)p, (uint32_t)r);
   return DA_OK;
+}
+
+int distr_attn_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out, const da_qk* p) {
+  int rc = check_qk(p, false);
+  if (rc) return rc;
+  if (!q || !q_out || !aligned16(q) || !aligned16(q_out)) return fail(DA_ERR_INVALID_ARG, "q, q_out must be non-null and 16-byte aligned");
+  if (p->Hkv == 0 ? k || k_out : !k || !k_out || !aligned16(k) || !aligned16(k_out))
+    return fail(DA_ERR_INVALID_ARG, "k, k_out must be non-null and 16-byte aligned (null with Hkv = 0)");
+  if (q_out == k || q_out == k_out || (k_out && k_out == q)) return fail(DA_ERR_INVALID_ARG, "q_out and k_out must not alias each other or the other input");
+  const int nq[] = {p->B, p->H, p->N}, nk[] = {p->B, p->Hkv, p->N};
+  rc = check_in_place(q, q_out, p->q_stride, p->q_out_stride, nq, "q");
+  if (!rc && p->Hkv) rc = check_in_place(k, k_out, p->k_stride, p->k_out_stride, nk, "k");
+  if (rc) return rc;
+  da::QkProblem r = qk_problem(p);
+  r.x[0] = q;
+  r.x[1] = k;
+  r.y[0] = q_out;
+  r.y[1] = k_out;
+  const hipStream_t stream = stream_of(p->stream);
+  return check_launch(da::launch_qk_forward(r, stream), "query/key norm and rotation launch", stream);
+}
+
+size_t distr_attn_qk_bwd_workspace_bytes(const da_qk* p) {
+  if (check_qk(p, true)) return 0;
+  return da::qk_backward_scratch_bytes(qk_problem(p));
+}
+
+int distr_attn_qk_norm_rope_bwd(const void* q, const void* k, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
+                                float* dk_weight, const da_qk* p) {
+  int rc = check_qk(p, true);
+  if (rc) return rc;
+  const bool norm = p->rotary.norm != 0, keys = p->Hkv != 0;
+  if (!dq_out || !dq || !aligned16(dq_out) || !aligned16(dq)) return fail(DA_ERR_INVALID_ARG, "dq_out, dq must be non-null and 16-byte aligned");
+  if (keys ? !dk_out || !dk || !aligned16(dk_out) || !aligned16(dk) : dk_out || dk || dk_weight)
+    return fail(DA_ERR_INVALID_ARG, "dk_out, dk must be non-null and 16-byte aligned (null with Hkv = 0)");
+  if (norm && (!q || !aligned16(q) || (keys && (!k || !aligned16(k)))))
+    return fail(DA_ERR_INVALID_ARG, "q, k must be non-null and 16-byte aligned where norm = 1");
+  if (!norm && (dq_weight || dk_weight)) return fail(DA_ERR_INVALID_ARG, "weight gradients without a norm");
+  if (((uintptr_t)dq_weight & 3u) != 0 || ((uintptr_t)dk_weight & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "dq_weight, dk_weight must be 4-byte aligned");
+  if (dq == q || dq == dk || dq == dk_out || (keys && (dk == k || dk == dq_out))) return fail(DA_ERR_INVALID_ARG, "dq and dk must not alias q, k or each other's gradients");
+  const int nq[] = {p->B, p->H, p->N}, nk[] = {p->B, p->Hkv, p->N};
+  rc = check_in_place(dq_out, dq, p->q_out_stride, p->q_stride, nq, "dq");
+  if (!rc && keys) rc = check_in_place(dk_out, dk, p->k_out_stride, p->k_stride, nk, "dk");
+  if (rc) return rc;
+  da::QkProblem r = qk_problem(p);
+  r.x[0] = q;
+  r.x[1] = k;
+  r.g[0] = dq_out;
+  r.g[1] = dk_out;
+  r.y[0] = dq;
+  r.y[1] = dk;
+  const hipStream_t stream = stream_of(p->stream);
+  char* part = nullptr;
+  if (dq_weight || dk_weight) {
+    da_params ws = {};
+    ws.workspace = p->workspace;
+    ws.workspace_bytes = p->workspace_bytes;
+    Resolved at = {};
+    at.stream = stream;
+    rc = scratch_base(&ws, at, da::qk_backward_scratch_bytes(r), false, &part);
+    if (rc) return rc;
+  }
+  float* const dweight[2] = {dq_weight, dk_weight};
+  return check_launch(da::launch_qk_backward(r, dweight, (float*)part, stream), "query/key norm and rotation backward launch", stream);
+}
+
+int distr_attn_cache_append(const void* k, const void* v, void* k_pages, void* v_pages, const da_paged* p) {
+  int rc = check_paged(p);
+  if (!rc) rc = check_rotary(p->rotary, p->d);
+  if (rc) return rc;
+  if (p->n_tokens == 0) return DA_OK;
+  if (!k || !v || !k_pages || !v_pages) return fail(DA_ERR_INVALID_ARG, "k, v, k_pages, v_pages must be non-null");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_pages) || !aligned16(v_pages))
+    return fail(DA_ERR_INVALID_ARG, "k, v, k_pages, v_pages must be 16-byte aligned");
+  if (k_pages == v_pages || k_pages == k || k_pages == v || v_pages == k || v_pages == v)
+    return fail(DA_ERR_INVALID_ARG, "k_pages and v_pages must not alias an input or each other");
+  if (((uintptr_t)p->positions & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+  const int sizes[] = {p->n_tokens, p->Hkv};
+  rc = check_strides(p->k_stride, sizes, 2, p->d, p->dtype, false, "k");
+  if (!rc) rc = check_strides(p->v_stride, sizes, 2, p->d, p->dtype, false, "v");
+  if (rc) return rc;
+  const hipStream_t stream = stream_of(p->stream);
+  return check_launch(da::launch_cache_append(k, v, k_pages, v_pages, *p, stream), "cache append launch", stream);
+}
+
+size_t distr_attn_paged_workspace_bytes(const da_paged* p) {
+  if (check_paged(p)) return 0;
+  return da::paged_scratch_bytes(*p);
+}
+
+int distr_attn_paged_fwd(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged* p) {
+  int rc = check_paged(p);
+  if (rc) return rc;
+  if (p->causal != 0 && p->causal != 1) return fail(DA_ERR_INVALID_ARG, "causal must be 0 or 1");
+  const float scale = paged_scale(p);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(DA_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
+  if (p->n_tokens == 0) return DA_OK;
+  rc = check_tensors(q, k_pages, v_pages, o);
+  if (rc) return rc;
+  const int sizes[] = {p->n_tokens, p->H};
+  rc = check_strides(p->q_stride, sizes, 2, p->d, p->dtype, false, "q");
+  if (rc) return rc;
+  if (((uintptr_t)p->lse_out & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
+  if (p->workspace && ((uintptr_t)p->workspace & 255u) != 0) return fail(DA_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  const hipStream_t stream = stream_of(p->stream);
+  void* scratch = p->workspace;
+  size_t bytes = scratch ? p->workspace_bytes : 0;
+  const size_t want = da::paged_scratch_bytes(*p);
+  ShareLease lease;
+  if (!scratch && want) {
+    lease.take(stream);
+    scratch = lease.ptr;
+    bytes = scratch ? kShareBytes : 0;
+  }
+  return check_launch(da::launch_paged(q, k_pages, v_pages, o, *p, scale, scratch, std::min(bytes, want), stream), "paged attention launch", stream);
 }
 
 int distr_attn_set_stream(void* hip_stream) {

@@ -1,0 +1,218 @@
+// Attention of new tokens over a paged cache, float tensors in float arithmetic: the reference-precision form of attn_paged.hip.
+//
+// The same units of 32 rows and ranges of tiles (paged_units.h), four waves that deal 32-key tiles out among themselves. Products by
+// v_mfma_f32_32x32x2_f32, S^T = K Q^T and O^T = V^T P^T, with the contraction dealt out so that a lane's operands are what it can
+// load itself: channel s and s + d / 2 in step s of the first (a lane walks half a row of K), keys acc_row(i, 0 / 1) in step i of the second
+// (where P already is; a lane takes one channel of V rows). Operands come from memory, without LDS: what bounds it are these loads
+// and the float products (1/16 of the bf16 rate).
+#include <cfloat>
+
+#include "f32_tiles.h"
+#include "paged.h"
+#include "paged_units.h"
+
+namespace da {
+
+namespace {
+
+constexpr int kWaves = 4, kThreads = kWaves * 64, kRows = 32;
+
+template <int D>
+__global__ __launch_bounds__(kThreads) void paged_f32_kernel(
+    const float* __restrict__ q, const float* __restrict__ k_pages, const float* __restrict__ v_pages, float* __restrict__ o,
+    const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
+    int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int64_t row_bytes, int64_t q_token,
+    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat) {
+  constexpr int NMB = D / 32, HALF = D / 2;
+  __shared__ __attribute__((aligned(16))) float sums[kWaves][kRows][D + 4];
+  __shared__ f32x2 stat_lds[kWaves][kRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, hh = lane >> 5;
+  const int group = H / Hkv;
+  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
+
+  long long pos = 0, end = 1, per_head = 1, length = 1;
+  if (ranges) {
+    per_head = paged_total<kRows, kTile>(batch);
+    length = paged_range(per_head * Hkv, gridDim.x, least);
+    pos = length * blockIdx.x;
+    end = min(pos + length, per_head * Hkv);
+  }
+  const long long begin = pos;
+  while (pos < end) {
+    PagedUnit u;
+    int head, t0, t1;
+    if (ranges) {
+      head = (int)(pos / per_head);
+      const unsigned at = (unsigned)(pos - head * per_head);
+      if (!paged_find<kRows, kTile, false>(batch, at, &u)) return;
+      t0 = (int)(at - u.first);
+      t1 = (int)min((long long)u.tiles, t0 + (end - pos));
+    } else {
+      head = blockIdx.x % Hkv;
+      if (!paged_find<kRows, kTile, true>(batch, blockIdx.x / Hkv, &u)) return;
+      t0 = 0;
+      t1 = u.tiles;
+    }
+    const bool whole = t0 == 0 && t1 == u.tiles;
+    const bool from_begin = pos == begin;
+    pos += t1 - t0;
+
+    const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);
+    const int token = u.q0 + m_ld / group;
+    const int n_keys = min(u.len, batch.max_keys);
+    const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);
+    const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (min(u.m0 + kRows, u.rows) - 1) / group + 1, 0)) : n_keys;
+    const int all_see = causal ? min(max(u.len - u.nq + u.m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
+    const int t_end = min(t1, (n_seen + kTile - 1) / kTile);
+    const float* q_row = q + token * q_token + (head * group + m_ld % group) * q_head + hh * HALF;
+    float qv[HALF];
+#pragma unroll
+    for (int s = 0; s < HALF; s += 4) {
+      const f32x4 x = *(const f32x4*)(q_row + s);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) qv[s + j] = x[j];
+    }
+    const int* table = page_table + (int64_t)u.seq * max_pages;
+    const char* k_base = (const char*)k_pages + head * head_bytes;
+    const char* v_base = (const char*)v_pages + head * head_bytes;
+
+    f32x16 oacc[NMB];
+#pragma unroll
+    for (int mb = 0; mb < NMB; ++mb) zero(oacc[mb]);
+    float ref = -FLT_MAX, l_run = 0.0f;
+    PageWindow window = page_window(table, (t0 + wave) * kTile + lq, n_seen, page_size, n_pages, page_bytes, row_bytes);
+    for (int t = t0 + wave; t < t_end; t += kWaves) {
+      const PageWindow mine = window;   // of key t * 32 + lq
+      const uint64_t off = mine.lo | (uint64_t)mine.hi << 32;
+      window = page_window(table, (t + kWaves) * kTile + lq, n_seen, page_size, n_pages, page_bytes, row_bytes);
+      const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(mine.there != 0);
+      ChannelSum<HALF> chain;
+#pragma unroll
+      for (int s = 0; s < HALF; s += 4) {
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (mine.there) x = *(const f32x4*)(k_base + off + (hh * HALF + s) * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) chain.step(s + j, x[j], qv[s + j]);
+      }
+      f32x16 sc = chain.sum();
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (t * kTile + acc_row(i, hh) > lim || !(there >> acc_row(i, hh) & 1)) sc[i] = -INFINITY;
+      float mx = sc[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+      const float ref_new = fmaxf(ref, half_swap_max(mx));
+      if (__builtin_amdgcn_ballot_w64(ref_new > ref) != 0) {
+        const float alpha = __builtin_amdgcn_exp2f((ref - ref_new) * scale_log2e);
+        l_run *= alpha;
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+        ref = ref_new;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[i] = __builtin_amdgcn_exp2f((sc[i] - ref) * scale_log2e);
+        l_run += sc[i];
+      }
+      auto v_rows = [&](auto take) {   // take(i, mb, value of key acc_row(i, hh), channel 32 mb + lq)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int from = acc_row(i, hh) << 2;
+          const uint64_t row = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)mine.lo) | (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)mine.hi) << 32;
+          const bool is = there >> acc_row(i, hh) & 1;
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb) take(i, mb, is ? *(const float*)(v_base + row + (32 * mb + lq) * 4) : 0.0f);
+        }
+      };
+      bool odd = false;
+      if (t * kTile + kTile > all_see) v_rows([&](int, int, float x) { odd |= !(__builtin_fabsf(x) < INFINITY); });
+      if (__builtin_amdgcn_ballot_w64(odd) == 0) {
+        v_rows([&](int i, int mb, float x) { oacc[mb] = mfma(x, sc[i], oacc[mb]); });
+        continue;
+      }
+      // An infinity or a NaN among values that not every row sees: it must not reach the rows with P = 0 (0 times it). The finite
+      // values, then the weight with which a row sees either infinity or a NaN.
+#pragma unroll 1
+      for (int kind = 0; kind < 4; ++kind) {
+        f32x16 z[NMB];
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) z[mb][i] = kind == 0 ? oacc[mb][i] : 0.0f;
+        v_rows([&](int i, int mb, float x) {
+          const int is = __builtin_fabsf(x) < INFINITY ? 0 : x != x ? 3 : x < 0.0f ? 2 : 1;
+          z[mb] = mfma(is != kind ? 0.0f : kind == 0 ? x : 1.0f, sc[i], z[mb]);
+        });
+        const float what = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : __builtin_nanf("");
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mb][i] = kind == 0 ? z[mb][i] : oacc[mb][i] + (z[mb][i] > 0.0f ? what : 0.0f);
+      }
+    }
+
+    const float l_tot = half_swap_sum(l_run);
+    if (hh == 0) stat_lds[wave][lq] = f32x2{ref, l_tot};
+    __syncthreads();
+    float ref_all = stat_lds[0][lq][0], l_all = 0.0f;
+#pragma unroll
+    for (int j = 1; j < kWaves; ++j) ref_all = fmaxf(ref_all, stat_lds[j][lq][0]);
+#pragma unroll
+    for (int j = 0; j < kWaves; ++j) l_all += stat_lds[j][lq][1] * __builtin_amdgcn_exp2f((stat_lds[j][lq][0] - ref_all) * scale_log2e);
+    const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
+#pragma unroll
+    for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4)
+        *(f32x4*)&sums[wave][lq][32 * mb + 8 * i4 + 4 * hh] =
+            f32x4{oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
+    __syncthreads();
+    const size_t slot = 2 * (size_t)blockIdx.x + (from_begin ? 0 : 1);
+    for (int i = tid; i < kRows * (D / 4); i += kThreads) {
+      const int row = i / (D / 4), c = i % (D / 4) * 4, mr = u.m0 + row;
+      if (mr >= u.rows) continue;
+      f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int j = 0; j < kWaves; ++j) x += *(const f32x4*)&sums[j][row][c];
+      if (whole) *(f32x4*)(o + ((int64_t)(u.q0 + mr / group) * H + head * group + mr % group) * D + c) = x;
+      else *(f32x4*)(part_o + (slot * kRows + row) * D + c) = x;
+    }
+    if (wave == 0 && hh == 0 && m < u.rows) {
+      if (!whole) part_stat[slot * kRows + lq] = f32x4{ref_all * scale_log2e, l_all, l_all, 0.0f};
+      else if (lse) lse[(int64_t)token * H + head * group + m % group] = row_statistic(ref_all * scale_log2e, l_all);
+    }
+    __syncthreads();
+  }
+}
+
+template <int D>
+hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                    const PagedLaunch& l, hipStream_t stream) {
+  const float scale_log2e = scale * 1.4426950408889634f;
+  float* part_o = (float*)scratch;
+  f32x4* part_stat = (f32x4*)((char*)scratch + paged_sum_bytes(l.workgroups, kRows, D));
+  hipLaunchKernelGGL((paged_f32_kernel<D>), dim3((unsigned)l.workgroups), dim3(kThreads), 0, stream, (const float*)q, (const float*)k_pages,
+                     (const float*)v_pages, (float*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.n_pages,
+                     p.page_size, p.max_pages, p.page_stride * 4, p.head_stride * 4, p.row_stride * 4, p.q_stride[0], p.q_stride[1], p.causal,
+                     scale_log2e, l.ranges, l.least, part_o, part_stat);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !l.ranges) return e;
+  hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows, kTile>), dim3((unsigned)(paged_units(p, kRows) * p.Hkv)), dim3(256), 0, stream, part_o,
+                     part_stat, (float*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.max_pages * p.page_size,
+                     l.workgroups, l.least);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_paged_f32(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                            size_t scratch_bytes, hipStream_t stream) {
+  const PagedLaunch l = paged_launch(p, kRows, kTile, 2 * kComputeUnits, scratch_bytes);
+  return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
+                   : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
+}
+
+}  // namespace da
