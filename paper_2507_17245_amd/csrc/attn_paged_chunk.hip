@@ -1,0 +1,441 @@
+// Attention of new tokens over a paged cache, bf16: chunks of a prompt. Work split: paged_units.h.
+//
+// Bound: the matrix products. A unit is 128 query rows of a kv head, all of its query heads together; four wave pairs own 32 rows
+// each, and each wave of a pair walks half of the unit's tiles (64 keys) in buffers of its half's own: two waves per SIMD on one
+// workgroup per compute unit, one exponentiating while the other multiplies. Loop, layouts, online softmax and the exchange of the halves
+// are those of attn_bf16_impl.h. What is new is where tiles come from: a wave loads 16 keys of each tile, which lie in one page, by a
+// scalar base and limit (rows behind the end of the sequence are never read); the table's entries for 64 tiles ahead are
+// held a lane for each, with a bit for each group of 16 keys that lies in the cache.
+#include <cfloat>
+
+#include "attn_bf16_impl.h"
+#include "paged.h"
+#include "paged_tiles.h"
+#include "paged_units.h"
+
+namespace da {
+
+namespace {
+
+constexpr int kChunkRows = 128, kChunkKeys = 64, kRW = 4, kHalves = 2, kChunkThreads = kRW * kHalves * 64;
+
+template <int D, bool STATS>
+__global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
+    const bf16* __restrict__ q, const bf16* __restrict__ k_pages, const bf16* __restrict__ v_pages, bf16* __restrict__ o,
+    const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
+    int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int row_bytes, int64_t q_token,
+    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat) {
+  constexpr int BC = kChunkKeys, ROWB = D * 2, CH = D / 8, TILEB = BC * ROWB;
+  constexpr int MB = BC / 32, TT = BC / 16, KSTEPS = D / 16, NMB = D / 32;
+  constexpr int LPG = 16 * ROWB / 1024;   // direct loads of 16 keys
+  constexpr float kSumTrigger = (BC / 2) * 256.0f;   // (as in attn_bf16_impl.h)
+  __shared__ __attribute__((aligned(1024))) char k_lds0[kHalves * TILEB];
+  __shared__ __attribute__((aligned(1024))) char k_lds1[kHalves * TILEB];
+  __shared__ __attribute__((aligned(1024))) char v_lds0[kHalves * TILEB];
+  __shared__ __attribute__((aligned(1024))) char v_lds1[kHalves * TILEB];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % kRW, half = wave / kRW;
+  const int lq = lane & 31, hh = lane >> 5;
+  const int group = H / Hkv;
+  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
+  auto k_buf = [&](int par) -> char* { return (par ? k_lds1 : k_lds0) + half * TILEB; };
+  auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
+
+  // lanes' places in the loads of 16 keys, and in the operands
+  int dma_k[LPG], dma_v[LPG];
+#pragma unroll
+  for (int j = 0; j < LPG; ++j) {
+    const int slot = j * 64 + lane, row = slot / CH, pc = slot % CH;
+    dma_k[j] = row * row_bytes + (pc ^ (D == 128 ? (row & 15) : ((row >> 1) & 7))) * 16;
+    dma_v[j] = row * row_bytes + ((((pc >> 1) ^ v_swizzle<ROWB>(row)) << 1) | (pc & 1)) * 16;
+  }
+  int ka_off[KSTEPS], va_off[NMB];
+#pragma unroll
+  for (int s = 0; s < KSTEPS; ++s) ka_off[s] = lq * ROWB + ((2 * s + hh) ^ (D == 128 ? (lq & 15) : ((lq >> 1) & 7))) * 16;
+  {
+    const int row_l = 4 * hh + ((lane & 15) >> 2);
+#pragma unroll
+    for (int mb = 0; mb < NMB; ++mb)
+      va_off[mb] = row_l * ROWB + ((2 * mb + ((lane >> 4) & 1)) ^ v_swizzle<ROWB>(row_l)) * 32 + 8 * (lane & 3);
+  }
+
+  long long pos = 0, end = 1, per_head = 1, length = 1;
+  int wg = blockIdx.x;
+  if (ranges) {
+    // Ranges that follow each other on one XCD: their units read the same keys.
+    if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
+    per_head = paged_total<kChunkRows, BC>(batch);
+    length = paged_range(per_head * Hkv, gridDim.x, least);
+    pos = length * wg;
+    end = min(pos + length, per_head * Hkv);
+  }
+  const long long begin = pos;
+  while (pos < end) {
+    PagedUnit u;
+    int head, t0, t1;
+    if (ranges) {
+      head = (int)(pos / per_head);
+      const unsigned at = (unsigned)(pos - head * per_head);
+      if (!paged_find<kChunkRows, BC, false>(batch, at, &u)) return;
+      t0 = (int)(at - u.first);
+      t1 = (int)min((long long)u.tiles, t0 + (end - pos));
+    } else {
+      // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
+      head = wg % Hkv;
+      if (!paged_find<kChunkRows, BC, true>(batch, wg / Hkv, &u)) return;
+      u.m0 = (u.rows - 1) / kChunkRows * kChunkRows - u.m0;
+      t0 = 0;
+      t1 = u.tiles;
+    }
+    const bool whole = t0 == 0 && t1 == u.tiles;
+    const bool from_begin = pos == begin;
+    pos += t1 - t0;
+
+    const int m = u.m0 + rw * 32 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
+    const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
+    const int n_keys = min(u.len, batch.max_keys);
+    const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
+    const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (min(u.m0 + kChunkRows, u.rows) - 1) / group + 1, 0)) : n_keys;   // no row sees more
+    const int all_see = causal ? min(max(u.len - u.nq + u.m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
+    const int seen_tiles = (n_seen + BC - 1) / BC;
+    // the halves' tiles; a half without any walks one behind the last key: zeros, masked out
+    const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + 1) / 2, 1);
+    const int n_tiles = half ? max(n_all - n_most, 1) : n_most;
+    const int tile0 = half ? (n_all > 1 ? t0 + n_most : seen_tiles) : (n_all > 0 ? t0 : seen_tiles);
+    const bool idle = u.m0 + rw * 32 >= u.rows;   // a wave without rows brings its part of the tiles in
+
+    bf16x8 qop[KSTEPS];
+    {
+      const bf16* q_row = q + token * q_token + q_of * q_head;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
+    }
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
+
+    const int* table = page_table + (int64_t)u.seq * max_pages;
+    const char* k_base = (const char*)k_pages + head * head_bytes;
+    const char* v_base = (const char*)v_pages + head * head_bytes;
+    // Lane i: where the wave's 16 keys of tile (first + i) of the half lie, and which of the tile's groups lie in the cache.
+    struct Window {
+      uint32_t lo, hi;
+      int there;
+    };
+    auto window_of = [&](int first) {
+      Window w = {0, 0, 0};
+      const int key = (tile0 + first + lane) * BC;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const PageWindow p = page_window(table, key + 16 * g, n_seen, page_size, n_pages, page_bytes, row_bytes);
+        w.there |= p.there << g;
+        if (g == rw) {
+          w.lo = p.lo;
+          w.hi = p.hi;
+        }
+      }
+      return w;
+    };
+    int base = 0;
+    Window now = window_of(0), next = window_of(64);
+    auto advance = [&](int it) {   // tiles before `it` are done with
+      if (it < base + 64) return;
+      base += 64;
+      now = next;
+      next = window_of(base + 64);
+    };
+    auto there_of = [&](int it) {
+      const int i = it - base;
+      return i < 64 ? __builtin_amdgcn_readlane(now.there, i) : __builtin_amdgcn_readlane(next.there, i - 64);
+    };
+    auto load_group = [&](const char* from, const int (&places)[LPG], int it, char* to) {
+      const int i = it - base, l = i & 63;
+      const bool ahead = i >= 64;
+      const uint32_t lo = (uint32_t)(ahead ? __builtin_amdgcn_readlane((int)next.lo, l) : __builtin_amdgcn_readlane((int)now.lo, l));
+      const uint32_t hi = (uint32_t)(ahead ? __builtin_amdgcn_readlane((int)next.hi, l) : __builtin_amdgcn_readlane((int)now.hi, l));
+      const int is = (ahead ? __builtin_amdgcn_readlane(next.there, l) : __builtin_amdgcn_readlane(now.there, l)) >> rw & 1;
+      const int rows = min(n_seen - ((tile0 + it) * BC + 16 * rw), 16);
+      const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
+#pragma unroll
+      for (int j = 0; j < LPG; ++j) load_lds(from + (lo | (uint64_t)hi << 32), bytes, places[j], to + (rw * LPG + j) * 1024);
+    };
+    // What tile `it` brings in: K(it + 2) where K(it) was, V(it + 1) where V(it - 1) was.
+    auto feed = [&](int it, int par) {
+      if (it + 2 < n_tiles) load_group(k_base, dma_k, it + 2, k_buf(par));
+      load_group(v_base, dma_v, it + 1, v_buf(par ^ 1));
+    };
+    auto dma_wait = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+    auto masked = [&](int it) { return (tile0 + it) * BC + BC > all_see || there_of(it) != 15; };
+
+    f32x16 oacc[NMB];
+#pragma unroll
+    for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
+    float nref = 0.0f, l_run = 0.0f, e_run = 0.0f;   // negated reference (exp2 domain), sums over this lane's half of the keys
+    // Below zero until the row has met a score above -infinity: its first one becomes the reference.
+    float trigger = kSumTrigger;
+
+    auto qk = [&](int par, f32x16 (&sacc)[MB]) {
+      const char* at = k_buf(par);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sacc[mb][i] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) sacc[mb] = mfma_32x32x16(*(const bf16x8*)(at + ka_off[s] + mb * 32 * ROWB), qop[s], sacc[mb]);
+      }
+    };
+    auto apply_mask = [&](int it, f32x16 (&sc)[MB]) {
+      const int there = there_of(it);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if ((tile0 + it) * BC + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(there >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
+    };
+    auto tile_max = [&](const f32x16 (&sc)[MB]) -> float {
+      float mt = sc[0][0];
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[mb][i]);
+      return __builtin_fmaf(half_swap_max(mt), scale_log2e, nref);
+    };
+    auto exp_tile = [&](const f32x16 (&sc)[MB], bf16x8 (&pop)[TT]) -> float {   // -> sum before rounding, with STATS
+      float sum = 0.0f;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], scale_log2e, nref));
+          const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i + 1], scale_log2e, nref));
+          const bf16x2 pr = {(bf16)x0, (bf16)x1};
+          pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
+          pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
+          if constexpr (STATS) sum += x0 + x1;
+        }
+      return sum;
+    };
+    const RowSum row_sum(lane);
+    auto shift_reference = [&](float delta) {
+      nref -= delta;
+      const float alpha = __builtin_amdgcn_exp2f(fminf(-delta, 0.0f));   // (a first reference has no sums)
+      l_run *= alpha;
+      if constexpr (STATS) e_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+    };
+    // One tile, as in attn_bf16_impl.h. clean_c: neither it nor the next needs the mask.
+    auto body = [&](auto clean_c, auto next_c, int it, int par, f32x16 (&sc)[MB], f32x16 (&sn)[MB]) {
+      constexpr bool CLEAN = decltype(clean_c)::value, HAS_NEXT = decltype(next_c)::value;
+      if constexpr (HAS_NEXT) {
+        feed(it, par);
+        qk(par ^ 1, sn);
+      }
+      bf16x8 pop[TT];
+      float es = exp_tile(sc, pop);
+      float rs = row_sum(pop);
+      if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
+        const float mt = tile_max(sc);
+        const bool first = trigger < 0.0f && mt > -INFINITY;
+        if (first) trigger = kSumTrigger;
+        shift_reference(mt > kTau || first ? mt : 0.0f);
+        es = exp_tile(sc, pop);
+        rs = RowSum::by_lanes(pop);
+      }
+      l_run += rs;
+      if constexpr (STATS) e_run += es;
+      const char* vb = v_buf(par);
+      auto v_operand = [&](int tt, int mb) {
+        const char* p0 = vb + va_off[mb] + 16 * tt * ROWB;
+        return lds_read_tr_pair<bf16x8>(p0, p0 + 8 * ROWB);
+      };
+      bool odd = false;
+      if constexpr (!CLEAN) {
+        if (masked(it)) {
+#pragma unroll
+          for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) odd |= has_odd(v_operand(tt, mb));
+        }
+      }
+      if (!CLEAN && __builtin_amdgcn_ballot_w64(odd) != 0) {
+        odd_values<TT, NMB>(oacc, pop, v_operand);
+      } else {
+        constexpr int PF = (4 / NMB < TT) ? 4 / NMB : TT - 1;
+        bf16x8 va[PF + 1][NMB];
+#pragma unroll
+        for (int s = 0; s < PF; ++s)
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb) va[s][mb] = v_operand(s, mb);
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt) {
+          if (tt + PF < TT) {
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) va[(tt + PF) % (PF + 1)][mb] = v_operand(tt + PF, mb);
+          }
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(va[tt % (PF + 1)][mb], pop[tt], oacc[mb]);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * NMB * PF, 0);
+#pragma unroll
+        for (int i = 0; i < (TT - PF) * NMB; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, PF * NMB, 0);
+      }
+      if constexpr (HAS_NEXT) {
+        if constexpr (!CLEAN) {
+          if (masked(it + 1)) apply_mask(it + 1, sn);
+        }
+        dma_wait();
+      }
+      __syncthreads();
+    };
+
+    load_group(v_base, dma_v, 0, v_buf(0));
+    load_group(k_base, dma_k, 0, k_buf(0));
+    if (n_tiles > 1) load_group(k_base, dma_k, 1, k_buf(1));
+    dma_wait();
+    __syncthreads();
+    const std::true_type yes;
+    const std::false_type no;
+    if (idle) {
+      __syncthreads();
+      for (int it = 0; it < n_tiles - 1; ++it) {
+        advance(it);
+        feed(it, it & 1);
+        dma_wait();
+        __syncthreads();
+      }
+      __syncthreads();
+    } else {
+      f32x16 s0[MB], s1[MB];
+      qk(0, s0);
+      if (masked(0)) apply_mask(0, s0);
+      const float first_max = tile_max(s0);
+      if (first_max > -INFINITY) nref -= first_max;
+      else trigger = -1.0f;
+      __syncthreads();
+      const int n_full = min(max(all_see / BC - tile0, 0), n_tiles);   // tiles that need no mask for their place
+      int it = 0;
+      while (it < n_tiles - 1) {
+        advance(it);
+        if ((it & 1) == 0) {
+          // clean tiles of the window from `it` on
+          const uint64_t bad = __builtin_amdgcn_ballot_w64(now.there != 15) >> (it - base);
+          const int clean = min(n_full, it + (bad ? __builtin_ctzll(bad) : base + 64 - it));
+          for (; it + 2 < clean; it += 2) {
+            body(yes, yes, it, 0, s0, s1);
+            body(yes, yes, it + 1, 1, s1, s0);
+          }
+          if (it == n_tiles - 1) break;
+        }
+        body(no, yes, it, it & 1, s0, s1);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) s0[mb] = s1[mb];
+        ++it;
+      }
+      advance(it);
+      body(no, no, it, it & 1, s0, s1);
+    }
+    if (n_tiles < n_most) __syncthreads();   // (the other half's last tile)
+
+    // ---- the halves meet: each hands the other one half of the channels and finishes the rest ----------------
+    constexpr int OB = NMB / 2;
+    const int c0 = half * (D / 2);
+    float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
+    static_assert(kRW * OB * 4096 <= kHalves * TILEB && kChunkThreads / 2 * 16 <= kHalves * TILEB, "the exchange fits the tile buffers");
+    f32x4* stat = (f32x4*)k_lds0;
+    f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
+    const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
+    f32x16 out[OB];
+    if (hh == 0) stat[wave * 32 + lq] = f32x4{-nref, l_tot, e_tot, 0.0f};
+#pragma unroll
+    for (int mb = 0; mb < OB; ++mb) {
+      f32x16 theirs;
+      if (half) {
+        theirs = oacc[mb];
+        out[mb] = oacc[mb + OB];
+      } else {
+        theirs = oacc[mb + OB];
+        out[mb] = oacc[mb];
+      }
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) give[(mb * 4 + i4) * 64] = f32x4{theirs[4 * i4], theirs[4 * i4 + 1], theirs[4 * i4 + 2], theirs[4 * i4 + 3]};
+    }
+    __syncthreads();
+    // (a half that saw nothing of a row has sum 0 and no reference; a NaN sum makes the row NaN)
+    const f32x4 st = stat[(wave ^ kRW) * 32 + lq];
+    const float mine_ref = l_tot == 0.0f ? -FLT_MAX : -nref, other_ref = st[1] == 0.0f ? -FLT_MAX : st[0];
+    const float ref = fmaxf(mine_ref, other_ref);
+    const float wm = __builtin_amdgcn_exp2f(mine_ref - ref), wo = __builtin_amdgcn_exp2f(other_ref - ref);
+    l_tot = __builtin_fmaf(wm, l_tot, wo * st[1]);
+    e_tot = __builtin_fmaf(wm, e_tot, wo * st[2]);
+    const float inv = !whole ? 1.0f : l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
+#pragma unroll
+    for (int mb = 0; mb < OB; ++mb)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 x = take[(mb * 4 + i4) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]) * inv;
+      }
+    if (m < u.rows) {
+      const int64_t row = (int64_t)token * H + q_of;
+      const size_t slot = (2 * (size_t)wg + (from_begin ? 0 : 1)) * kChunkRows + rw * 32 + lq;
+      if (hh == 0 && half == 0) {
+        if (!whole) part_stat[slot] = f32x4{ref, l_tot, e_tot, 0.0f};
+        else if (STATS) lse[row] = row_statistic(ref, e_tot);
+      }
+#pragma unroll
+      for (int mb = 0; mb < OB; ++mb)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int c = c0 + 32 * mb + 8 * i4 + 4 * hh;
+          const f32x4 x = {out[mb][4 * i4], out[mb][4 * i4 + 1], out[mb][4 * i4 + 2], out[mb][4 * i4 + 3]};
+          if (whole) *(bf16x4*)(o + row * D + c) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+          else *(f32x4*)(part_o + slot * D + c) = x;
+        }
+    }
+    __syncthreads();   // (the next unit's tiles take the place of the sums)
+  }
+}
+
+template <int D>
+hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                    const PagedLaunch& l, hipStream_t stream) {
+  const float scale_log2e = scale * 1.4426950408889634f;
+  float* part_o = (float*)scratch;
+  f32x4* part_stat = (f32x4*)((char*)scratch + paged_sum_bytes(l.workgroups, kChunkRows, D));
+  hipLaunchKernelGGL((p.lse_out ? paged_chunk_kernel<D, true> : paged_chunk_kernel<D, false>), dim3((unsigned)l.workgroups), dim3(kChunkThreads), 0,
+                     stream, (const bf16*)q, (const bf16*)k_pages, (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H,
+                     p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, p.page_stride * 2, p.head_stride * 2, (int)(p.row_stride * 2),
+                     p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !l.ranges) return e;
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kChunkRows, kChunkKeys>), dim3((unsigned)(paged_units(p, kChunkRows) * p.Hkv)), dim3(256), 0,
+                     stream, part_o, part_stat, (bf16*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens,
+                     p.max_pages * p.page_size, l.workgroups, l.least);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t paged_chunk_scratch_bytes(const da_paged& p) { return paged_launch_bytes(kComputeUnits, kChunkRows, p.d); }
+
+hipError_t launch_paged_chunk(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                              size_t scratch_bytes, hipStream_t stream) {
+  PagedLaunch l = paged_launch(p, kChunkRows, kChunkKeys, kComputeUnits, scratch_bytes);
+  const long long units = (long long)p.n_tokens * (p.H / p.Hkv) / kChunkRows * p.Hkv;   // at least
+  if (units >= 2 * kComputeUnits) l = PagedLaunch{(int)(paged_units(p, kChunkRows) * p.Hkv), 0, l.least};
+  return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
+                   : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
+}
+
+}  // namespace da
