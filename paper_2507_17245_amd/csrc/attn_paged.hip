@@ -69,9 +69,10 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
   }
 
   // this workgroup's range of the line
+  const PagedLine<kFewRows, KT> line(batch);
   long long pos = 0, end = 1, per_head = 1, length = 1;
   if (ranges) {
-    per_head = paged_total<kFewRows, KT>(batch);
+    per_head = line.total;
     length = paged_range(per_head * Hkv, gridDim.x, least);
     pos = length * blockIdx.x;
     end = min(pos + length, per_head * Hkv);
@@ -83,12 +84,12 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
     if (ranges) {
       head = (int)(pos / per_head);
       const unsigned at = (unsigned)(pos - head * per_head);
-      if (!paged_find<kFewRows, KT, false>(batch, at, &u)) return;
+      if (!line.template find<false>(at, &u)) return;
       t0 = (int)(at - u.first);
       t1 = (int)min((long long)u.tiles, t0 + (end - pos));
     } else {
       head = blockIdx.x % Hkv;
-      if (!paged_find<kFewRows, KT, true>(batch, blockIdx.x / Hkv, &u)) return;
+      if (!line.template find<true>(blockIdx.x / Hkv, &u)) return;
       t0 = 0;
       t1 = u.tiles;
     }
@@ -318,7 +319,7 @@ hipError_t launch_few(const void* q, const void* k_pages, const void* v_pages, v
                      p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kFewRows, kFewKeys<D>>), dim3((unsigned)(paged_units(p, kFewRows) * p.Hkv)), dim3(256), 0,
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kFewRows, kFewKeys<D>>), dim3((unsigned)(paged_units(p, kFewRows) * p.Hkv * kCombinePieces<D, kFewRows>)), dim3(256), 0,
                      stream, part_o, part_stat, (bf16*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens,
                      p.max_pages * p.page_size, l.workgroups, l.least);
   return hipGetLastError();

@@ -61,12 +61,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
       va_off[mb] = row_l * ROWB + ((2 * mb + ((lane >> 4) & 1)) ^ v_swizzle<ROWB>(row_l)) * 32 + 8 * (lane & 3);
   }
 
+  const PagedLine<kChunkRows, BC> line(batch);
   long long pos = 0, end = 1, per_head = 1, length = 1;
   int wg = blockIdx.x;
   if (ranges) {
     // Ranges that follow each other on one XCD: their units read the same keys.
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
-    per_head = paged_total<kChunkRows, BC>(batch);
+    per_head = line.total;
     length = paged_range(per_head * Hkv, gridDim.x, least);
     pos = length * wg;
     end = min(pos + length, per_head * Hkv);
@@ -78,13 +79,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
     if (ranges) {
       head = (int)(pos / per_head);
       const unsigned at = (unsigned)(pos - head * per_head);
-      if (!paged_find<kChunkRows, BC, false>(batch, at, &u)) return;
+      if (!line.template find<false>(at, &u)) return;
       t0 = (int)(at - u.first);
       t1 = (int)min((long long)u.tiles, t0 + (end - pos));
     } else {
       // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
       head = wg % Hkv;
-      if (!paged_find<kChunkRows, BC, true>(batch, wg / Hkv, &u)) return;
+      if (!line.template find<true>(wg / Hkv, &u)) return;
       u.m0 = (u.rows - 1) / kChunkRows * kChunkRows - u.m0;
       t0 = 0;
       t1 = u.tiles;
@@ -419,7 +420,7 @@ hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, voi
                      p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kChunkRows, kChunkKeys>), dim3((unsigned)(paged_units(p, kChunkRows) * p.Hkv)), dim3(256), 0,
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kChunkRows, kChunkKeys>), dim3((unsigned)(paged_units(p, kChunkRows) * p.Hkv * kCombinePieces<D, kChunkRows>)), dim3(256), 0,
                      stream, part_o, part_stat, (bf16*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens,
                      p.max_pages * p.page_size, l.workgroups, l.least);
   return hipGetLastError();

@@ -31,9 +31,10 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
   const int group = H / Hkv;
   const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
 
+  const PagedLine<kRows, kTile> line(batch);
   long long pos = 0, end = 1, per_head = 1, length = 1;
   if (ranges) {
-    per_head = paged_total<kRows, kTile>(batch);
+    per_head = line.total;
     length = paged_range(per_head * Hkv, gridDim.x, least);
     pos = length * blockIdx.x;
     end = min(pos + length, per_head * Hkv);
@@ -45,12 +46,12 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
     if (ranges) {
       head = (int)(pos / per_head);
       const unsigned at = (unsigned)(pos - head * per_head);
-      if (!paged_find<kRows, kTile, false>(batch, at, &u)) return;
+      if (!line.template find<false>(at, &u)) return;
       t0 = (int)(at - u.first);
       t1 = (int)min((long long)u.tiles, t0 + (end - pos));
     } else {
       head = blockIdx.x % Hkv;
-      if (!paged_find<kRows, kTile, true>(batch, blockIdx.x / Hkv, &u)) return;
+      if (!line.template find<true>(blockIdx.x / Hkv, &u)) return;
       t0 = 0;
       t1 = u.tiles;
     }
@@ -200,7 +201,7 @@ hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, voi
                      scale_log2e, l.ranges, l.least, part_o, part_stat);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows, kTile>), dim3((unsigned)(paged_units(p, kRows) * p.Hkv)), dim3(256), 0, stream, part_o,
+  hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows, kTile>), dim3((unsigned)(paged_units(p, kRows) * p.Hkv * kCombinePieces<D, kRows>)), dim3(256), 0, stream, part_o,
                      part_stat, (float*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.max_pages * p.page_size,
                      l.workgroups, l.least);
   return hipGetLastError();

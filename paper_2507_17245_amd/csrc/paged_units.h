@@ -35,70 +35,90 @@ struct PagedUnit {
   unsigned first;      // place of the unit's first tile among a kv head's
 };
 
+template <int CTRL, int ROWS>
+__device__ inline unsigned dpp_add(unsigned x) {
+  return x + (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
 __device__ inline unsigned wave_scan(unsigned x) {   // sums over the lanes up to one's own
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const unsigned y = (unsigned)__builtin_amdgcn_ds_bpermute((((threadIdx.x & 63) - d) & 63) << 2, (int)x);
-    if ((int)(threadIdx.x & 63) >= d) x += y;
-  }
-  return x;
+  x = dpp_add<0x111, 0xf>(x);   // row_shr 1, 2, 4, 8: sums within rows of 16 lanes
+  x = dpp_add<0x112, 0xf>(x);
+  x = dpp_add<0x114, 0xf>(x);
+  x = dpp_add<0x118, 0xf>(x);
+  x = dpp_add<0x142, 0xa>(x);   // row_bcast 15: a row's last lane to the next row
+  return dpp_add<0x143, 0xc>(x);   // row_bcast 31: the second row's last lane to the upper two
 }
 
 template <int ROWS, int KEYS>
 struct PagedSequence {   // what a lane knows of its sequence
   int q0, nq, len, units, tiles;
+  unsigned sum, unit_sum;   // tiles and units of the sequences up to it, in its 64
   __device__ PagedSequence(const PagedBatch& b, int s) {
     q0 = nq = len = units = tiles = 0;
-    if (s >= b.n_seq) return;
-    q0 = min(max(b.q_start[s], 0), b.n_tokens);
-    nq = max(min(max(b.q_start[s + 1], 0), b.n_tokens) - q0, 0);
-    len = max(b.kv_len[s], 0);
-    units = (int)(((long long)nq * b.group + ROWS - 1) / ROWS);
-    tiles = max((min(len, b.max_keys) + KEYS - 1) / KEYS, 1);
+    if (s < b.n_seq) {
+      const int at = b.q_start[s], to = b.q_start[s + 1], keys = b.kv_len[s];
+      q0 = min(max(at, 0), b.n_tokens);
+      nq = max(min(max(to, 0), b.n_tokens) - q0, 0);
+      len = max(keys, 0);
+      units = (int)(((unsigned)nq * (unsigned)b.group + (ROWS - 1)) / ROWS);
+      tiles = max((min(len, b.max_keys) + KEYS - 1) / KEYS, 1);
+    }
+    sum = wave_scan((unsigned)units * (unsigned)tiles);
+    unit_sum = wave_scan((unsigned)units);
   }
+  __device__ unsigned all_tiles() const { return (unsigned)__builtin_amdgcn_readlane((int)sum, 63); }
+  __device__ unsigned all_units() const { return (unsigned)__builtin_amdgcn_readlane((int)unit_sum, 63); }
 };
 
-// All tiles of a kv head.
+// The line of a kv head. The first 64 sequences stay in registers, a lane each; others are loaded again where they are asked for.
 template <int ROWS, int KEYS>
-__device__ inline unsigned paged_total(const PagedBatch& b) {
-  unsigned total = 0;
-  for (int s0 = 0; s0 < b.n_seq; s0 += 64) {
-    const PagedSequence<ROWS, KEYS> q(b, s0 + (threadIdx.x & 63));
-    total += (unsigned)__builtin_amdgcn_readlane((int)wave_scan((unsigned)q.units * (unsigned)q.tiles), 63);
+struct PagedLine {
+  typedef PagedSequence<ROWS, KEYS> Sequence;
+  const PagedBatch b;
+  const Sequence head;
+  unsigned total;   // its tiles
+  __device__ explicit PagedLine(const PagedBatch& batch) : b(batch), head(batch, threadIdx.x & 63) {
+    total = head.all_tiles();
+    for (int s0 = 64; s0 < b.n_seq; s0 += 64) total += Sequence(b, s0 + (threadIdx.x & 63)).all_tiles();
   }
-  return total;
-}
-
-// The unit that holds place `x` of a kv head's line (BY_UNIT: its x-th unit); false behind the last one.
-template <int ROWS, int KEYS, bool BY_UNIT>
-__device__ inline bool paged_find(const PagedBatch& b, unsigned x, PagedUnit* out) {
-  unsigned before = 0, tiles_before = 0;
-  for (int s0 = 0; s0 < b.n_seq; s0 += 64) {
-    const PagedSequence<ROWS, KEYS> q(b, s0 + (threadIdx.x & 63));
-    const unsigned w = (unsigned)q.units * (unsigned)q.tiles, sum = wave_scan(w);
-    const unsigned at = BY_UNIT ? wave_scan((unsigned)q.units) : sum;
-    const uint64_t past = __builtin_amdgcn_ballot_w64(before + at > x);
-    if (past != 0) {
-      const int i = __builtin_ctzll(past);
-      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
-      const unsigned in = x - before - (unsigned)of((int)(at - (BY_UNIT ? (unsigned)q.units : w)));
-      const int tiles = of(q.tiles);
-      const int unit = BY_UNIT ? (int)in : (int)(in / (unsigned)tiles);
-      out->seq = s0 + i;
-      out->q0 = of(q.q0);
-      out->nq = of(q.nq);
-      out->len = of(q.len);
-      out->m0 = unit * ROWS;
-      out->rows = out->nq * b.group;
-      out->tiles = tiles;
-      out->first = tiles_before + (unsigned)of((int)(sum - w)) + (unsigned)unit * (unsigned)tiles;
-      return true;
+  // The unit that holds place `x` (BY_UNIT: the x-th unit); false behind the last one.
+  template <bool BY_UNIT>
+  __device__ bool find(unsigned x, PagedUnit* out) const {
+    unsigned before = 0;
+    if (in<BY_UNIT>(head, 0, x, &before, out)) return true;
+    unsigned units = head.all_units();
+    for (int s0 = 64; s0 < b.n_seq; s0 += 64) {
+      const Sequence q(b, s0 + (threadIdx.x & 63));
+      if (in<BY_UNIT>(q, s0, BY_UNIT ? x - units : x, &before, out)) return true;
+      units += q.all_units();
     }
-    before += (unsigned)__builtin_amdgcn_readlane((int)at, 63);
-    tiles_before += (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
+    return false;
   }
-  return false;
-}
+
+ private:
+  template <bool BY_UNIT>
+  __device__ bool in(const Sequence& q, int s0, unsigned x, unsigned* before, PagedUnit* out) const {
+    const unsigned w = (unsigned)q.units * (unsigned)q.tiles;
+    const uint64_t past = __builtin_amdgcn_ballot_w64((BY_UNIT ? q.unit_sum : *before + q.sum) > x);
+    if (past == 0) {
+      *before += q.all_tiles();
+      return false;
+    }
+    const int i = __builtin_ctzll(past);
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
+    const unsigned first = *before + (unsigned)of((int)(q.sum - w));
+    const int tiles = of(q.tiles);
+    const int unit = BY_UNIT ? (int)(x - (unsigned)of((int)(q.unit_sum - (unsigned)q.units))) : (int)((x - first) / (unsigned)tiles);
+    out->seq = s0 + i;
+    out->q0 = of(q.q0);
+    out->nq = of(q.nq);
+    out->len = of(q.len);
+    out->m0 = unit * ROWS;
+    out->rows = out->nq * b.group;
+    out->tiles = tiles;
+    out->first = first + (unsigned)unit * (unsigned)tiles;
+    return true;
+  }
+};
 
 // Length of a range: equal ones for `workgroups` of them, none shorter than `least` tiles.
 __device__ inline long long paged_range(long long total, int workgroups, int least) {
@@ -128,50 +148,60 @@ __device__ inline PageWindow page_window(const int* __restrict__ table, int key,
 // log-sum-exp of a row from its reference (log2 units) and the sum relative to it
 __device__ inline float row_statistic(float ref, float sum) { return sum == 0.0f ? -INFINITY : 0.6931471805599453f * (ref + __builtin_log2f(sum)); }
 
-// Units that ranges have cut, from the sums of their parts. E: type of o.
+// Units that ranges have cut, from the sums of their parts; a workgroup takes 1024 / D rows of one. E: type of o.
 template <typename E, int D, int ROWS, int KEYS>
 __global__ __launch_bounds__(256) void paged_combine_kernel(
     const float* __restrict__ part_o, const f32x4* __restrict__ part_stat, E* __restrict__ o, const int* __restrict__ q_start,
     const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv, int n_seq, int n_tokens, int max_keys, int workgroups, int least) {
-  const int group = H / Hkv, head = blockIdx.x % Hkv;
-  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_keys, 0};
+  constexpr int TAKE = 1024 / D;
+  const int group = H / Hkv, head = blockIdx.x % Hkv, piece = blockIdx.x / Hkv % (ROWS / TAKE);
+  const PagedLine<ROWS, KEYS> line(PagedBatch{q_start, kv_len, n_seq, n_tokens, Hkv, group, max_keys, 0});
   PagedUnit u;
-  if (!paged_find<ROWS, KEYS, true>(batch, blockIdx.x / Hkv, &u)) return;
-  const long long per_head = paged_total<ROWS, KEYS>(batch);
-  const long long length = paged_range(per_head * Hkv, workgroups, least);
-  const long long first = head * per_head + u.first, last = first + u.tiles - 1;
+  if (!line.template find<true>(blockIdx.x / Hkv / (ROWS / TAKE), &u)) return;
+  const long long length = paged_range((long long)line.total * Hkv, workgroups, least);
+  const long long first = (long long)head * line.total + u.first, last = first + u.tiles - 1;
   const int w0 = (int)(first / length), w1 = (int)(last / length);
-  if (w0 == w1) return;
-  const int rows = min(ROWS, u.rows - u.m0);
-  for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
-    const int row = i / (D / 4), c = i % (D / 4) * 4;
-    // (all but the first part begin with their range)
-    const size_t slot0 = (2 * (size_t)w0 + (w0 * length >= first ? 0 : 1)) * ROWS + row;
-    auto slot_of = [&](int w) { return w == w0 ? slot0 : 2 * (size_t)w * ROWS + row; };
-    float ref = -FLT_MAX;
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) ref = fmaxf(ref, part_stat[slot_of(w)][0]);
-    float l = 0.0f, e = 0.0f;
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const size_t slot = slot_of(w);
-      const f32x4 st = part_stat[slot];
-      const float weight = __builtin_amdgcn_exp2f(st[0] - ref);
-      l = __builtin_fmaf(weight, st[1], l);
-      e = __builtin_fmaf(weight, st[2], e);
-      const f32x4 y = *(const f32x4*)(part_o + slot * D + c);
+  const int row = piece * TAKE + threadIdx.x / (D / 4), c = threadIdx.x % (D / 4) * 4, mr = u.m0 + row;
+  if (w0 == w1 || row >= ROWS || mr >= u.rows) return;
+  // (all but the first part begin with their range)
+  const size_t slot0 = (2 * (size_t)w0 + (w0 * length >= first ? 0 : 1)) * ROWS + row;
+  auto slot_of = [&](int w) { return w == w0 ? slot0 : 2 * (size_t)w * ROWS + row; };
+  float ref = -FLT_MAX, l = 0.0f, e = 0.0f;
+  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int w = w0; w <= w1; w += 8) {   // eight parts in flight
+    f32x4 st[8], y[8];
+    float most = ref;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(weight, y[j], x[j]);
+    for (int j = 0; j < 8; ++j) {
+      const size_t slot = slot_of(min(w + j, w1));
+      st[j] = part_stat[slot];
+      y[j] = *(const f32x4*)(part_o + slot * D + c);
     }
-    const int mr = u.m0 + row;
-    const int64_t at = (int64_t)(u.q0 + mr / group) * H + head * group + mr % group;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[at * D + c + j] = (E)(x[j] * inv);
-    if (lse && c == 0) lse[at] = row_statistic(ref, e);
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, st[j][0]);
+    const float alpha = __builtin_amdgcn_exp2f(ref - most);
+    ref = most;
+    l *= alpha;
+    e *= alpha;
+    x *= alpha;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (w + j > w1) break;
+      const float weight = __builtin_amdgcn_exp2f(st[j][0] - ref);
+      l = __builtin_fmaf(weight, st[j][1], l);
+      e = __builtin_fmaf(weight, st[j][2], e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(weight, y[j][i], x[i]);
+    }
   }
+  const int64_t at = (int64_t)(u.q0 + mr / group) * H + head * group + mr % group;
+  x *= l == 0.0f ? 0.0f : 1.0f / l;
+  typedef __attribute__((ext_vector_type(4))) E Four;
+  *(Four*)(o + at * D + c) = Four{(E)x[0], (E)x[1], (E)x[2], (E)x[3]};
+  if (lse && c == 0) lse[at] = row_statistic(ref, e);
 }
+template <int D, int ROWS>
+constexpr int kCombinePieces = ROWS * D / 1024;   // workgroups of a unit
 
 // How a call is launched: units dealt out whole, or ranges with sums of their parts in scratch.
 struct PagedLaunch {
