@@ -141,8 +141,8 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
         there |= is << g;
 #pragma unroll
         for (int j = 0; j < LPG; ++j) {
-          load_lds(k_base + off, bytes, dma_k[j], kd + (g * LPG + j) * 1024);
-          load_lds(v_base + off, bytes, dma_v[j], vd + (g * LPG + j) * 1024);
+          load_lds(k_base + off, bytes, dma_k[j], 0, kd + (g * LPG + j) * 1024);
+          load_lds(v_base + off, bytes, dma_v[j], 0, vd + (g * LPG + j) * 1024);
         }
       }
       ++in_window;
@@ -194,10 +194,7 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             if (n0 + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(seen >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-          for (int mb = 0; mb < NMB; ++mb) odd |= has_odd(v_operand(tt, mb));
+        odd = any_odd<TT, NMB>(v_operand);
       }
       float mx = sc[0][0];
 #pragma unroll
@@ -230,7 +227,7 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
           pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
           l_run = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run, false);
         }
-      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+      if (odd) {
         odd_values<TT, NMB>(oacc, pop, v_operand);
         return;
       }
@@ -334,7 +331,7 @@ PagedLaunch few_launch(const da_paged& p, size_t scratch_bytes) {
 
 // Whether the call has sequences with enough rows for the kernel of units of 128. The host knows the rows of all of them alone.
 static bool paged_many_rows(const da_paged& p) {
-  return (long long)(p.n_tokens - p.n_seq) * (p.H / p.Hkv) >= 64;
+  return true;
 }
 
 size_t paged_scratch_bytes(const da_paged& p) {

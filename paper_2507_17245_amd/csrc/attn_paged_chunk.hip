@@ -19,47 +19,73 @@ namespace {
 
 constexpr int kChunkRows = 128, kChunkKeys = 64, kRW = 4, kHalves = 2, kChunkThreads = kRW * kHalves * 64;
 
+// Nothing is known of x from here on: what is computed of it stays where it is used, instead of in registers that the walk has not got.
+__device__ inline int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// A lane's places: in the loads of 16 keys, and in the operands. Swizzles as in attn_bf16_impl.h; they are exclusive ors, so that
+// load j and operands s and mb differ from the first by one, too.
+template <int D>
+struct Places {
+  static constexpr int ROWB = D * 2, CH = D / 8, LPG = 16 * ROWB / 1024, RPL = 16 / LPG;   // loads of 16 keys, rows of one
+  int lq, hh;
+  int row, kc, v, ka, va;
+  __device__ Places(int lane, int row_bytes) {
+    lq = lane & 31;
+    hh = lane >> 5;
+    const int pc = lane % CH;
+    row = lane / CH * row_bytes;
+    kc = (pc ^ (lane >> 4)) * 16;
+    v = row + ((((pc >> 1) ^ v_swizzle<ROWB>(lane / CH)) << 1) | (pc & 1)) * 16;
+    ka = lq * ROWB + (hh ^ (D == 128 ? (lq & 15) : ((lq >> 1) & 7))) * 16;
+    const int row_l = 4 * hh + ((lane & 15) >> 2);
+    va = row_l * ROWB + (((lane >> 4) & 1) ^ v_swizzle<ROWB>(row_l)) * 32 + 8 * (lane & 3);
+  }
+  // 16 rows of K or V, `bytes` of them from `from` on
+  __device__ void load_k(const char* from, unsigned bytes, int row_bytes, char* to) const {
+    const int c = here(kc);
+#pragma unroll
+    for (int j = 0; j < LPG; ++j) load_lds(from, bytes, row + (c ^ (j * 64)), j * RPL * row_bytes, to + j * 1024);
+  }
+  __device__ void load_v(const char* from, unsigned bytes, int row_bytes, char* to) const {
+#pragma unroll
+    for (int j = 0; j < LPG; ++j) load_lds(from, bytes, v, j * RPL * row_bytes, to + j * 1024);
+  }
+  // operands of the products: rows 32 mb + lq of K, channels 16 s + 8 hh ..; rows 16 tt .. of V, channels 32 mb ..
+  __device__ static bf16x8 k_operand(const char* tile, int ka, int mb, int s) { return *(const bf16x8*)(tile + (ka ^ (s * 32)) + mb * 32 * ROWB); }
+  __device__ static bf16x8 v_operand(const char* tile, int va, int tt, int mb) {
+    const char* p0 = tile + (va ^ (mb * 64)) + 16 * tt * ROWB;
+    return lds_read_tr_pair<bf16x8>(p0, p0 + 8 * ROWB);
+  }
+};
+
 template <int D, bool STATS>
 __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
     const bf16* __restrict__ q, const bf16* __restrict__ k_pages, const bf16* __restrict__ v_pages, bf16* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int row_bytes, int64_t q_token,
     int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat) {
-  constexpr int BC = kChunkKeys, ROWB = D * 2, CH = D / 8, TILEB = BC * ROWB;
+  constexpr int BC = kChunkKeys, ROWB = D * 2, TILEB = BC * ROWB;
   constexpr int MB = BC / 32, TT = BC / 16, KSTEPS = D / 16, NMB = D / 32;
   constexpr int LPG = 16 * ROWB / 1024;   // direct loads of 16 keys
   constexpr float kSumTrigger = (BC / 2) * 256.0f;   // (as in attn_bf16_impl.h)
-  __shared__ __attribute__((aligned(1024))) char k_lds0[kHalves * TILEB];
-  __shared__ __attribute__((aligned(1024))) char k_lds1[kHalves * TILEB];
-  __shared__ __attribute__((aligned(1024))) char v_lds0[kHalves * TILEB];
-  __shared__ __attribute__((aligned(1024))) char v_lds1[kHalves * TILEB];
+  // Two tiles of K and V for each half; or, with few rows, one of 8 KB for each wave.
+  constexpr int FEWB = 8192, FT = FEWB / ROWB, BUFB = 4 * FEWB;
+  static_assert(kHalves * TILEB <= BUFB, "a buffer holds the halves' tiles");
+  __shared__ __attribute__((aligned(1024))) char k_lds0[BUFB];
+  __shared__ __attribute__((aligned(1024))) char k_lds1[BUFB];
+  __shared__ __attribute__((aligned(1024))) char v_lds0[BUFB];
+  __shared__ __attribute__((aligned(1024))) char v_lds1[BUFB];
+  __shared__ f32x4 few_stat[kRW * kHalves][32];
 
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % kRW, half = wave / kRW;
-  const int lq = lane & 31, hh = lane >> 5;
   const int group = H / Hkv;
   const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
   auto k_buf = [&](int par) -> char* { return (par ? k_lds1 : k_lds0) + half * TILEB; };
   auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
-
-  // lanes' places in the loads of 16 keys, and in the operands
-  int dma_k[LPG], dma_v[LPG];
-#pragma unroll
-  for (int j = 0; j < LPG; ++j) {
-    const int slot = j * 64 + lane, row = slot / CH, pc = slot % CH;
-    dma_k[j] = row * row_bytes + (pc ^ (D == 128 ? (row & 15) : ((row >> 1) & 7))) * 16;
-    dma_v[j] = row * row_bytes + ((((pc >> 1) ^ v_swizzle<ROWB>(row)) << 1) | (pc & 1)) * 16;
-  }
-  int ka_off[KSTEPS], va_off[NMB];
-#pragma unroll
-  for (int s = 0; s < KSTEPS; ++s) ka_off[s] = lq * ROWB + ((2 * s + hh) ^ (D == 128 ? (lq & 15) : ((lq >> 1) & 7))) * 16;
-  {
-    const int row_l = 4 * hh + ((lane & 15) >> 2);
-#pragma unroll
-    for (int mb = 0; mb < NMB; ++mb)
-      va_off[mb] = row_l * ROWB + ((2 * mb + ((lane >> 4) & 1)) ^ v_swizzle<ROWB>(row_l)) * 32 + 8 * (lane & 3);
-  }
 
   const PagedLine<kChunkRows, BC> line(batch);
   long long pos = 0, end = 1, per_head = 1, length = 1;
@@ -94,12 +120,210 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
     const bool from_begin = pos == begin;
     pos += t1 - t0;
 
-    const int m = u.m0 + rw * 32 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
-    const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
     const int n_keys = min(u.len, batch.max_keys);
-    const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
     const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (min(u.m0 + kChunkRows, u.rows) - 1) / group + 1, 0)) : n_keys;   // no row sees more
     const int all_see = causal ? min(max(u.len - u.nq + u.m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
+    const int* table = page_table + (int64_t)u.seq * max_pages;
+    const char* k_base = (const char*)k_pages + head * head_bytes;
+    const char* v_base = (const char*)v_pages + head * head_bytes;
+
+    if (u.rows - u.m0 <= 32) {
+      // ---- few rows: a wave has all of them, and every eighth tile of 8 KB. Bound: reading the keys and values. ----
+      // Each wave has a softmax state of its own and no barrier; K of its next tile is asked for when the scores are
+      // taken, V when it is multiplied, so that 128 KB a compute unit are on their way most of the time.
+      constexpr int GROUPS = FT / 16, FMB = FT / 32, FTT = FT / 16, CPT = FEWB / 1024, WINDOW = 64 / GROUPS, WAVES = kRW * kHalves;
+      const int lane = here(tid) & 63;
+      const Places<D> at_lane(lane, row_bytes);
+      const int lq = at_lane.lq, hh = at_lane.hh;
+      const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);
+      const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
+      const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);
+      bf16x8 qop[KSTEPS];
+      const bf16* q_row = q + token * q_token + q_of * q_head;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
+      int tile = t0 * (BC / FT) + wave;
+      const int t_end = min(t1 * (BC / FT), (n_seen + FT - 1) / FT);
+      // the window's lane for this wave's tile tile + 8 i is that of i * GROUPS, and of the groups of 16 keys behind it
+      auto window_of = [&](int first) {
+        const int t = first + (lane / GROUPS) * WAVES;
+        return page_window(table, t * FT + lane % GROUPS * 16, n_seen, page_size, n_pages, page_bytes, row_bytes);
+      };
+      // Two windows, the second from the middle of the first on; it takes the first's place when that half is asked for.
+      PageWindow now = window_of(tile), next = window_of(tile + WINDOW / 2 * WAVES);
+      int at = 0;   // place in the window of the tile that is asked for
+      auto ask = [&](auto of_k, const char* from, int t, char* to) -> int {
+        int there = 0;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          const int l = at * GROUPS + g;
+          const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l);
+          const int is = __builtin_amdgcn_readlane(now.there, l);
+          const int rows = min(n_seen - (t * FT + 16 * g), 16);
+          const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
+          there |= is << g;
+          if constexpr (decltype(of_k)::value) at_lane.load_k(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + g * LPG * 1024);
+          else at_lane.load_v(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + g * LPG * 1024);
+        }
+        return there;
+      };
+      const std::true_type of_k;
+      const std::false_type of_v;
+      char* kb = (wave < 4 ? k_lds0 : k_lds1) + (wave & 3) * FEWB;
+      char* vb = (wave < 4 ? v_lds0 : v_lds1) + (wave & 3) * FEWB;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
+      int there = 0;
+      if (tile < t_end) {
+        there = ask(of_k, k_base, tile, kb);
+        ask(of_v, v_base, tile, vb);
+      }
+      f32x16 oacc[NMB];
+#pragma unroll
+      for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
+      // The reference is the largest score so far, unscaled (a scaled one is rounded, which shows on large scores).
+      float ref = -FLT_MAX, l_run = 0.0f, e_run = 0.0f;
+      for (; tile < t_end; tile += WAVES) {
+        const int seen = there;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // K is there
+        const int ka = here(at_lane.ka), va = here(at_lane.va);
+        f32x16 sc[FMB];
+#pragma unroll
+        for (int mb = 0; mb < FMB; ++mb) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[mb][i] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < KSTEPS; ++s) sc[mb] = mfma_32x32x16(at_lane.k_operand(kb, ka, mb, s), qop[s], sc[mb]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // and read
+        const bool more = tile + WAVES < t_end;
+        if (more) {
+          ++at;
+          there = ask(of_k, k_base, tile + WAVES, kb);
+        }
+        const int n0 = tile * FT;
+        const bool some = n0 + FT > all_see || seen != (1 << GROUPS) - 1;
+        if (some) {
+#pragma unroll
+          for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (n0 + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(seen >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[mb][i]);
+        const float ref_new = fmaxf(ref, half_swap_max(mx));
+        if (__builtin_amdgcn_ballot_w64(ref_new > ref) != 0) {
+          const float alpha = __builtin_amdgcn_exp2f((ref - ref_new) * scale_log2e);
+          l_run *= alpha;
+          if constexpr (STATS) e_run *= alpha;
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+          ref = ref_new;
+        }
+        // P rounded to bf16 as the operands of P.V; the row sum is taken over the rounded values, so that the rounding of a row's
+        // largest weights cancels
+        bf16x8 pop[FTT];
+        const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+#pragma unroll
+        for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float x0 = __builtin_amdgcn_exp2f((sc[mb][i] - ref) * scale_log2e), x1 = __builtin_amdgcn_exp2f((sc[mb][i + 1] - ref) * scale_log2e);
+            const bf16x2 pr = {(bf16)x0, (bf16)x1};
+            if constexpr (STATS) e_run += x0 + x1;
+            pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
+            pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
+            l_run = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run, false);
+          }
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // V is there
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
+        bool odd = false;
+        if (some) odd = any_odd<FTT, NMB>(v_operand);
+        if (odd) {
+          odd_values<FTT, NMB>(oacc, pop, v_operand);
+        } else {
+#pragma unroll
+          for (int tt = 0; tt < FTT; ++tt)
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(v_operand(tt, mb), pop[tt], oacc[mb]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) ask(of_v, v_base, tile + WAVES, vb);
+        if (at == WINDOW / 2) {   // (the next to be asked for is behind it)
+          at = 0;
+          now = next;
+          next = window_of(tile + (1 + WINDOW / 2) * WAVES);
+        }
+        // (the wait behind these products as in attn_bf16_few.hip)
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 1");
+      }
+      // the waves' states meet
+      const float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
+      if (hh == 0) few_stat[wave][lq] = f32x4{ref, l_tot, e_tot, 0.0f};
+      __syncthreads();
+      float ref_all = few_stat[0][lq][0], l_all = 0.0f, e_all = 0.0f;
+#pragma unroll
+      for (int j = 1; j < WAVES; ++j) ref_all = fmaxf(ref_all, few_stat[j][lq][0]);
+#pragma unroll
+      for (int j = 0; j < WAVES; ++j) {
+        const f32x4 st = few_stat[j][lq];
+        const float x = __builtin_amdgcn_exp2f((st[0] - ref_all) * scale_log2e);
+        l_all += st[1] * x;
+        e_all += st[2] * x;
+      }
+      // (a row that sees nothing has sum 0 and is 0)
+      const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
+      // wave w's sums: 32 rows of D floats in its own buffers (K at d = 64, K and V at d = 128), the 16-byte pieces exchanged by the row
+#pragma unroll
+      for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int piece = 8 * mb + 2 * i4 + hh;   // channels 4*piece ..
+          float* dst = (float*)(mb < 2 ? kb : vb);
+          const f32x4 x = {oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
+          *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
+        }
+      __syncthreads();
+      const size_t slot = (2 * (size_t)wg + (from_begin ? 0 : 1)) * kChunkRows;
+      for (int i = tid; i < min(u.rows - u.m0, 32) * (D / 4); i += kChunkThreads) {
+        const int row = i / (D / 4), piece = i % (D / 4), mr = u.m0 + row;
+        const int at = row * 256 + (((piece & 15) ^ (row & 15)) << 4);
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < WAVES; ++j) {
+          const char* of = piece < 16 ? (j < 4 ? k_lds0 : k_lds1) : (j < 4 ? v_lds0 : v_lds1);
+          x += *(const f32x4*)(of + (j & 3) * FEWB + at);
+        }
+        if (whole) {
+          const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+          *(bf16x4*)(o + ((int64_t)(u.q0 + mr / group) * H + head * group + mr % group) * D + piece * 4) = y;
+        } else {
+          *(f32x4*)(part_o + (slot + row) * D + piece * 4) = x;
+        }
+      }
+      if (wave == 0 && hh == 0 && m < u.rows) {
+        if (!whole) part_stat[slot + lq] = f32x4{ref_all * scale_log2e, l_all, e_all, 0.0f};
+        else if (STATS) lse[(int64_t)token * H + q_of] = row_statistic(ref_all * scale_log2e, e_all);
+      }
+      __syncthreads();   // (the next unit's tiles take the place of the sums)
+      continue;
+    }
+    const int lane = here(tid) & 63;
+    const Places<D> at_lane(lane, row_bytes);
+    const int lq = at_lane.lq, hh = at_lane.hh;
+    const int m = u.m0 + rw * 32 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
+    const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
+    const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
     const int seen_tiles = (n_seen + BC - 1) / BC;
     // the halves' tiles; a half without any walks one behind the last key: zeros, masked out
     const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + 1) / 2, 1);
@@ -116,9 +340,6 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
 #pragma unroll
     for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
 
-    const int* table = page_table + (int64_t)u.seq * max_pages;
-    const char* k_base = (const char*)k_pages + head * head_bytes;
-    const char* v_base = (const char*)v_pages + head * head_bytes;
     // Lane i: where the wave's 16 keys of tile (first + i) of the half lie, and which of the tile's groups lie in the cache.
     struct Window {
       uint32_t lo, hi;
@@ -138,33 +359,31 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
       }
       return w;
     };
+    // Two windows, the second from the middle of the first on; it takes the first's place when that half is done with.
     int base = 0;
-    Window now = window_of(0), next = window_of(64);
-    auto advance = [&](int it) {   // tiles before `it` are done with
-      if (it < base + 64) return;
-      base += 64;
+    Window now = window_of(0), next = window_of(32);
+    auto advance = [&](int it) {   // tiles before `it` are done with: those up to it + 31 lie in the window from here on
+      if (it < base + 32) return;
+      base += 32;
       now = next;
-      next = window_of(base + 64);
+      next = window_of(base + 32);
     };
-    auto there_of = [&](int it) {
-      const int i = it - base;
-      return i < 64 ? __builtin_amdgcn_readlane(now.there, i) : __builtin_amdgcn_readlane(next.there, i - 64);
-    };
-    auto load_group = [&](const char* from, const int (&places)[LPG], int it, char* to) {
-      const int i = it - base, l = i & 63;
-      const bool ahead = i >= 64;
-      const uint32_t lo = (uint32_t)(ahead ? __builtin_amdgcn_readlane((int)next.lo, l) : __builtin_amdgcn_readlane((int)now.lo, l));
-      const uint32_t hi = (uint32_t)(ahead ? __builtin_amdgcn_readlane((int)next.hi, l) : __builtin_amdgcn_readlane((int)now.hi, l));
-      const int is = (ahead ? __builtin_amdgcn_readlane(next.there, l) : __builtin_amdgcn_readlane(now.there, l)) >> rw & 1;
+    auto there_of = [&](int it) { return __builtin_amdgcn_readlane(now.there, it - base); };
+    const std::true_type yes;
+    const std::false_type no;
+    auto load_group = [&](auto of_k, const char* from, int it, char* to) {
+      const int l = it - base;
+      const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l);
+      const int is = there_of(it) >> rw & 1;
       const int rows = min(n_seen - ((tile0 + it) * BC + 16 * rw), 16);
       const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
-#pragma unroll
-      for (int j = 0; j < LPG; ++j) load_lds(from + (lo | (uint64_t)hi << 32), bytes, places[j], to + (rw * LPG + j) * 1024);
+      if constexpr (decltype(of_k)::value) at_lane.load_k(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + rw * LPG * 1024);
+      else at_lane.load_v(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + rw * LPG * 1024);
     };
     // What tile `it` brings in: K(it + 2) where K(it) was, V(it + 1) where V(it - 1) was.
     auto feed = [&](int it, int par) {
-      if (it + 2 < n_tiles) load_group(k_base, dma_k, it + 2, k_buf(par));
-      load_group(v_base, dma_v, it + 1, v_buf(par ^ 1));
+      if (it + 2 < n_tiles) load_group(yes, k_base, it + 2, k_buf(par));
+      load_group(no, v_base, it + 1, v_buf(par ^ 1));
     };
     auto dma_wait = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
     auto masked = [&](int it) { return (tile0 + it) * BC + BC > all_see || there_of(it) != 15; };
@@ -180,12 +399,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
 
     auto qk = [&](int par, f32x16 (&sacc)[MB]) {
       const char* at = k_buf(par);
+      const int ka = here(at_lane.ka);
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) sacc[mb][i] = 0.0f;
 #pragma unroll
-        for (int s = 0; s < KSTEPS; ++s) sacc[mb] = mfma_32x32x16(*(const bf16x8*)(at + ka_off[s] + mb * 32 * ROWB), qop[s], sacc[mb]);
+        for (int s = 0; s < KSTEPS; ++s) sacc[mb] = mfma_32x32x16(at_lane.k_operand(at, ka, mb, s), qop[s], sacc[mb]);
       }
     };
     auto apply_mask = [&](int it, f32x16 (&sc)[MB]) {
@@ -251,20 +471,13 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
       l_run += rs;
       if constexpr (STATS) e_run += es;
       const char* vb = v_buf(par);
-      auto v_operand = [&](int tt, int mb) {
-        const char* p0 = vb + va_off[mb] + 16 * tt * ROWB;
-        return lds_read_tr_pair<bf16x8>(p0, p0 + 8 * ROWB);
-      };
+      const int va = here(at_lane.va);
+      auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
       bool odd = false;
       if constexpr (!CLEAN) {
-        if (masked(it)) {
-#pragma unroll
-          for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-            for (int mb = 0; mb < NMB; ++mb) odd |= has_odd(v_operand(tt, mb));
-        }
+        if (masked(it)) odd = any_odd<TT, NMB>(v_operand);
       }
-      if (!CLEAN && __builtin_amdgcn_ballot_w64(odd) != 0) {
+      if (!CLEAN && odd) {
         odd_values<TT, NMB>(oacc, pop, v_operand);
       } else {
         constexpr int PF = (4 / NMB < TT) ? 4 / NMB : TT - 1;
@@ -290,6 +503,10 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
         }
         __builtin_amdgcn_sched_group_barrier(0x008, PF * NMB, 0);
       }
+      if constexpr (!CLEAN) {   // (the wait behind these products as in attn_bf16_few.hip)
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 3");
+      }
       if constexpr (HAS_NEXT) {
         if constexpr (!CLEAN) {
           if (masked(it + 1)) apply_mask(it + 1, sn);
@@ -299,13 +516,11 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
       __syncthreads();
     };
 
-    load_group(v_base, dma_v, 0, v_buf(0));
-    load_group(k_base, dma_k, 0, k_buf(0));
-    if (n_tiles > 1) load_group(k_base, dma_k, 1, k_buf(1));
+    load_group(no, v_base, 0, v_buf(0));
+    load_group(yes, k_base, 0, k_buf(0));
+    if (n_tiles > 1) load_group(yes, k_base, 1, k_buf(1));
     dma_wait();
     __syncthreads();
-    const std::true_type yes;
-    const std::false_type no;
     if (idle) {
       __syncthreads();
       for (int it = 0; it < n_tiles - 1; ++it) {
@@ -330,7 +545,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
         if ((it & 1) == 0) {
           // clean tiles of the window from `it` on
           const uint64_t bad = __builtin_amdgcn_ballot_w64(now.there != 15) >> (it - base);
-          const int clean = min(n_full, it + (bad ? __builtin_ctzll(bad) : base + 64 - it));
+          const int clean = min(min(n_full, it + (bad ? __builtin_ctzll(bad) : 64)), base + 62);   // (loads run three tiles ahead)
           for (; it + 2 < clean; it += 2) {
             body(yes, yes, it, 0, s0, s1);
             body(yes, yes, it + 1, 1, s1, s0);
