@@ -74,10 +74,9 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
   if (ranges) {
     per_head = line.total;
     length = paged_range(per_head * Hkv, gridDim.x, least);
-    pos = length * blockIdx.x;
-    end = min(pos + length, per_head * Hkv);
+    pos = paged_cut(line, blockIdx.x, length, per_head * Hkv, per_head);
+    end = paged_cut(line, blockIdx.x + 1LL, length, per_head * Hkv, per_head);
   }
-  const long long begin = pos;
   while (pos < end) {
     PagedUnit u;
     int head, t0, t1;
@@ -94,7 +93,6 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
       t1 = u.tiles;
     }
     const bool whole = t0 == 0 && t1 == u.tiles;
-    const bool from_begin = pos == begin;
     pos += t1 - t0;
 
     const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
@@ -277,7 +275,7 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
         *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
       }
     __syncthreads();
-    const size_t slot = 2 * (size_t)blockIdx.x + (from_begin ? 0 : 1);
+    const size_t slot = 2 * (size_t)blockIdx.x + (t0 == 0 ? 2 : 1);   // (the part in front of the next one's cut)
     auto finish = [&](const char (*sums)[kFewTileBytes], int c0) {   // 64 channels from c0 on
 #pragma unroll
       for (int i = tid; i < kFewRows * 16; i += kFewThreads) {
@@ -316,7 +314,7 @@ hipError_t launch_few(const void* q, const void* k_pages, const void* v_pages, v
                      p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kFewRows, kFewKeys<D>>), dim3((unsigned)(paged_units(p, kFewRows) * p.Hkv * kCombinePieces<D, kFewRows>)), dim3(256), 0,
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kFewRows, kFewKeys<D>>), dim3(paged_combine_grid(p, kFewRows)), dim3(256), 0,
                      stream, part_o, part_stat, (bf16*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens,
                      p.max_pages * p.page_size, l.workgroups, l.least);
   return hipGetLastError();

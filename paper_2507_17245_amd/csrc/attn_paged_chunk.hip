@@ -95,10 +95,9 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
     per_head = line.total;
     length = paged_range(per_head * Hkv, gridDim.x, least);
-    pos = length * wg;
-    end = min(pos + length, per_head * Hkv);
+    pos = paged_cut(line, wg, length, per_head * Hkv, per_head);
+    end = paged_cut(line, wg + 1LL, length, per_head * Hkv, per_head);
   }
-  const long long begin = pos;
   while (pos < end) {
     PagedUnit u;
     int head, t0, t1;
@@ -117,7 +116,6 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
       t1 = u.tiles;
     }
     const bool whole = t0 == 0 && t1 == u.tiles;
-    const bool from_begin = pos == begin;
     pos += t1 - t0;
 
     const int n_keys = min(u.len, batch.max_keys);
@@ -294,7 +292,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
           *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
         }
       __syncthreads();
-      const size_t slot = (2 * (size_t)wg + (from_begin ? 0 : 1)) * kChunkRows;
+      const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kChunkRows;
       for (int i = tid; i < min(u.rows - u.m0, 32) * (D / 4); i += kChunkThreads) {
         const int row = i / (D / 4), piece = i % (D / 4), mr = u.m0 + row;
         const int at = row * 256 + (((piece & 15) ^ (row & 15)) << 4);
@@ -549,6 +547,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
           for (; it + 2 < clean; it += 2) {
             body(yes, yes, it, 0, s0, s1);
             body(yes, yes, it + 1, 1, s1, s0);
+            __builtin_amdgcn_sched_barrier(0);   // (as above, for the way out of this loop)
+            asm volatile("s_nop 3");
           }
           if (it == n_tiles - 1) break;
         }
@@ -604,7 +604,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
       }
     if (m < u.rows) {
       const int64_t row = (int64_t)token * H + q_of;
-      const size_t slot = (2 * (size_t)wg + (from_begin ? 0 : 1)) * kChunkRows + rw * 32 + lq;
+      const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kChunkRows + rw * 32 + lq;
       if (hh == 0 && half == 0) {
         if (!whole) part_stat[slot] = f32x4{ref, l_tot, e_tot, 0.0f};
         else if (STATS) lse[row] = row_statistic(ref, e_tot);
@@ -635,7 +635,7 @@ hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, voi
                      p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kChunkRows, kChunkKeys>), dim3((unsigned)(paged_units(p, kChunkRows) * p.Hkv * kCombinePieces<D, kChunkRows>)), dim3(256), 0,
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kChunkRows, kChunkKeys>), dim3(paged_combine_grid(p, kChunkRows)), dim3(256), 0,
                      stream, part_o, part_stat, (bf16*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens,
                      p.max_pages * p.page_size, l.workgroups, l.least);
   return hipGetLastError();

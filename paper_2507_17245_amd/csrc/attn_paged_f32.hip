@@ -36,10 +36,9 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
   if (ranges) {
     per_head = line.total;
     length = paged_range(per_head * Hkv, gridDim.x, least);
-    pos = length * blockIdx.x;
-    end = min(pos + length, per_head * Hkv);
+    pos = paged_cut(line, blockIdx.x, length, per_head * Hkv, per_head);
+    end = paged_cut(line, blockIdx.x + 1LL, length, per_head * Hkv, per_head);
   }
-  const long long begin = pos;
   while (pos < end) {
     PagedUnit u;
     int head, t0, t1;
@@ -56,7 +55,6 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
       t1 = u.tiles;
     }
     const bool whole = t0 == 0 && t1 == u.tiles;
-    const bool from_begin = pos == begin;
     pos += t1 - t0;
 
     const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);
@@ -91,10 +89,9 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
       ChannelSum<HALF> chain;
 #pragma unroll
       for (int s = 0; s < HALF; s += 4) {
-        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (mine.there) x = *(const f32x4*)(k_base + off + (hh * HALF + s) * 4);
+        const f32x4 x = *(const f32x4*)(k_base + off + (hh * HALF + s) * 4);   // (of an absent key the cache's first)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) chain.step(s + j, x[j], qv[s + j]);
+        for (int j = 0; j < 4; ++j) chain.step(s + j, mine.there ? x[j] : 0.0f, qv[s + j]);
       }
       f32x16 sc = chain.sum();
 #pragma unroll
@@ -125,7 +122,10 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
           const uint64_t row = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)mine.lo) | (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)mine.hi) << 32;
           const bool is = there >> acc_row(i, hh) & 1;
 #pragma unroll
-          for (int mb = 0; mb < NMB; ++mb) take(i, mb, is ? *(const float*)(v_base + row + (32 * mb + lq) * 4) : 0.0f);
+          for (int mb = 0; mb < NMB; ++mb) {
+            const float x = *(const float*)(v_base + row + (32 * mb + lq) * 4);
+            take(i, mb, is ? x : 0.0f);
+          }
         }
       };
       bool odd = false;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
         *(f32x4*)&sums[wave][lq][32 * mb + 8 * i4 + 4 * hh] =
             f32x4{oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
     __syncthreads();
-    const size_t slot = 2 * (size_t)blockIdx.x + (from_begin ? 0 : 1);
+    const size_t slot = 2 * (size_t)blockIdx.x + (t0 == 0 ? 2 : 1);   // (the part in front of the next one's cut)
     for (int i = tid; i < kRows * (D / 4); i += kThreads) {
       const int row = i / (D / 4), c = i % (D / 4) * 4, mr = u.m0 + row;
       if (mr >= u.rows) continue;
@@ -201,7 +201,7 @@ hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, voi
                      scale_log2e, l.ranges, l.least, part_o, part_stat);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows, kTile>), dim3((unsigned)(paged_units(p, kRows) * p.Hkv * kCombinePieces<D, kRows>)), dim3(256), 0, stream, part_o,
+  hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows, kTile>), dim3(paged_combine_grid(p, kRows)), dim3(256), 0, stream, part_o,
                      part_stat, (float*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.max_pages * p.page_size,
                      l.workgroups, l.least);
   return hipGetLastError();

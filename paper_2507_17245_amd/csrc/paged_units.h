@@ -4,10 +4,11 @@
 // keys that they see, in tiles. The lengths lie on the device, so every workgroup finds its own work: it sums the
 // units and tiles of the sequences, 64 at a time, a lane for each.
 //   whole units   workgroup w takes unit w / Hkv of kv head w % Hkv.
-//   ranges        all tiles, unit after unit and kv head after kv head, are one line, which is cut into equal ranges: every
-//                 workgroup has the same walk whatever the lengths are. A unit that ranges cut is put together by the combine kernel from the
-//                 sums that they leave: workgroup w those of the unit that its range begins in at 2 w, of the one that it ends in, if that
-//                 is another, at 2 w + 1. The ones in between are whole.
+//   ranges        all tiles, unit after unit and kv head after kv head, are one line, which is cut into equal ranges, one a workgroup:
+//                 each has the same walk whatever the lengths are. A cut less than `snap` tiles from an end of its unit moves
+//                 there (beginning and ending a unit costs as much as several tiles). A unit that cuts fall into is put together by the
+//                 combine kernel from the sums of its parts: those of the part in front of its first cut, which workgroup w begins
+//                 at, at 2 w, those of a part that begins with workgroup w's cut at 2 w + 1.
 #pragma once
 #include <cfloat>
 
@@ -75,21 +76,26 @@ struct PagedLine {
   typedef PagedSequence<ROWS, KEYS> Sequence;
   const PagedBatch b;
   const Sequence head;
-  unsigned total;   // its tiles
+  unsigned total, units;   // its tiles and units
   __device__ explicit PagedLine(const PagedBatch& batch) : b(batch), head(batch, threadIdx.x & 63) {
     total = head.all_tiles();
-    for (int s0 = 64; s0 < b.n_seq; s0 += 64) total += Sequence(b, s0 + (threadIdx.x & 63)).all_tiles();
+    units = head.all_units();
+    for (int s0 = 64; s0 < b.n_seq; s0 += 64) {
+      const Sequence q(b, s0 + (threadIdx.x & 63));
+      total += q.all_tiles();
+      units += q.all_units();
+    }
   }
   // The unit that holds place `x` (BY_UNIT: the x-th unit); false behind the last one.
   template <bool BY_UNIT>
   __device__ bool find(unsigned x, PagedUnit* out) const {
     unsigned before = 0;
     if (in<BY_UNIT>(head, 0, x, &before, out)) return true;
-    unsigned units = head.all_units();
+    unsigned units_before = head.all_units();
     for (int s0 = 64; s0 < b.n_seq; s0 += 64) {
       const Sequence q(b, s0 + (threadIdx.x & 63));
-      if (in<BY_UNIT>(q, s0, BY_UNIT ? x - units : x, &before, out)) return true;
-      units += q.all_units();
+      if (in<BY_UNIT>(q, s0, BY_UNIT ? x - units_before : x, &before, out)) return true;
+      units_before += q.all_units();
     }
     return false;
   }
@@ -124,6 +130,18 @@ struct PagedLine {
 __device__ inline long long paged_range(long long total, int workgroups, int least) {
   return max((total + workgroups - 1) / workgroups, (long long)least);
 }
+__device__ inline int paged_snap(long long length) { return (int)min(max(length / 8, 1LL), 6LL); }
+// Where range w begins.
+template <typename LINE>
+__device__ inline long long paged_cut(const LINE& line, long long w, long long length, long long total, long long per_head) {
+  const long long at = w * length;
+  if (at >= total) return total;
+  PagedUnit u;
+  const long long head = at / per_head;
+  if (!line.template find<false>((unsigned)(at - head * per_head), &u)) return total;
+  const int in = (int)(at - head * per_head - u.first), snap = paged_snap(length);
+  return in < snap ? at - in : u.tiles - in < snap ? at - in + u.tiles : at;
+}
 
 // Where the keys of 16 successive places lie: a lane for each such group of a wave's next 64. The group's first row of
 // the page, in bytes, and whether the page is one of the cache's.
@@ -148,60 +166,70 @@ __device__ inline PageWindow page_window(const int* __restrict__ table, int key,
 // log-sum-exp of a row from its reference (log2 units) and the sum relative to it
 __device__ inline float row_statistic(float ref, float sum) { return sum == 0.0f ? -INFINITY : 0.6931471805599453f * (ref + __builtin_log2f(sum)); }
 
-// Units that ranges have cut, from the sums of their parts; a workgroup takes 1024 / D rows of one. E: type of o.
+// Units that cuts fall into, from the sums of their parts; a workgroup takes 1024 / D rows of one at a time, first those of all
+// units that every unit has. Where there are fewer rows, lanes share a row's parts. E: type of o.
 template <typename E, int D, int ROWS, int KEYS>
 __global__ __launch_bounds__(256) void paged_combine_kernel(
     const float* __restrict__ part_o, const f32x4* __restrict__ part_stat, E* __restrict__ o, const int* __restrict__ q_start,
     const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv, int n_seq, int n_tokens, int max_keys, int workgroups, int least) {
-  constexpr int TAKE = 1024 / D;
-  const int group = H / Hkv, head = blockIdx.x % Hkv, piece = blockIdx.x / Hkv % (ROWS / TAKE);
+  constexpr int TAKE = 1024 / D, C4 = D / 4;
+  const int group = H / Hkv;
+  __shared__ f32x4 x_lds[256], stat_lds[256];
   const PagedLine<ROWS, KEYS> line(PagedBatch{q_start, kv_len, n_seq, n_tokens, Hkv, group, max_keys, 0});
-  PagedUnit u;
-  if (!line.template find<true>(blockIdx.x / Hkv / (ROWS / TAKE), &u)) return;
   const long long length = paged_range((long long)line.total * Hkv, workgroups, least);
-  const long long first = (long long)head * line.total + u.first, last = first + u.tiles - 1;
-  const int w0 = (int)(first / length), w1 = (int)(last / length);
-  const int row = piece * TAKE + threadIdx.x / (D / 4), c = threadIdx.x % (D / 4) * 4, mr = u.m0 + row;
-  if (w0 == w1 || row >= ROWS || mr >= u.rows) return;
-  // (all but the first part begin with their range)
-  const size_t slot0 = (2 * (size_t)w0 + (w0 * length >= first ? 0 : 1)) * ROWS + row;
-  auto slot_of = [&](int w) { return w == w0 ? slot0 : 2 * (size_t)w * ROWS + row; };
-  float ref = -FLT_MAX, l = 0.0f, e = 0.0f;
-  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int w = w0; w <= w1; w += 8) {   // eight parts in flight
-    f32x4 st[8], y[8];
-    float most = ref;
+  const int snap = paged_snap(length);
+  const unsigned each = line.units * (unsigned)Hkv;
+  for (unsigned item = blockIdx.x; item < each * (ROWS / TAKE); item += gridDim.x) {
+    const unsigned piece = item / each, of = item % each;
+    const int head = (int)(of % (unsigned)Hkv);
+    PagedUnit u;
+    if (!line.template find<true>(of / (unsigned)Hkv, &u)) return;
+    const long long first = (long long)head * line.total + u.first;
+    const int w0 = (int)((first + snap + length - 1) / length), w1 = (int)((first + u.tiles - snap) / length);   // its cuts
+    const int rows = min(u.rows - u.m0 - (int)piece * TAKE, TAKE);
+    if (w0 > w1 || rows <= 0) continue;
+    int side = 1;   // lanes' rows side by side, a power of two
+    while (side < rows) side *= 2;
+    const int c = threadIdx.x % C4 * 4, at_row = threadIdx.x / C4 % side, share = threadIdx.x / (C4 * side), shares = TAKE / side;
+    const int row = (int)piece * TAKE + min(at_row, rows - 1), parts = w1 - w0 + 2;
+    auto slot_of = [&](int i) { return (i == 0 ? 2 * (size_t)w0 : 2 * (size_t)(w0 + i - 1) + 1) * ROWS + row; };
+    f32x4 all = {-FLT_MAX, 0.0f, 0.0f, 0.0f}, x = {0.0f, 0.0f, 0.0f, 0.0f};   // reference, sum, sum before rounding
+    auto add = [&](f32x4 st, f32x4 y) {
+      const float ref = fmaxf(all[0], st[0]);
+      const float a = __builtin_amdgcn_exp2f(all[0] - ref), b = __builtin_amdgcn_exp2f(st[0] - ref);
+      all = f32x4{ref, __builtin_fmaf(b, st[1], a * all[1]), __builtin_fmaf(b, st[2], a * all[2]), 0.0f};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const size_t slot = slot_of(min(w + j, w1));
-      st[j] = part_stat[slot];
-      y[j] = *(const f32x4*)(part_o + slot * D + c);
+      for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(b, y[i], a * x[i]);
+    };
+    for (int i = share; i < parts; i += 4 * shares) {   // four parts in flight
+      f32x4 st[4], y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const size_t slot = slot_of(min(i + j * shares, parts - 1));
+        st[j] = part_stat[slot];
+        y[j] = *(const f32x4*)(part_o + slot * D + c);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + j * shares < parts) add(st[j], y[j]);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) most = fmaxf(most, st[j][0]);
-    const float alpha = __builtin_amdgcn_exp2f(ref - most);
-    ref = most;
-    l *= alpha;
-    e *= alpha;
-    x *= alpha;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (w + j > w1) break;
-      const float weight = __builtin_amdgcn_exp2f(st[j][0] - ref);
-      l = __builtin_fmaf(weight, st[j][1], l);
-      e = __builtin_fmaf(weight, st[j][2], e);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(weight, y[j][i], x[i]);
+    if (shares > 1) {
+      x_lds[threadIdx.x] = x;
+      stat_lds[threadIdx.x] = all;
+      __syncthreads();
+      if (share == 0)
+        for (int j = 1; j < shares; ++j) add(stat_lds[threadIdx.x + j * C4 * side], x_lds[threadIdx.x + j * C4 * side]);
+      __syncthreads();
     }
+    if (share != 0 || at_row >= rows) continue;
+    const int mr = u.m0 + row;
+    const int64_t at = (int64_t)(u.q0 + mr / group) * H + head * group + mr % group;
+    x *= all[1] == 0.0f ? 0.0f : 1.0f / all[1];
+    typedef __attribute__((ext_vector_type(4))) E Four;
+    *(Four*)(o + at * D + c) = Four{(E)x[0], (E)x[1], (E)x[2], (E)x[3]};
+    if (lse && c == 0) lse[at] = row_statistic(all[0], all[2]);
   }
-  const int64_t at = (int64_t)(u.q0 + mr / group) * H + head * group + mr % group;
-  x *= l == 0.0f ? 0.0f : 1.0f / l;
-  typedef __attribute__((ext_vector_type(4))) E Four;
-  *(Four*)(o + at * D + c) = Four{(E)x[0], (E)x[1], (E)x[2], (E)x[3]};
-  if (lse && c == 0) lse[at] = row_statistic(ref, e);
 }
-template <int D, int ROWS>
-constexpr int kCombinePieces = ROWS * D / 1024;   // workgroups of a unit
 
 // How a call is launched: units dealt out whole, or ranges with sums of their parts in scratch.
 struct PagedLaunch {
@@ -211,6 +239,10 @@ struct PagedLaunch {
 inline long long paged_units(const da_paged& p, int rows) { return (long long)p.n_tokens * (p.H / p.Hkv) / rows + std::min(p.n_seq, p.n_tokens); }
 inline size_t paged_sum_bytes(int workgroups, int rows, int d) { return (size_t)2 * workgroups * rows * d * 4; }
 inline size_t paged_launch_bytes(int workgroups, int rows, int d) { return (size_t)2 * workgroups * rows * (d + 4) * 4; }
+// Workgroups of the combine kernel: no more than are resident at a time, which find their sequences once.
+inline unsigned paged_combine_grid(const da_paged& p, int rows) {
+  return (unsigned)std::min(paged_units(p, rows) * p.Hkv * (rows * p.d / 1024), (long long)4 * kComputeUnits);
+}
 // `most` workgroups are resident at a time. Ranges, unless no sequence is long enough for two of them, with what fits the scratch.
 inline PagedLaunch paged_launch(const da_paged& p, int rows, int keys, int most, size_t scratch_bytes) {
   const long long room = ((long long)p.max_pages * p.page_size + keys - 1) / keys;
