@@ -43,14 +43,16 @@ struct Places {
     va = row_l * ROWB + (((lane >> 4) & 1) ^ v_swizzle<ROWB>(row_l)) * 32 + 8 * (lane & 3);
   }
   // 16 rows of K or V, `bytes` of them from `from` on
+  template <bool ONCE = false>
   __device__ void load_k(const char* from, unsigned bytes, int row_bytes, char* to) const {
     const int c = here(kc);
 #pragma unroll
-    for (int j = 0; j < LPG; ++j) load_lds(from, bytes, row + (c ^ (j * 64)), j * RPL * row_bytes, to + j * 1024);
+    for (int j = 0; j < LPG; ++j) load_lds<ONCE>(from, bytes, row + (c ^ (j * 64)), j * RPL * row_bytes, to + j * 1024);
   }
+  template <bool ONCE = false>
   __device__ void load_v(const char* from, unsigned bytes, int row_bytes, char* to) const {
 #pragma unroll
-    for (int j = 0; j < LPG; ++j) load_lds(from, bytes, v, j * RPL * row_bytes, to + j * 1024);
+    for (int j = 0; j < LPG; ++j) load_lds<ONCE>(from, bytes, v, j * RPL * row_bytes, to + j * 1024);
   }
   // operands of the products: rows 32 mb + lq of K, channels 16 s + 8 hh ..; rows 16 tt .. of V, channels 32 mb ..
   __device__ static bf16x8 k_operand(const char* tile, int ka, int mb, int s) { return *(const bf16x8*)(tile + (ka ^ (s * 32)) + mb * 32 * ROWB); }
@@ -147,6 +149,9 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
         const int t = first + (lane / GROUPS) * WAVES;
         return page_window(table, t * FT + lane % GROUPS * 16, n_seen, page_size, n_pages, page_bytes, row_bytes);
       };
+      // Every key is read once. Calls that read more than the caches hold (256 MB) leave them alone: B1 H16 100003 keys d128 171 -> 159 us, 64
+      // sequences of 5 on 4096 159 -> 144; smaller ones may find in them what a program read a step ago (14 sequences of 1100-3900 39, 41 so).
+      const bool once = (long long)line.total * Hkv * (2 * TILEB) > 256LL << 20;
       // Two windows, the second from the middle of the first on; it takes the first's place when that half is asked for.
       PageWindow now = window_of(tile), next = window_of(tile + WINDOW / 2 * WAVES);
       int at = 0;   // place in the window of the tile that is asked for
@@ -160,8 +165,15 @@ __global__ __launch_bounds__(kChunkThreads, 2) void paged_chunk_kernel(
           const int rows = min(n_seen - (t * FT + 16 * g), 16);
           const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
           there |= is << g;
-          if constexpr (decltype(of_k)::value) at_lane.load_k(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + g * LPG * 1024);
-          else at_lane.load_v(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + g * LPG * 1024);
+          const char* rows_at = from + (lo | (uint64_t)hi << 32);
+          char* rows_to = to + g * LPG * 1024;
+          if constexpr (decltype(of_k)::value) {
+            if (once) at_lane.template load_k<true>(rows_at, bytes, row_bytes, rows_to);
+            else at_lane.load_k(rows_at, bytes, row_bytes, rows_to);
+          } else {
+            if (once) at_lane.template load_v<true>(rows_at, bytes, row_bytes, rows_to);
+            else at_lane.load_v(rows_at, bytes, row_bytes, rows_to);
+          }
         }
         return there;
       };

@@ -7,10 +7,12 @@ namespace da {
 namespace {
 
 // One direct load into LDS: 16 bytes a lane from `offset` and `more` (of all lanes) bytes behind base, zeros where they end behind `bytes`.
+// ONCE: what is read is not kept in the caches for longer.
+template <bool ONCE = false>
 __device__ inline void load_lds(const char* base, unsigned bytes, int offset, int more, char* to) {
   typedef __attribute__((address_space(3))) void lds_void;
   const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)to, 16, offset, more, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)to, 16, offset, more, 0, ONCE ? 2 : 0);
 }
 
 // Whether one of eight values is an infinity or a NaN.
