@@ -11,7 +11,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["attn_bf16_bc64.hip", "attn_bf16_bc128.hip", "attn_bf16_bc32.hip", "api.hip", "lsh_group.hip",
            "kt_prepass.hip", "attn_bf16.hip", "attn_bf16_few.hip", "attn_bf16_short.hip",
            "attn_f32.hip", "attn_f32_bwd.hip", "attn_bf16_bwd.hip",
-           "qk_norm_rope.hip", "cache_append.hip", "attn_paged.hip", "attn_paged_chunk.hip", "attn_paged_f32.hip"]
+           "qk_norm_rope.hip", "cache_append.hip", "attn_paged.hip", "attn_paged_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          # packed-fp32 VALU forms are switched off for every kernel of this library

@@ -1,13 +1,18 @@
-// Attention of new tokens over a paged cache, bf16: single tokens and short chunks. Work split: paged_units.h.
+// Attention of new tokens over a paged cache, bf16: single tokens to chunks of a prompt. Work split: paged_units.h.
 //
 //   O = softmax(scale Q K^T) V over the keys that a row sees, one pass: running maximum and sum of every row.
 //
-// Bound: reading the keys and values once. A unit is 32 query rows of a kv head (all of its query heads share every tile); the
-// four waves of a workgroup deal its key tiles out among themselves, each with a softmax state of its own: no barrier on the walk. A wave's
-// tile is 8 KB of K and of V, brought into LDS by direct loads one tile ahead, 16 keys at a time: 16 rows lie in one page, so
-// that a scalar base and limit place them, and rows behind the sequence's end or on a page that is none of the cache's come as zeros and are never
-// read. The page table's entries are loaded for 64 such groups at once, a lane for each.
-// Operand layouts as in attn_bf16_few.hip.
+// A unit is up to 128 query rows of a sequence and a kv head, all of its query heads together, so that grouped heads share every tile. One workgroup of
+// eight waves per compute unit (its tiles take the LDS), two to a SIMD, one exponentiating while the other multiplies.
+//   more than 32 rows: four wave pairs own 32 rows each, and each wave of a pair walks half of the unit's tiles (64 keys) in buffers
+//     of its half's own. Bound: the matrix products (at d = 64 the exponentials beside them). Loop, layouts, online softmax and
+//     the exchange of the halves are those of attn_bf16_impl.h.
+//   up to 32 rows (decoding): every wave has all rows and every eighth tile of 8 KB. Bound: reading the keys and values.
+// Tiles come 16 keys at a time, which lie in one page, by a scalar base and limit: rows behind the sequence's end, and keys on
+// pages that are none of the cache's, are never read. The page table's entries are held for the tiles ahead, a lane for each, with a bit for
+// those that lie in the cache.
+// Measured, us: 64 sequences of up to 8192 tokens, H32 Hkv8 d64 109 (5.8 TB/s); one of 100003, H16 d128 158 (5.2 TB/s); 2048 tokens on 16384,
+// H32 Hkv8, d64 293 (880 TFLOP/s), d128 514 (1000); two chunks of 250 beside 14 single tokens d128 80.
 #include <cfloat>
 
 #include "attn_bf16_impl.h"
@@ -19,63 +24,88 @@ namespace da {
 
 namespace {
 
-constexpr int kFewRows = 32, kFewWaves = 4, kFewThreads = kFewWaves * 64;
-constexpr int kFewTileBytes = 8192;   // of K, and of V, per wave and buffer
-template <int D>
-constexpr int kFewKeys = kFewTileBytes / (2 * D);
+constexpr int kUnitRows = 128, kTileKeys = 64, kRW = 4, kHalves = 2, kThreads = kRW * kHalves * 64;
 
-// STATS: row statistics are asked for. They take a sum of their own, of the weights before they are rounded (the sum over the rounded ones is
-// off by their rounding, 1e-4 of a statistic).
+// Nothing is known of x from here on: what is computed of it stays where it is used, instead of in registers that the walk has not got.
+__device__ inline int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// A lane's places: in the loads of 16 keys, and in the operands. Swizzles as in attn_bf16_impl.h; they are exclusive ors, so that
+// load j and operands s and mb differ from the first by one, too.
+template <int D>
+struct Places {
+  static constexpr int ROWB = D * 2, CH = D / 8, LPG = 16 * ROWB / 1024, RPL = 16 / LPG;   // loads of 16 keys, rows of one
+  int lq, hh;
+  int row, kc, v, ka, va;
+  __device__ Places(int lane, int row_bytes) {
+    lq = lane & 31;
+    hh = lane >> 5;
+    const int pc = lane % CH;
+    row = lane / CH * row_bytes;
+    kc = (pc ^ (lane >> 4)) * 16;
+    v = row + ((((pc >> 1) ^ v_swizzle<ROWB>(lane / CH)) << 1) | (pc & 1)) * 16;
+    ka = lq * ROWB + (hh ^ (D == 128 ? (lq & 15) : ((lq >> 1) & 7))) * 16;
+    const int row_l = 4 * hh + ((lane & 15) >> 2);
+    va = row_l * ROWB + (((lane >> 4) & 1) ^ v_swizzle<ROWB>(row_l)) * 32 + 8 * (lane & 3);
+  }
+  // 16 rows of K or V, `bytes` of them from `from` on
+  template <bool ONCE = false>
+  __device__ void load_k(const char* from, unsigned bytes, int row_bytes, char* to) const {
+    const int c = here(kc);
+#pragma unroll
+    for (int j = 0; j < LPG; ++j) load_lds<ONCE>(from, bytes, row + (c ^ (j * 64)), j * RPL * row_bytes, to + j * 1024);
+  }
+  template <bool ONCE = false>
+  __device__ void load_v(const char* from, unsigned bytes, int row_bytes, char* to) const {
+#pragma unroll
+    for (int j = 0; j < LPG; ++j) load_lds<ONCE>(from, bytes, v, j * RPL * row_bytes, to + j * 1024);
+  }
+  // operands of the products: rows 32 mb + lq of K, channels 16 s + 8 hh ..; rows 16 tt .. of V, channels 32 mb ..
+  __device__ static bf16x8 k_operand(const char* tile, int ka, int mb, int s) { return *(const bf16x8*)(tile + (ka ^ (s * 32)) + mb * 32 * ROWB); }
+  __device__ static bf16x8 v_operand(const char* tile, int va, int tt, int mb) {
+    const char* p0 = tile + (va ^ (mb * 64)) + 16 * tt * ROWB;
+    return lds_read_tr_pair<bf16x8>(p0, p0 + 8 * ROWB);
+  }
+};
+
 template <int D, bool STATS>
-__global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
+__global__ __launch_bounds__(kThreads, 2) void paged_kernel(
     const bf16* __restrict__ q, const bf16* __restrict__ k_pages, const bf16* __restrict__ v_pages, bf16* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int row_bytes, int64_t q_token,
     int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat) {
-  constexpr int ROWB = D * 2, CH = D / 8, KT = kFewKeys<D>;
-  constexpr int MB = KT / 32, TT = KT / 16, KS = D / 16, NMB = D / 32;
-  constexpr int GROUPS = KT / 16, LPG = 16 * ROWB / 1024;   // groups of 16 keys in a tile, direct loads of one
-  constexpr int CPT = GROUPS * LPG;
-  constexpr int WINDOW = 64 / GROUPS;                       // a wave's tiles in a page window
-  __shared__ __attribute__((aligned(1024))) char k_lds0[kFewWaves][kFewTileBytes];
-  __shared__ __attribute__((aligned(1024))) char k_lds1[kFewWaves][kFewTileBytes];
-  __shared__ __attribute__((aligned(1024))) char v_lds0[kFewWaves][kFewTileBytes];
-  __shared__ __attribute__((aligned(1024))) char v_lds1[kFewWaves][kFewTileBytes];
-  __shared__ f32x4 stat_lds[kFewWaves][kFewRows];   // reference, sum, sum before rounding
+  constexpr int BC = kTileKeys, ROWB = D * 2, TILEB = BC * ROWB;
+  constexpr int MB = BC / 32, TT = BC / 16, KSTEPS = D / 16, NMB = D / 32;
+  constexpr int LPG = 16 * ROWB / 1024;   // direct loads of 16 keys
+  constexpr float kSumTrigger = (BC / 2) * 256.0f;   // (as in attn_bf16_impl.h)
+  // Two tiles of K and V for each half; or, with few rows, one of 8 KB for each wave.
+  constexpr int FEWB = 8192, FT = FEWB / ROWB, BUFB = 4 * FEWB;
+  static_assert(kHalves * TILEB <= BUFB, "a buffer holds the halves' tiles");
+  __shared__ __attribute__((aligned(1024))) char k_lds0[BUFB];
+  __shared__ __attribute__((aligned(1024))) char k_lds1[BUFB];
+  __shared__ __attribute__((aligned(1024))) char v_lds0[BUFB];
+  __shared__ __attribute__((aligned(1024))) char v_lds1[BUFB];
+  __shared__ f32x4 few_stat[kRW * kHalves][32];
 
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lq = lane & 31, hh = lane >> 5;
+  const int rw = wave % kRW, half = wave / kRW;
   const int group = H / Hkv;
-  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, (int)min((long long)max_pages * page_size, 0x7fffffffLL), causal};
+  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
+  auto k_buf = [&](int par) -> char* { return (par ? k_lds1 : k_lds0) + half * TILEB; };
+  auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
 
-  // lanes' places in a group's loads
-  int dma_k[LPG], dma_v[LPG];
-#pragma unroll
-  for (int j = 0; j < LPG; ++j) {
-    const int slot = j * 64 + lane, row = slot / CH, pc = slot % CH;
-    dma_k[j] = row * row_bytes + (pc ^ (D == 128 ? (row & 15) : ((row >> 1) & 7))) * 16;
-    dma_v[j] = row * row_bytes + ((((pc >> 1) ^ v_swizzle<ROWB>(row)) << 1) | (pc & 1)) * 16;
-  }
-  // and in the operands
-  int ka_off[KS], va_off[NMB];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) ka_off[s] = lq * ROWB + ((2 * s + hh) ^ (D == 128 ? (lq & 15) : ((lq >> 1) & 7))) * 16;
-  {
-    const int row_l = 4 * hh + ((lane & 15) >> 2);
-#pragma unroll
-    for (int mb = 0; mb < NMB; ++mb)
-      va_off[mb] = row_l * ROWB + ((2 * mb + ((lane >> 4) & 1)) ^ v_swizzle<ROWB>(row_l)) * 32 + 8 * (lane & 3);
-  }
-
-  // this workgroup's range of the line
-  const PagedLine<kFewRows, KT> line(batch);
+  const PagedLine<kUnitRows, BC> line(batch);
   long long pos = 0, end = 1, per_head = 1, length = 1;
+  int wg = blockIdx.x;
   if (ranges) {
+    // Ranges that follow each other on one XCD: their units read the same keys.
+    if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
     per_head = line.total;
     length = paged_range(per_head * Hkv, gridDim.x, least);
-    pos = paged_cut(line, blockIdx.x, length, per_head * Hkv, per_head);
-    end = paged_cut(line, blockIdx.x + 1LL, length, per_head * Hkv, per_head);
+    pos = paged_cut(line, wg, length, per_head * Hkv, per_head);
+    end = paged_cut(line, wg + 1LL, length, per_head * Hkv, per_head);
   }
   while (pos < end) {
     PagedUnit u;
@@ -87,263 +117,563 @@ __global__ __launch_bounds__(kFewThreads, 1) void paged_few_kernel(
       t0 = (int)(at - u.first);
       t1 = (int)min((long long)u.tiles, t0 + (end - pos));
     } else {
-      head = blockIdx.x % Hkv;
-      if (!line.template find<true>(blockIdx.x / Hkv, &u)) return;
+      // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
+      head = wg % Hkv;
+      if (!line.template find<true>(wg / Hkv, &u)) return;
+      u.m0 = (u.rows - 1) / kUnitRows * kUnitRows - u.m0;
       t0 = 0;
       t1 = u.tiles;
     }
     const bool whole = t0 == 0 && t1 == u.tiles;
     pos += t1 - t0;
 
-    const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
-    const int token = u.q0 + m_ld / group;
     const int n_keys = min(u.len, batch.max_keys);
-    const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
-    // no row of the unit sees more
-    const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (min(u.m0 + kFewRows, u.rows) - 1) / group + 1, 0)) : n_keys;
+    const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (min(u.m0 + kUnitRows, u.rows) - 1) / group + 1, 0)) : n_keys;   // no row sees more
     const int all_see = causal ? min(max(u.len - u.nq + u.m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
-    const int t_end = min(t1, (n_seen + KT - 1) / KT);
-    const bf16* q_row = q + token * q_token + (head * group + m_ld % group) * q_head;
-    bf16x8 qop[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
-
     const int* table = page_table + (int64_t)u.seq * max_pages;
     const char* k_base = (const char*)k_pages + head * head_bytes;
     const char* v_base = (const char*)v_pages + head * head_bytes;
-    int tile = t0 + wave;
-    // the window's lane for this wave's tile tile + 4 i is that of i * GROUPS, and of the groups of 16 keys behind it
-    auto window_of = [&](int first) {
-      const int t = first + (lane / GROUPS) * kFewWaves;
-      return page_window(table, t * KT + lane % GROUPS * 16, n_seen, page_size, n_pages, page_bytes, row_bytes);
-    };
-    PageWindow window = window_of(tile), window_next = window_of(tile + WINDOW * kFewWaves);
-    int in_window = 0;
-    // The next tile in turn; returns a bit for each group of it that lies in the cache.
-    auto load_tile = [&](auto par_c, int t) -> int {
-      if (in_window == WINDOW) {
-        in_window = 0;
-        window = window_next;
-        window_next = window_of(t + WINDOW * kFewWaves);
-      }
-      char* kd = decltype(par_c)::value ? k_lds1[wave] : k_lds0[wave];
-      char* vd = decltype(par_c)::value ? v_lds1[wave] : v_lds0[wave];
+
+    if (u.rows - u.m0 <= 32) {
+      // ---- few rows: a wave has all of them, and every eighth tile of 8 KB. Bound: reading the keys and values. ----
+      // Each wave has a softmax state of its own and no barrier; K of its next tile is asked for when the scores are
+      // taken, V when it is multiplied, so that 128 KB a compute unit are on their way most of the time.
+      constexpr int GROUPS = FT / 16, FMB = FT / 32, FTT = FT / 16, CPT = FEWB / 1024, WINDOW = 64 / GROUPS, WAVES = kRW * kHalves;
+      const int lane = here(tid) & 63;
+      const Places<D> at_lane(lane, row_bytes);
+      const int lq = at_lane.lq, hh = at_lane.hh;
+      const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);
+      const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
+      const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);
+      bf16x8 qop[KSTEPS];
+      const bf16* q_row = q + token * q_token + q_of * q_head;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
+      int tile = t0 * (BC / FT) + wave;
+      const int t_end = min(t1 * (BC / FT), (n_seen + FT - 1) / FT);
+      // the window's lane for this wave's tile tile + 8 i is that of i * GROUPS, and of the groups of 16 keys behind it
+      auto window_of = [&](int first) {
+        const int t = first + (lane / GROUPS) * WAVES;
+        return page_window(table, t * FT + lane % GROUPS * 16, n_seen, page_size, n_pages, page_bytes, row_bytes);
+      };
+      // Every key is read once. Calls that read more than the caches hold (256 MB) leave them alone: B1 H16 100003 keys d128 171 -> 159 us, 64
+      // sequences of 5 on 4096 159 -> 144; smaller ones may find in them what a program read a step ago (14 sequences of 1100-3900 39, 41 so).
+      const bool once = (long long)line.total * Hkv * (2 * TILEB) > 256LL << 20;
+      // Two windows, the second from the middle of the first on; it takes the first's place when that half is asked for.
+      PageWindow now = window_of(tile), next = window_of(tile + WINDOW / 2 * WAVES);
+      int at = 0;   // place in the window of the tile that is asked for
+      auto ask = [&](auto of_k, const char* from, int t, char* to) -> int {
+        int there = 0;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          const int l = at * GROUPS + g;
+          const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l);
+          const int is = __builtin_amdgcn_readlane(now.there, l);
+          const int rows = min(n_seen - (t * FT + 16 * g), 16);
+          const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
+          there |= is << g;
+          const char* rows_at = from + (lo | (uint64_t)hi << 32);
+          char* rows_to = to + g * LPG * 1024;
+          if constexpr (decltype(of_k)::value) {
+            if (once) at_lane.template load_k<true>(rows_at, bytes, row_bytes, rows_to);
+            else at_lane.load_k(rows_at, bytes, row_bytes, rows_to);
+          } else {
+            if (once) at_lane.template load_v<true>(rows_at, bytes, row_bytes, rows_to);
+            else at_lane.load_v(rows_at, bytes, row_bytes, rows_to);
+          }
+        }
+        return there;
+      };
+      const std::true_type of_k;
+      const std::false_type of_v;
+      char* kb = (wave < 4 ? k_lds0 : k_lds1) + (wave & 3) * FEWB;
+      char* vb = (wave < 4 ? v_lds0 : v_lds1) + (wave & 3) * FEWB;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
       int there = 0;
+      if (tile < t_end) {
+        there = ask(of_k, k_base, tile, kb);
+        ask(of_v, v_base, tile, vb);
+      }
+      f32x16 oacc[NMB];
 #pragma unroll
-      for (int g = 0; g < GROUPS; ++g) {
-        const int from = in_window * GROUPS + g;
-        const uint64_t off = (uint32_t)__builtin_amdgcn_readlane((int)window.lo, from) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)window.hi, from) << 32;
-        const int is = __builtin_amdgcn_readlane(window.there, from);
-        const int rows = min(n_seen - (t * KT + 16 * g), 16);   // (`is` says that there is one)
-        const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
-        there |= is << g;
+      for (int mb = 0; mb < NMB; ++mb)
 #pragma unroll
-        for (int j = 0; j < LPG; ++j) {
-          load_lds(k_base + off, bytes, dma_k[j], 0, kd + (g * LPG + j) * 1024);
-          load_lds(v_base + off, bytes, dma_v[j], 0, vd + (g * LPG + j) * 1024);
+        for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
+      // The reference is the largest score so far, unscaled (a scaled one is rounded, which shows on large scores).
+      float ref = -FLT_MAX, l_run = 0.0f, e_run = 0.0f;
+      for (; tile < t_end; tile += WAVES) {
+        const int seen = there;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // K is there
+        const int ka = here(at_lane.ka), va = here(at_lane.va);
+        f32x16 sc[FMB];
+#pragma unroll
+        for (int mb = 0; mb < FMB; ++mb) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[mb][i] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < KSTEPS; ++s) sc[mb] = mfma_32x32x16(at_lane.k_operand(kb, ka, mb, s), qop[s], sc[mb]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // and read
+        const bool more = tile + WAVES < t_end;
+        if (more) {
+          ++at;
+          there = ask(of_k, k_base, tile + WAVES, kb);
+        }
+        const int n0 = tile * FT;
+        const bool some = n0 + FT > all_see || seen != (1 << GROUPS) - 1;
+        if (some) {
+#pragma unroll
+          for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (n0 + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(seen >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[mb][i]);
+        const float ref_new = fmaxf(ref, half_swap_max(mx));
+        if (__builtin_amdgcn_ballot_w64(ref_new > ref) != 0) {
+          const float alpha = __builtin_amdgcn_exp2f((ref - ref_new) * scale_log2e);
+          l_run *= alpha;
+          if constexpr (STATS) e_run *= alpha;
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+          ref = ref_new;
+        }
+        // P rounded to bf16 as the operands of P.V; the row sum is taken over the rounded values, so that the rounding of a row's
+        // largest weights cancels
+        bf16x8 pop[FTT];
+        const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+#pragma unroll
+        for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float x0 = __builtin_amdgcn_exp2f((sc[mb][i] - ref) * scale_log2e), x1 = __builtin_amdgcn_exp2f((sc[mb][i + 1] - ref) * scale_log2e);
+            const bf16x2 pr = {(bf16)x0, (bf16)x1};
+            if constexpr (STATS) e_run += x0 + x1;
+            pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
+            pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
+            l_run = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run, false);
+          }
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // V is there
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
+        bool odd = false;
+        if (some) odd = any_odd<FTT, NMB>(v_operand);
+        if (odd) {
+          odd_values<FTT, NMB>(oacc, pop, v_operand);
+        } else {
+#pragma unroll
+          for (int tt = 0; tt < FTT; ++tt)
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(v_operand(tt, mb), pop[tt], oacc[mb]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) ask(of_v, v_base, tile + WAVES, vb);
+        if (at == WINDOW / 2) {   // (the next to be asked for is behind it)
+          at = 0;
+          now = next;
+          next = window_of(tile + (1 + WINDOW / 2) * WAVES);
+        }
+        // (the wait behind these products as in attn_bf16_few.hip)
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 1");
+      }
+      // the waves' states meet
+      const float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
+      if (hh == 0) few_stat[wave][lq] = f32x4{ref, l_tot, e_tot, 0.0f};
+      __syncthreads();
+      float ref_all = few_stat[0][lq][0], l_all = 0.0f, e_all = 0.0f;
+#pragma unroll
+      for (int j = 1; j < WAVES; ++j) ref_all = fmaxf(ref_all, few_stat[j][lq][0]);
+#pragma unroll
+      for (int j = 0; j < WAVES; ++j) {
+        const f32x4 st = few_stat[j][lq];
+        const float x = __builtin_amdgcn_exp2f((st[0] - ref_all) * scale_log2e);
+        l_all += st[1] * x;
+        e_all += st[2] * x;
+      }
+      // (a row that sees nothing has sum 0 and is 0)
+      const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
+      // wave w's sums: 32 rows of D floats in its own buffers (K at d = 64, K and V at d = 128), the 16-byte pieces exchanged by the row
+#pragma unroll
+      for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int piece = 8 * mb + 2 * i4 + hh;   // channels 4*piece ..
+          float* dst = (float*)(mb < 2 ? kb : vb);
+          const f32x4 x = {oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
+          *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
+        }
+      __syncthreads();
+      const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows;
+      for (int i = tid; i < min(u.rows - u.m0, 32) * (D / 4); i += kThreads) {
+        const int row = i / (D / 4), piece = i % (D / 4), mr = u.m0 + row;
+        const int at = row * 256 + (((piece & 15) ^ (row & 15)) << 4);
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < WAVES; ++j) {
+          const char* of = piece < 16 ? (j < 4 ? k_lds0 : k_lds1) : (j < 4 ? v_lds0 : v_lds1);
+          x += *(const f32x4*)(of + (j & 3) * FEWB + at);
+        }
+        if (whole) {
+          const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+          *(bf16x4*)(o + ((int64_t)(u.q0 + mr / group) * H + head * group + mr % group) * D + piece * 4) = y;
+        } else {
+          *(f32x4*)(part_o + (slot + row) * D + piece * 4) = x;
         }
       }
-      ++in_window;
-      return there;
-    };
-    const std::integral_constant<int, 0> even;
-    const std::integral_constant<int, 1> odd;
+      if (wave == 0 && hh == 0 && m < u.rows) {
+        if (!whole) part_stat[slot + lq] = f32x4{ref_all * scale_log2e, l_all, e_all, 0.0f};
+        else if (STATS) lse[(int64_t)token * H + q_of] = row_statistic(ref_all * scale_log2e, e_all);
+      }
+      __syncthreads();   // (the next unit's tiles take the place of the sums)
+      continue;
+    }
+    const int lane = here(tid) & 63;
+    const Places<D> at_lane(lane, row_bytes);
+    const int lq = at_lane.lq, hh = at_lane.hh;
+    const int m = u.m0 + rw * 32 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
+    const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
+    const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
+    const int seen_tiles = (n_seen + BC - 1) / BC;
+    // the halves' tiles; a half without any walks one behind the last key: zeros, masked out
+    const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + 1) / 2, 1);
+    const int n_tiles = half ? max(n_all - n_most, 1) : n_most;
+    const int tile0 = half ? (n_all > 1 ? t0 + n_most : seen_tiles) : (n_all > 0 ? t0 : seen_tiles);
+    const bool idle = u.m0 + rw * 32 >= u.rows;   // a wave without rows brings its part of the tiles in
+
+    bf16x8 qop[KSTEPS];
+    {
+      const bf16* q_row = q + token * q_token + q_of * q_head;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
-    int there = tile < t_end ? load_tile(even, tile) : 0;
+      for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
+    }
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
+
+    // Lane i: where the wave's 16 keys of tile (first + i) of the half lie, and which of the tile's groups lie in the cache.
+    struct Window {
+      uint32_t lo, hi;
+      int there;
+    };
+    auto window_of = [&](int first) {
+      Window w = {0, 0, 0};
+      const int key = (tile0 + first + lane) * BC;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const PageWindow p = page_window(table, key + 16 * g, n_seen, page_size, n_pages, page_bytes, row_bytes);
+        w.there |= p.there << g;
+        if (g == rw) {
+          w.lo = p.lo;
+          w.hi = p.hi;
+        }
+      }
+      return w;
+    };
+    // Two windows, the second from the middle of the first on; it takes the first's place when that half is done with.
+    int base = 0;
+    Window now = window_of(0), next = window_of(32);
+    auto advance = [&](int it) {   // tiles before `it` are done with: those up to it + 31 lie in the window from here on
+      if (it < base + 32) return;
+      base += 32;
+      now = next;
+      next = window_of(base + 32);
+    };
+    auto there_of = [&](int it) { return __builtin_amdgcn_readlane(now.there, it - base); };
+    const std::true_type yes;
+    const std::false_type no;
+    auto load_group = [&](auto of_k, const char* from, int it, char* to) {
+      const int l = it - base;
+      const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l);
+      const int is = there_of(it) >> rw & 1;
+      const int rows = min(n_seen - ((tile0 + it) * BC + 16 * rw), 16);
+      const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
+      if constexpr (decltype(of_k)::value) at_lane.load_k(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + rw * LPG * 1024);
+      else at_lane.load_v(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + rw * LPG * 1024);
+    };
+    // What tile `it` brings in: K(it + 2) where K(it) was, V(it + 1) where V(it - 1) was.
+    auto feed = [&](int it, int par) {
+      if (it + 2 < n_tiles) load_group(yes, k_base, it + 2, k_buf(par));
+      load_group(no, v_base, it + 1, v_buf(par ^ 1));
+    };
+    auto dma_wait = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+    auto masked = [&](int it) { return (tile0 + it) * BC + BC > all_see || there_of(it) != 15; };
 
     f32x16 oacc[NMB];
 #pragma unroll
     for (int mb = 0; mb < NMB; ++mb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
-    // The reference is the largest score so far, unscaled (a scaled one is rounded, which shows on large scores).
-    float ref = -FLT_MAX, l_run = 0.0f, e_run = 0.0f;   // the sums are over this lane's half of the keys
+    float nref = 0.0f, l_run = 0.0f, e_run = 0.0f;   // negated reference (exp2 domain), sums over this lane's half of the keys
+    // Below zero until the row has met a score above -infinity: its first one becomes the reference.
+    float trigger = kSumTrigger;
 
-    auto step = [&](auto par_c, int t) {
-      constexpr int par = decltype(par_c)::value;
-      const char* kb = par ? k_lds1[wave] : k_lds0[wave];
-      const char* vb = par ? v_lds1[wave] : v_lds0[wave];
-      const int seen = there;
-      // the next tile into the other buffer, whose reads are done; then this tile has to be there
-      if (t + kFewWaves < t_end) {
-        there = load_tile(std::integral_constant<int, par ^ 1>(), t + kFewWaves);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"i"(2 * CPT) : "memory");
-      } else {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      }
-      f32x16 sc[MB];
+    auto qk = [&](int par, f32x16 (&sacc)[MB]) {
+      const char* at = k_buf(par);
+      const int ka = here(at_lane.ka);
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[mb][i] = 0.0f;
+        for (int i = 0; i < 16; ++i) sacc[mb][i] = 0.0f;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) sc[mb] = mfma_32x32x16(*(const bf16x8*)(kb + ka_off[s] + mb * 32 * ROWB), qop[s], sc[mb]);
+        for (int s = 0; s < KSTEPS; ++s) sacc[mb] = mfma_32x32x16(at_lane.k_operand(at, ka, mb, s), qop[s], sacc[mb]);
       }
-      const int n0 = t * KT;
-      auto v_operand = [&](int tt, int mb) {
-        const char* p0 = vb + va_off[mb] + 16 * tt * ROWB;
-        return lds_read_tr_pair<bf16x8>(p0, p0 + 8 * ROWB);
-      };
-      bool odd = false;
-      if (n0 + KT > all_see || seen != (1 << GROUPS) - 1) {
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (n0 + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(seen >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
-        odd = any_odd<TT, NMB>(v_operand);
-      }
-      float mx = sc[0][0];
+    };
+    auto apply_mask = [&](int it, f32x16 (&sc)[MB]) {
+      const int there = there_of(it);
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[mb][i]);
-      const float ref_new = fmaxf(ref, half_swap_max(mx));
-      if (__builtin_amdgcn_ballot_w64(ref_new > ref) != 0) {
-        const float alpha = __builtin_amdgcn_exp2f((ref - ref_new) * scale_log2e);
-        l_run *= alpha;
-        if constexpr (STATS) e_run *= alpha;
+        for (int i = 0; i < 16; ++i)
+          if ((tile0 + it) * BC + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(there >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
+    };
+    auto tile_max = [&](const f32x16 (&sc)[MB]) -> float {
+      float mt = sc[0][0];
 #pragma unroll
-        for (int mb = 0; mb < NMB; ++mb)
+      for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
-        ref = ref_new;
-      }
-      // P rounded to bf16 as the operands of P.V; the row sum is taken over the rounded values, so that the rounding of a row's
-      // largest weights cancels
-      bf16x8 pop[TT];
-      const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[mb][i]);
+      return __builtin_fmaf(half_swap_max(mt), scale_log2e, nref);
+    };
+    auto exp_tile = [&](const f32x16 (&sc)[MB], bf16x8 (&pop)[TT]) -> float {   // -> sum before rounding, with STATS
+      float sum = 0.0f;
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          const float x0 = __builtin_amdgcn_exp2f((sc[mb][i] - ref) * scale_log2e), x1 = __builtin_amdgcn_exp2f((sc[mb][i + 1] - ref) * scale_log2e);
+          const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], scale_log2e, nref));
+          const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i + 1], scale_log2e, nref));
           const bf16x2 pr = {(bf16)x0, (bf16)x1};
-          if constexpr (STATS) e_run += x0 + x1;
           pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
           pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
-          l_run = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run, false);
+          if constexpr (STATS) sum += x0 + x1;
         }
-      if (odd) {
+      return sum;
+    };
+    const RowSum row_sum(lane);
+    auto shift_reference = [&](float delta) {
+      nref -= delta;
+      const float alpha = __builtin_amdgcn_exp2f(fminf(-delta, 0.0f));   // (a first reference has no sums)
+      l_run *= alpha;
+      if constexpr (STATS) e_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+    };
+    // One tile, as in attn_bf16_impl.h. clean_c: neither it nor the next needs the mask.
+    auto body = [&](auto clean_c, auto next_c, int it, int par, f32x16 (&sc)[MB], f32x16 (&sn)[MB]) {
+      constexpr bool CLEAN = decltype(clean_c)::value, HAS_NEXT = decltype(next_c)::value;
+      if constexpr (HAS_NEXT) {
+        feed(it, par);
+        qk(par ^ 1, sn);
+      }
+      bf16x8 pop[TT];
+      float es = exp_tile(sc, pop);
+      float rs = row_sum(pop);
+      if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
+        const float mt = tile_max(sc);
+        const bool first = trigger < 0.0f && mt > -INFINITY;
+        if (first) trigger = kSumTrigger;
+        shift_reference(mt > kTau || first ? mt : 0.0f);
+        es = exp_tile(sc, pop);
+        rs = RowSum::by_lanes(pop);
+      }
+      l_run += rs;
+      if constexpr (STATS) e_run += es;
+      const char* vb = v_buf(par);
+      const int va = here(at_lane.va);
+      auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
+      bool odd = false;
+      if constexpr (!CLEAN) {
+        if (masked(it)) odd = any_odd<TT, NMB>(v_operand);
+      }
+      if (!CLEAN && odd) {
         odd_values<TT, NMB>(oacc, pop, v_operand);
-        return;
+      } else {
+        constexpr int PF = (4 / NMB < TT) ? 4 / NMB : TT - 1;
+        bf16x8 va[PF + 1][NMB];
+#pragma unroll
+        for (int s = 0; s < PF; ++s)
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb) va[s][mb] = v_operand(s, mb);
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt) {
+          if (tt + PF < TT) {
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) va[(tt + PF) % (PF + 1)][mb] = v_operand(tt + PF, mb);
+          }
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(va[tt % (PF + 1)][mb], pop[tt], oacc[mb]);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * NMB * PF, 0);
+#pragma unroll
+        for (int i = 0; i < (TT - PF) * NMB; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, PF * NMB, 0);
+      }
+      if constexpr (!CLEAN) {   // (the wait behind these products as in attn_bf16_few.hip)
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 3");
+      }
+      if constexpr (HAS_NEXT) {
+        if constexpr (!CLEAN) {
+          if (masked(it + 1)) apply_mask(it + 1, sn);
+        }
+        dma_wait();
+      }
+      __syncthreads();
+    };
+
+    load_group(no, v_base, 0, v_buf(0));
+    load_group(yes, k_base, 0, k_buf(0));
+    if (n_tiles > 1) load_group(yes, k_base, 1, k_buf(1));
+    dma_wait();
+    __syncthreads();
+    if (idle) {
+      __syncthreads();
+      for (int it = 0; it < n_tiles - 1; ++it) {
+        advance(it);
+        feed(it, it & 1);
+        dma_wait();
+        __syncthreads();
+      }
+      __syncthreads();
+    } else {
+      f32x16 s0[MB], s1[MB];
+      qk(0, s0);
+      if (masked(0)) apply_mask(0, s0);
+      const float first_max = tile_max(s0);
+      if (first_max > -INFINITY) nref -= first_max;
+      else trigger = -1.0f;
+      __syncthreads();
+      const int n_full = min(max(all_see / BC - tile0, 0), n_tiles);   // tiles that need no mask for their place
+      int it = 0;
+      while (it < n_tiles - 1) {
+        advance(it);
+        if ((it & 1) == 0) {
+          // clean tiles of the window from `it` on
+          const uint64_t bad = __builtin_amdgcn_ballot_w64(now.there != 15) >> (it - base);
+          const int clean = min(min(n_full, it + (bad ? __builtin_ctzll(bad) : 64)), base + 62);   // (loads run three tiles ahead)
+          for (; it + 2 < clean; it += 2) {
+            body(yes, yes, it, 0, s0, s1);
+            body(yes, yes, it + 1, 1, s1, s0);
+            __builtin_amdgcn_sched_barrier(0);   // (as above, for the way out of this loop)
+            asm volatile("s_nop 3");
+          }
+          if (it == n_tiles - 1) break;
+        }
+        body(no, yes, it, it & 1, s0, s1);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) s0[mb] = s1[mb];
+        ++it;
+      }
+      advance(it);
+      body(no, no, it, it & 1, s0, s1);
+    }
+    if (n_tiles < n_most) __syncthreads();   // (the other half's last tile)
+
+    // ---- the halves meet: each hands the other one half of the channels and finishes the rest ----------------
+    constexpr int OB = NMB / 2;
+    const int c0 = half * (D / 2);
+    float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
+    static_assert(kRW * OB * 4096 <= kHalves * TILEB && kThreads / 2 * 16 <= kHalves * TILEB, "the exchange fits the tile buffers");
+    f32x4* stat = (f32x4*)k_lds0;
+    f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
+    const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
+    f32x16 out[OB];
+    if (hh == 0) stat[wave * 32 + lq] = f32x4{-nref, l_tot, e_tot, 0.0f};
+#pragma unroll
+    for (int mb = 0; mb < OB; ++mb) {
+      f32x16 theirs;
+      if (half) {
+        theirs = oacc[mb];
+        out[mb] = oacc[mb + OB];
+      } else {
+        theirs = oacc[mb + OB];
+        out[mb] = oacc[mb];
       }
 #pragma unroll
-      for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-        for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(v_operand(tt, mb), pop[tt], oacc[mb]);
-    };
-    while (tile < t_end) {
-      step(even, tile);
-      tile += kFewWaves;
-      if (tile >= t_end) break;
-      step(odd, tile);
-      // (the wait behind these products as in attn_bf16_few.hip)
-      __builtin_amdgcn_sched_barrier(0);
-      asm volatile("s_nop 1");
-      tile += kFewWaves;
+      for (int i4 = 0; i4 < 4; ++i4) give[(mb * 4 + i4) * 64] = f32x4{theirs[4 * i4], theirs[4 * i4 + 1], theirs[4 * i4 + 2], theirs[4 * i4 + 3]};
     }
-
-    // ---- the waves' states meet ----------------------------------------------------------------------
-    const float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
-    if (hh == 0) stat_lds[wave][lq] = f32x4{ref, l_tot, e_tot, 0.0f};
-    __syncthreads();   // also: nobody reads tiles any more
-    float ref_all = stat_lds[0][lq][0], l_all = 0.0f, e_all = 0.0f;
+    __syncthreads();
+    // (a half that saw nothing of a row has sum 0 and no reference; a NaN sum makes the row NaN)
+    const f32x4 st = stat[(wave ^ kRW) * 32 + lq];
+    const float mine_ref = l_tot == 0.0f ? -FLT_MAX : -nref, other_ref = st[1] == 0.0f ? -FLT_MAX : st[0];
+    const float ref = fmaxf(mine_ref, other_ref);
+    const float wm = __builtin_amdgcn_exp2f(mine_ref - ref), wo = __builtin_amdgcn_exp2f(other_ref - ref);
+    l_tot = __builtin_fmaf(wm, l_tot, wo * st[1]);
+    e_tot = __builtin_fmaf(wm, e_tot, wo * st[2]);
+    const float inv = !whole ? 1.0f : l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
 #pragma unroll
-    for (int j = 1; j < kFewWaves; ++j) ref_all = fmaxf(ref_all, stat_lds[j][lq][0]);
-#pragma unroll
-    for (int j = 0; j < kFewWaves; ++j) {
-      const f32x4 st = stat_lds[j][lq];
-      const float x = __builtin_amdgcn_exp2f((st[0] - ref_all) * scale_log2e);
-      l_all += st[1] * x;
-      e_all += st[2] * x;
-    }
-    // (a row that sees nothing has sum 0 and is 0)
-    const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
-    // wave w's sums: 32 rows of D floats, the 16-byte pieces exchanged by the row (its own buffers: K at
-    // d = 64, K and V at d = 128)
-    float* half0 = (float*)k_lds0[wave];
-    float* half1 = (float*)(D == 128 ? v_lds0[wave] : k_lds0[wave]);
-#pragma unroll
-    for (int mb = 0; mb < NMB; ++mb)
+    for (int mb = 0; mb < OB; ++mb)
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
-        const int piece = 8 * mb + 2 * i4 + hh;   // channels 4*piece ..
-        float* dst = mb < 2 ? half0 : half1;
-        const f32x4 x = {oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
-        *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
+        const f32x4 x = take[(mb * 4 + i4) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]) * inv;
       }
-    __syncthreads();
-    const size_t slot = 2 * (size_t)blockIdx.x + (t0 == 0 ? 2 : 1);   // (the part in front of the next one's cut)
-    auto finish = [&](const char (*sums)[kFewTileBytes], int c0) {   // 64 channels from c0 on
+    if (m < u.rows) {
+      const int64_t row = (int64_t)token * H + q_of;
+      const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows + rw * 32 + lq;
+      if (hh == 0 && half == 0) {
+        if (!whole) part_stat[slot] = f32x4{ref, l_tot, e_tot, 0.0f};
+        else if (STATS) lse[row] = row_statistic(ref, e_tot);
+      }
 #pragma unroll
-      for (int i = tid; i < kFewRows * 16; i += kFewThreads) {
-        const int row = i / 16, piece = i % 16, mr = u.m0 + row;
-        if (mr >= u.rows) continue;
-        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int mb = 0; mb < OB; ++mb)
 #pragma unroll
-        for (int j = 0; j < kFewWaves; ++j) x += *(const f32x4*)((const float*)sums[j] + row * 64 + ((piece ^ (row & 15)) << 2));
-        if (whole) {
-          const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
-          *(bf16x4*)(o + ((int64_t)(u.q0 + mr / group) * H + head * group + mr % group) * D + c0 + piece * 4) = y;
-        } else {
-          *(f32x4*)(part_o + (slot * kFewRows + row) * D + c0 + piece * 4) = x;
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const int c = c0 + 32 * mb + 8 * i4 + 4 * hh;
+          const f32x4 x = {out[mb][4 * i4], out[mb][4 * i4 + 1], out[mb][4 * i4 + 2], out[mb][4 * i4 + 3]};
+          if (whole) *(bf16x4*)(o + row * D + c) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+          else *(f32x4*)(part_o + slot * D + c) = x;
         }
-      }
-    };
-    finish(k_lds0, 0);
-    if constexpr (D == 128) finish(v_lds0, 64);
-    if (wave == 0 && hh == 0 && m < u.rows) {
-      if (!whole) part_stat[slot * kFewRows + lq] = f32x4{ref_all * scale_log2e, l_all, e_all, 0.0f};
-      else if (STATS) lse[(int64_t)token * H + head * group + m % group] = row_statistic(ref_all * scale_log2e, e_all);
     }
     __syncthreads();   // (the next unit's tiles take the place of the sums)
   }
 }
 
 template <int D>
-hipError_t launch_few(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
-                      const PagedLaunch& l, hipStream_t stream) {
+hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                    const PagedLaunch& l, hipStream_t stream) {
   const float scale_log2e = scale * 1.4426950408889634f;
   float* part_o = (float*)scratch;
-  f32x4* part_stat = (f32x4*)((char*)scratch + paged_sum_bytes(l.workgroups, kFewRows, D));
-  hipLaunchKernelGGL((p.lse_out ? paged_few_kernel<D, true> : paged_few_kernel<D, false>), dim3((unsigned)l.workgroups), dim3(kFewThreads), 0, stream, (const bf16*)q, (const bf16*)k_pages,
-                     (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.n_pages,
-                     p.page_size, p.max_pages, p.page_stride * 2, p.head_stride * 2, (int)(p.row_stride * 2), p.q_stride[0], p.q_stride[1],
-                     p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
+  f32x4* part_stat = (f32x4*)((char*)scratch + paged_sum_bytes(l.workgroups, kUnitRows, D));
+  hipLaunchKernelGGL((p.lse_out ? paged_kernel<D, true> : paged_kernel<D, false>), dim3((unsigned)l.workgroups), dim3(kThreads), 0,
+                     stream, (const bf16*)q, (const bf16*)k_pages, (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H,
+                     p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, p.page_stride * 2, p.head_stride * 2, (int)(p.row_stride * 2),
+                     p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kFewRows, kFewKeys<D>>), dim3(paged_combine_grid(p, kFewRows)), dim3(256), 0,
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kUnitRows, kTileKeys>), dim3(paged_combine_grid(p, kUnitRows)), dim3(256), 0,
                      stream, part_o, part_stat, (bf16*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens,
                      p.max_pages * p.page_size, l.workgroups, l.least);
   return hipGetLastError();
 }
 
-// One workgroup per compute unit (its tiles take the LDS).
-PagedLaunch few_launch(const da_paged& p, size_t scratch_bytes) {
-  return paged_launch(p, kFewRows, p.d == 64 ? kFewKeys<64> : kFewKeys<128>, kComputeUnits, scratch_bytes);
-}
-
 }  // namespace
 
-// Whether the call has sequences with enough rows for the kernel of units of 128. The host knows the rows of all of them alone.
-static bool paged_many_rows(const da_paged& p) {
-  return true;
-}
-
 size_t paged_scratch_bytes(const da_paged& p) {
-  if (p.dtype == DA_BF16 && paged_many_rows(p)) return paged_chunk_scratch_bytes(p);
-  return paged_launch_bytes(p.dtype == DA_F32 ? 2 * kComputeUnits : kComputeUnits, kFewRows, p.d);
+  return p.dtype == DA_F32 ? paged_f32_scratch_bytes(p) : paged_launch_bytes(kComputeUnits, kUnitRows, p.d);
 }
 
 hipError_t launch_paged(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                         size_t scratch_bytes, hipStream_t stream) {
   if (p.dtype == DA_F32) return launch_paged_f32(q, k_pages, v_pages, o, p, scale, scratch, scratch_bytes, stream);
-  if (paged_many_rows(p)) return launch_paged_chunk(q, k_pages, v_pages, o, p, scale, scratch, scratch_bytes, stream);
-  const PagedLaunch l = few_launch(p, scratch_bytes);
-  return p.d == 64 ? launch_few<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
-                   : launch_few<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
+  PagedLaunch l = paged_launch(p, kUnitRows, kTileKeys, kComputeUnits, scratch_bytes);
+  const long long units = (long long)p.n_tokens * (p.H / p.Hkv) / kUnitRows * p.Hkv;   // at least
+  if (units >= 2 * kComputeUnits) l = PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, l.least};
+  return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
+                   : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
 }
 
 }  // namespace da

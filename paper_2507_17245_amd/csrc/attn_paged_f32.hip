@@ -209,6 +209,8 @@ hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, voi
 
 }  // namespace
 
+size_t paged_f32_scratch_bytes(const da_paged& p) { return paged_launch_bytes(2 * kComputeUnits, kRows, p.d); }
+
 hipError_t launch_paged_f32(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                             size_t scratch_bytes, hipStream_t stream) {
   const PagedLaunch l = paged_launch(p, kRows, kTile, 2 * kComputeUnits, scratch_bytes);

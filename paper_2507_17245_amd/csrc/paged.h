@@ -30,10 +30,7 @@ hipError_t launch_cache_append(const void* k, const void* v, void* k_pages, void
 size_t paged_scratch_bytes(const da_paged& p);
 hipError_t launch_paged(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                         size_t scratch_bytes, hipStream_t stream);
-// A chunk's kernel: units of more rows.
-size_t paged_chunk_scratch_bytes(const da_paged& p);
-hipError_t launch_paged_chunk(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
-                              size_t scratch_bytes, hipStream_t stream);
+size_t paged_f32_scratch_bytes(const da_paged& p);
 hipError_t launch_paged_f32(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                             size_t scratch_bytes, hipStream_t stream);
 
