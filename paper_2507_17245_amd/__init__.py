@@ -350,6 +350,10 @@ def distr_attn_version():
 ROPE = {"none": 0, "halves": 1, "neighbours": 2}
 
 
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
 def _strides(t, what):
     """Strides of all dimensions but the last, which has to be contiguous; those of a single entry do not matter."""
     if t.stride(-1) != 1:
@@ -362,7 +366,7 @@ def _layout(t):
 
 
 def _check_layout(t, like, what):
-    if (t.shape, t.stride(), t.dtype, t.device) != like:
+    if _layout(t) != like:
         raise ValueError(f"params were made for a {what} of another shape, stride, dtype or device")
 
 
@@ -462,7 +466,7 @@ def _check_qk(params, tensors):
 def distr_attn_qk_norm_rope(q, k, q_out, k_out, params):
     """q_out, k_out = rotation(norm(q)), rotation(norm(k)), in one launch. -> (q_out, k_out)"""
     _check_qk(params, ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")))
-    _check(lib().distr_attn_qk_norm_rope(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), ctypes.byref(params)))
+    _check(lib().distr_attn_qk_norm_rope(_at(q), _at(k), _at(q_out), _at(k_out), ctypes.byref(params)))
     return q_out, k_out
 
 
@@ -480,7 +484,7 @@ def distr_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, params, dq_weight=
         shape = (params.H if of == "q" else params.Hkv, params.d) if params.rotary.weight_heads else (params.d,)
         if t.dtype != torch.float32 or tuple(t.shape) != (tuple(w.shape) if w is not None else shape) or not t.is_contiguous() or t.device != dq.device:
             raise ValueError(f"d{of}_weight must be contiguous float32 of the weight's shape")
-    _check(lib().distr_attn_qk_norm_rope_bwd(_ptr(q), _ptr(k), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk), _ptr(dq_weight), _ptr(dk_weight),
+    _check(lib().distr_attn_qk_norm_rope_bwd(_at(q), _at(k), _at(dq_out), _at(dk_out), _at(dq), _at(dk), _at(dq_weight), _at(dk_weight),
                                              ctypes.byref(params)))
     return dq, dk
 
@@ -554,7 +558,7 @@ def distr_attn_cache_append(k, v, k_pages, v_pages, params):
     _check_layout(k, params.layouts["k"], "k")
     _check_layout(v, params.layouts["v"], "v")
     _check_pages(k_pages, v_pages, params)
-    _check(lib().distr_attn_cache_append(_ptr(k), _ptr(v), _ptr(k_pages), _ptr(v_pages), ctypes.byref(params)))
+    _check(lib().distr_attn_cache_append(_at(k), _at(v), _at(k_pages), _at(v_pages), ctypes.byref(params)))
     return k_pages, v_pages
 
 
@@ -566,7 +570,7 @@ def distr_attn_paged_fwd(q, k_pages, v_pages, o, params):
     if o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or not o.is_contiguous():
         raise ValueError("o must be contiguous, of q's shape and dtype, on its device")
     _check_pages(k_pages, v_pages, params)
-    _check(lib().distr_attn_paged_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(o), ctypes.byref(params)))
+    _check(lib().distr_attn_paged_fwd(_at(q), _at(k_pages), _at(v_pages), _at(o), ctypes.byref(params)))
     return o
 
 

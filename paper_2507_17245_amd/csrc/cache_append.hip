@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 
-template <typename E, int D, int ROPE>
+template <typename E, int D, int ROPE, bool ONCE>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(
     const E* __restrict__ k, const E* __restrict__ v, E* __restrict__ k_pages, E* __restrict__ v_pages, const int* __restrict__ page_table,
     const int* __restrict__ kv_len, const int* __restrict__ q_start, const int* __restrict__ positions, const void* __restrict__ weight,
@@ -26,10 +26,10 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(
   Eight<E> kl, kh, vl, vh;
   const E* kp = k + token * k_token + head * k_head;
   const E* vp = v + token * v_token + head * v_head;
-  kl.load(kp + at.lo);
-  kh.load(kp + at.hi);
-  vl.load(vp + at.lo);
-  vh.load(vp + at.hi);
+  kl.template load<ONCE>(kp + at.lo);
+  kh.template load<ONCE>(kp + at.hi);
+  vl.template load<ONCE>(vp + at.lo);
+  vh.template load<ONCE>(vp + at.hi);
 
   // sequences that begin at or before the wave's first token
   const int first = __builtin_amdgcn_readfirstlane(token), lane = threadIdx.x & 63;
@@ -68,10 +68,10 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(
     rotate<ROPE, 1>(x, angles);
   }
   const int64_t to = page * page_stride + head * head_stride + place % page_size * row_stride;
-  Eight<E>::store(k_pages + to + at.lo, x);
-  Eight<E>::store(k_pages + to + at.hi, x + 8);
-  *(Eight<E>*)(v_pages + to + at.lo) = vl;
-  *(Eight<E>*)(v_pages + to + at.hi) = vh;
+  Eight<E>::template store<ONCE>(k_pages + to + at.lo, x);
+  Eight<E>::template store<ONCE>(k_pages + to + at.hi, x + 8);
+  vl.template put<ONCE>(v_pages + to + at.lo);
+  vh.template put<ONCE>(v_pages + to + at.hi);
 }
 
 template <typename E, int D, int ROPE>
@@ -79,7 +79,9 @@ void append(const void* k, const void* v, void* k_pages, void* v_pages, const da
   const Rotary r = {p.rotary.norm, p.rotary.eps, p.rotary.weight_dtype, p.rotary.weight_heads, p.rotary.rope,
                     p.rotary.rope ? p.rotary.rot_dim : 0, p.rotary.n_pos, p.rotary.cos_table, p.rotary.sin_table};
   const long long lanes = (long long)p.n_tokens * p.Hkv * (D / 16);
-  hipLaunchKernelGGL((cache_append_kernel<E, D, ROPE>), dim3((unsigned)((lanes + kAppendThreads - 1) / kAppendThreads)), dim3(kAppendThreads),
+  constexpr bool kCan = sizeof(E) == 2;
+  const bool once = kCan && lanes * 16 * 2 * 4 > kPastCaches;
+  hipLaunchKernelGGL((once ? cache_append_kernel<E, D, ROPE, kCan> : cache_append_kernel<E, D, ROPE, false>), dim3((unsigned)((lanes + kAppendThreads - 1) / kAppendThreads)), dim3(kAppendThreads),
                      0, stream, (const E*)k, (const E*)v, (E*)k_pages, (E*)v_pages, p.page_table, p.kv_len, p.q_start, p.positions,
                      p.rotary.k_weight, r, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, p.page_stride, p.head_stride,
                      p.row_stride, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);

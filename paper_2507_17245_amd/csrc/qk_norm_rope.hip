@@ -32,7 +32,7 @@ struct QkArgs {
   const int* positions;
 };
 
-template <typename E, int D, int ROPE, int HC>
+template <typename E, int D, int ROPE, int HC, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void qk_forward_kernel(const QkArgs a, int chunks) {
   constexpr int LPR = D / 16;
   const int chunk = blockIdx.x % chunks;
@@ -49,8 +49,8 @@ __global__ __launch_bounds__(kRowThreads) void qk_forward_kernel(const QkArgs a,
 #pragma unroll
   for (int i = 0; i < HC; ++i) {
     const E* p = x + min(h0 + i, t.heads - 1) * t.x_stride[1];
-    lo[i].load(p + at.lo);
-    hi[i].load(p + at.hi);
+    lo[i].template load<ONCE>(p + at.lo);
+    hi[i].template load<ONCE>(p + at.hi);
   }
   Angles angles;
   angles.load(a.r, a.positions ? a.positions[row_ld] : n, at.pair, at.turn);
@@ -71,14 +71,14 @@ __global__ __launch_bounds__(kRowThreads) void qk_forward_kernel(const QkArgs a,
     if (at.turn) rotate<ROPE, 1>(v, angles);
     if (row < a.rows) {
       E* p = y + (h0 + i) * t.y_stride[1];
-      Eight<E>::store(p + at.lo, v);
-      Eight<E>::store(p + at.hi, v + 8);
+      Eight<E>::template store<ONCE>(p + at.lo, v);
+      Eight<E>::template store<ONCE>(p + at.hi, v + 8);
     }
   }
 }
 
 // part: [chunks][gridDim.x / chunks][D] sums of a workgroup's rows, null where no weight gradient is asked for
-template <typename E, int D, int ROPE, int HC>
+template <typename E, int D, int ROPE, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void qk_backward_kernel(const QkArgs a, int chunks, float* part) {
   constexpr int LPR = D / 16, ROWS = kRowThreads / LPR;
   const int chunk = blockIdx.x % chunks, group = blockIdx.x / chunks, groups = gridDim.x / chunks;
@@ -98,47 +98,39 @@ __global__ __launch_bounds__(kRowThreads) void qk_backward_kernel(const QkArgs a
     E* y = (E*)t.y + b * t.y_stride[0] + n * t.y_stride[2];
     Angles angles;
     angles.load(a.r, a.positions ? a.positions[row_ld] : n, at.pair, at.turn);
-    for (int h = h0; h < h1; h += HC) {
-      Eight<E> xl[HC], xh[HC], gl[HC], gh[HC];
-#pragma unroll
-      for (int i = 0; i < HC; ++i) {
-        const int64_t hd = min(h + i, h1 - 1);
-        gl[i].load(g + hd * t.g_stride[1] + at.lo);
-        gh[i].load(g + hd * t.g_stride[1] + at.hi);
-        if (a.r.norm) {
-          xl[i].load(x + hd * t.x_stride[1] + at.lo);
-          xh[i].load(x + hd * t.x_stride[1] + at.hi);
-        }
+    for (int64_t h = h0; h < h1; ++h) {
+      Eight<E> xl, xh, gl, gh;
+      gl.template load<ONCE>(g + h * t.g_stride[1] + at.lo);
+      gh.template load<ONCE>(g + h * t.g_stride[1] + at.hi);
+      if (a.r.norm) {
+        xl.template load<ONCE>(x + h * t.x_stride[1] + at.lo);
+        xh.template load<ONCE>(x + h * t.x_stride[1] + at.hi);
       }
+      float u[16];
+      gl.values(u);
+      gh.values(u + 8);
+      if (at.turn) rotate<ROPE, -1>(u, angles);
+      if (a.r.norm) {
+        float v[16];
+        xl.values(v);
+        xh.values(v + 8);
+        const float r = inverse_rms<LPR>(v, a.r.eps);
+        float s = 0.0f;
 #pragma unroll
-      for (int i = 0; i < HC; ++i) {
-        if (h + i >= h1) break;
-        float u[16];
-        gl[i].values(u);
-        gh[i].values(u + 8);
-        if (at.turn) rotate<ROPE, -1>(u, angles);
-        if (a.r.norm) {
-          float v[16];
-          xl[i].values(v);
-          xh[i].values(v + 8);
-          const float r = inverse_rms<LPR>(v, a.r.eps);
-          float s = 0.0f;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            v[j] *= r;
-            if (row < a.rows) dw[j] = __builtin_fmaf(u[j], v[j], dw[j]);
-            u[j] *= w[j];
-            s = __builtin_fmaf(u[j], v[j], s);
-          }
-          s = row_sum<LPR>(s) * (1.0f / D);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) u[j] = r * __builtin_fmaf(-s, v[j], u[j]);
+        for (int j = 0; j < 16; ++j) {
+          v[j] *= r;
+          if (row < a.rows) dw[j] = __builtin_fmaf(u[j], v[j], dw[j]);
+          u[j] *= w[j];
+          s = __builtin_fmaf(u[j], v[j], s);
         }
-        if (row < a.rows) {
-          E* p = y + (h + i) * t.y_stride[1];
-          Eight<E>::store(p + at.lo, u);
-          Eight<E>::store(p + at.hi, u + 8);
-        }
+        s = row_sum<LPR>(s) * (1.0f / D);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) u[j] = r * __builtin_fmaf(-s, v[j], u[j]);
+      }
+      if (row < a.rows) {
+        E* p = y + h * t.y_stride[1];
+        Eight<E>::template store<ONCE>(p + at.lo, u);
+        Eight<E>::template store<ONCE>(p + at.hi, u + 8);
       }
     }
   }
@@ -212,18 +204,24 @@ QkArgs arguments(const QkProblem& p, int chunk, bool backward) {
   return a;
 }
 int all_chunks(const QkProblem& p, int chunk) { return (p.heads[0] + chunk - 1) / chunk + (p.heads[1] + chunk - 1) / chunk; }
+// bytes of `tensors` that the call reads or writes
+bool past_caches(const QkProblem& p, int tensors) {
+  return p.dtype == 0 && (long long)tensors * p.B * p.N * (p.heads[0] + p.heads[1]) * p.d * 2 > kPastCaches;
+}
 int row_groups(const QkProblem& p) { return (p.B * p.N + kRowThreads * 16 / p.d - 1) / (kRowThreads * 16 / p.d); }
 
 template <typename E, int D, int ROPE>
 void forward(const QkProblem& p, hipStream_t stream) {
   const int groups = row_groups(p);
   // Four heads to a workgroup where that still leaves four workgroups to a compute unit.
-  const bool four = (long long)groups * all_chunks(p, 4) >= 4 * kComputeUnits;
+  const bool four = past_caches(p, 2) || (long long)groups * all_chunks(p, 4) >= 4 * kComputeUnits;
   const int chunk = four ? 4 : 1, chunks = all_chunks(p, chunk);
   const dim3 grid((unsigned)(groups * chunks)), block(kRowThreads);
   const QkArgs a = arguments(p, chunk, false);
-  if (four) hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 4>), grid, block, 0, stream, a, chunks);
-  else hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 1>), grid, block, 0, stream, a, chunks);
+  constexpr bool kCan = sizeof(E) == 2;
+  if (kCan && past_caches(p, 2)) hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 4, kCan>), grid, block, 0, stream, a, chunks);   // (four heads, by its size)
+  else if (four) hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 4, false>), grid, block, 0, stream, a, chunks);
+  else hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 1, false>), grid, block, 0, stream, a, chunks);
 }
 
 // Backward: heads of a workgroup and workgroups along the rows.
@@ -234,7 +232,7 @@ BackwardSplit backward_split(const QkProblem& p) {
   BackwardSplit s;
   s.chunk = p.rotary.norm && p.rotary.weight_heads ? 1 : 4;
   s.chunks = all_chunks(p, s.chunk);
-  const int most = (8 * kComputeUnits + s.chunks - 1) / s.chunks;   // (what is resident at a time: rows beyond are walked)
+  const int most = (4 * kComputeUnits + s.chunks - 1) / s.chunks;   // (what is resident at a time: rows beyond are walked)
   s.groups = std::max(1, std::min(row_groups(p), most));
   return s;
 }
@@ -242,8 +240,10 @@ BackwardSplit backward_split(const QkProblem& p) {
 template <typename E, int D, int ROPE>
 void backward(const QkProblem& p, float* part, hipStream_t stream) {
   const BackwardSplit s = backward_split(p);
-  hipLaunchKernelGGL((qk_backward_kernel<E, D, ROPE, 2>), dim3((unsigned)(s.groups * s.chunks)), dim3(kRowThreads), 0, stream,
-                     arguments(p, s.chunk, true), s.chunks, part);
+  constexpr bool kCan = sizeof(E) == 2;
+  const bool once = kCan && past_caches(p, p.rotary.norm ? 3 : 2);
+  hipLaunchKernelGGL((once ? qk_backward_kernel<E, D, ROPE, kCan> : qk_backward_kernel<E, D, ROPE, false>), dim3((unsigned)(s.groups * s.chunks)),
+                     dim3(kRowThreads), 0, stream, arguments(p, s.chunk, true), s.chunks, part);
 }
 
 #define DA_QK_DISPATCH(CALL)                                                        \

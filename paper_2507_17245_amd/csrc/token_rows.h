@@ -22,12 +22,31 @@ struct Rotary {
   const float* sin_table;
 };
 
+// Calls that read and write more than 128 MB leave the caches (256 MB) alone: what they hold would be gone before it is read again. us, in the
+// caches | past them: rows of B4 H16 Hkv16 N8192 d128, forward and gradient (537 and 805 MB) 278 | 252, appends of 149 MB 33.5 | 27.8; but
+// appends of 71 MB 14.1 | 15.5, rows of 43 MB 11.5 | 16.0, forward and gradient of 43 and 64 MB 30 | 40, of 84 and 126 MB 52 | 57. Not
+// floats, whose eight channels are two accesses that share a line (forward and gradient of 270 and 405 MB 151 | 161).
+constexpr long long kPastCaches = 128LL << 20;
+template <bool ONCE, typename V>
+__device__ inline V read16(const V* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool ONCE, typename V>
+__device__ inline void write16(V* p, V x) {
+  if constexpr (ONCE) __builtin_nontemporal_store(x, p);
+  else *p = x;
+}
+
 template <typename E>
 struct Eight;   // eight consecutive channels, as loaded
 template <>
 struct Eight<bf16> {
   u32x4 raw;
-  __device__ void load(const bf16* p) { raw = *(const u32x4*)p; }
+  template <bool ONCE = false>
+  __device__ void load(const bf16* p) { raw = read16<ONCE>((const u32x4*)p); }
+  template <bool ONCE>
+  __device__ void put(bf16* p) const { write16<ONCE>((u32x4*)p, raw); }
   __device__ void values(float* x) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -35,24 +54,32 @@ struct Eight<bf16> {
       x[2 * j + 1] = __builtin_bit_cast(float, raw[j] & 0xffff0000u);
     }
   }
+  template <bool ONCE>
   static __device__ void store(bf16* p, const float* x) {
     bf16x8 y;
 #pragma unroll
     for (int j = 0; j < 8; ++j) y[j] = (bf16)x[j];
-    *(bf16x8*)p = y;
+    write16<ONCE>((bf16x8*)p, y);
   }
 };
 template <>
 struct Eight<float> {
   f32x4 raw[2];
+  template <bool ONCE = false>
   __device__ void load(const float* p) {
     raw[0] = *(const f32x4*)p;
     raw[1] = *(const f32x4*)(p + 4);
+  }
+  template <bool ONCE>
+  __device__ void put(float* p) const {
+    *(f32x4*)p = raw[0];
+    *(f32x4*)(p + 4) = raw[1];
   }
   __device__ void values(float* x) const {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = raw[j >> 2][j & 3];
   }
+  template <bool ONCE>
   static __device__ void store(float* p, const float* x) {
     *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
     *(f32x4*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
