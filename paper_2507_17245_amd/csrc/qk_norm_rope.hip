@@ -204,23 +204,24 @@ QkArgs arguments(const QkProblem& p, int chunk, bool backward) {
   return a;
 }
 int all_chunks(const QkProblem& p, int chunk) { return (p.heads[0] + chunk - 1) / chunk + (p.heads[1] + chunk - 1) / chunk; }
-// bytes of `tensors` that the call reads or writes
+// whether the call reads and writes, `tensors` of them in all, more than the caches are asked to hold
 bool past_caches(const QkProblem& p, int tensors) {
-  return p.dtype == 0 && (long long)tensors * p.B * p.N * (p.heads[0] + p.heads[1]) * p.d * 2 > kPastCaches;
+  return (long long)tensors * p.B * p.N * (p.heads[0] + p.heads[1]) * p.d * (p.dtype == 0 ? 2 : 4) > kPastCaches;
 }
 int row_groups(const QkProblem& p) { return (p.B * p.N + kRowThreads * 16 / p.d - 1) / (kRowThreads * 16 / p.d); }
 
 template <typename E, int D, int ROPE>
 void forward(const QkProblem& p, hipStream_t stream) {
   const int groups = row_groups(p);
-  // Four heads to a workgroup where that still leaves four workgroups to a compute unit.
-  const bool four = past_caches(p, 2) || (long long)groups * all_chunks(p, 4) >= 4 * kComputeUnits;
-  const int chunk = four ? 4 : 1, chunks = all_chunks(p, chunk);
+  // Two heads to a workgroup, which share its angles, where that still leaves two workgroups to a compute unit (one | two | four heads, us: H32 Hkv8
+  // N4096 d64 11.5 | 11.3 | 12.1, H8 Hkv8 N4096 d128 10.4 | 11.1 | 10.9, with its gradient H32 Hkv8 N4096 d128 51.4 | 49.8 | 51.4).
+  const bool two = (long long)groups * all_chunks(p, 2) >= 2 * kComputeUnits;
+  const int chunk = two ? 2 : 1, chunks = all_chunks(p, chunk);
   const dim3 grid((unsigned)(groups * chunks)), block(kRowThreads);
   const QkArgs a = arguments(p, chunk, false);
   constexpr bool kCan = sizeof(E) == 2;
-  if (kCan && past_caches(p, 2)) hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 4, kCan>), grid, block, 0, stream, a, chunks);   // (four heads, by its size)
-  else if (four) hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 4, false>), grid, block, 0, stream, a, chunks);
+  if (kCan && two && past_caches(p, 2)) hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 2, kCan>), grid, block, 0, stream, a, chunks);
+  else if (two) hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 2, false>), grid, block, 0, stream, a, chunks);
   else hipLaunchKernelGGL((qk_forward_kernel<E, D, ROPE, 1, false>), grid, block, 0, stream, a, chunks);
 }
 
@@ -232,7 +233,9 @@ BackwardSplit backward_split(const QkProblem& p) {
   BackwardSplit s;
   s.chunk = p.rotary.norm && p.rotary.weight_heads ? 1 : 4;
   s.chunks = all_chunks(p, s.chunk);
-  const int most = (4 * kComputeUnits + s.chunks - 1) / s.chunks;   // (what is resident at a time: rows beyond are walked)
+  // Workgroups that walk the rows: four to a compute unit, two for tensors that come from memory (B4 H16 Hkv16 N8192 d128 252 | 247 us; but H32 Hkv8
+  // N4096 d64 29.5 | 32.3): fewer sums to add up.
+  const int most = ((past_caches(p, 3) ? 2 : 4) * kComputeUnits + s.chunks - 1) / s.chunks;
   s.groups = std::max(1, std::min(row_groups(p), most));
   return s;
 }
