@@ -577,7 +577,7 @@ int check_paged(const da_paged* p) {
     return fail(DA_ERR_INVALID_ARG, "page_table, kv_len, q_start must be 4-byte aligned");
   const int keys = 32, rows = 32;   // the smallest tile and unit of the kernels
   const double units = (double)p->n_tokens * (p->H / p->Hkv) / rows + p->n_seq;
-  if (units * ((double)p->max_pages * p->page_size / keys + 1) > 4e9 || units * p->Hkv * 16 > 4e9 || (double)p->n_tokens * p->H > 2e9)
+  if (units * ((double)p->max_pages * p->page_size / keys + 1) * p->Hkv > 2e9 || units * p->Hkv * 16 > 4e9 || (double)p->n_tokens * p->H > 2e9)
     return fail(DA_ERR_UNSUPPORTED, "too many rows and keys for one call");
   return DA_OK;
 }

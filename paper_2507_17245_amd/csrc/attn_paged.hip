@@ -97,25 +97,24 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
   auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
 
   const PagedLine<kUnitRows, BC> line(batch);
-  long long pos = 0, end = 1, per_head = 1, length = 1;
+  unsigned pos = 0, end = 1;
   int wg = blockIdx.x;
   if (ranges) {
     // Ranges that follow each other on one XCD: their units read the same keys.
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
-    per_head = line.total;
-    length = paged_range(per_head * Hkv, gridDim.x, least);
-    pos = paged_cut(line, wg, length, per_head * Hkv, per_head);
-    end = paged_cut(line, wg + 1LL, length, per_head * Hkv, per_head);
+    const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
+    pos = paged_cut(line, wg, length, total);
+    end = paged_cut(line, wg + 1, length, total);
   }
   while (pos < end) {
     PagedUnit u;
     int head, t0, t1;
     if (ranges) {
-      head = (int)(pos / per_head);
-      const unsigned at = (unsigned)(pos - head * per_head);
+      head = (int)(pos / line.total);
+      const unsigned at = pos - (unsigned)head * line.total;
       if (!line.template find<false>(at, &u)) return;
       t0 = (int)(at - u.first);
-      t1 = (int)min((long long)u.tiles, t0 + (end - pos));
+      t1 = min(u.tiles, t0 + (int)(end - pos));
     } else {
       // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
       head = wg % Hkv;
@@ -125,7 +124,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
       t1 = u.tiles;
     }
     const bool whole = t0 == 0 && t1 == u.tiles;
-    pos += t1 - t0;
+    pos += (unsigned)(t1 - t0);
 
     const int n_keys = min(u.len, batch.max_keys);
     const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (min(u.m0 + kUnitRows, u.rows) - 1) / group + 1, 0)) : n_keys;   // no row sees more

@@ -1,10 +1,11 @@
 // Attention of new tokens over a paged cache, float tensors in float arithmetic: the reference-precision form of attn_paged.hip.
 //
-// The same units of 32 rows and ranges of tiles (paged_units.h), four waves that deal 32-key tiles out among themselves. Products by
+// Units of 32 rows and ranges of tiles (paged_units.h); four waves deal 32-key tiles out among themselves. Products by
 // v_mfma_f32_32x32x2_f32, S^T = K Q^T and O^T = V^T P^T, with the contraction dealt out so that a lane's operands are what it can
-// load itself: channel s and s + d / 2 in step s of the first (a lane walks half a row of K), keys acc_row(i, 0 / 1) in step i of the second
-// (where P already is; a lane takes one channel of V rows). Operands come from memory, without LDS: what bounds it are these loads
-// and the float products (1/16 of the bf16 rate).
+// load itself in 16 bytes (V at d = 64: 8): channels s and s + d / 2 in step s of the first (a lane walks half a row of K), keys
+// acc_row(i, 0 / 1) in step i of the second, where P already is, with channels r * d / 32 + mb as row r of block mb (a lane takes consecutive
+// ones of a row of V). Bound: the float products, 1/16 of the bf16 rate; V of a tile is asked for before its scores are taken and K of
+// the next one behind them. Operands do not pass through LDS.
 #include <cfloat>
 
 #include "f32_tiles.h"
@@ -18,7 +19,7 @@ namespace {
 constexpr int kWaves = 4, kThreads = kWaves * 64, kRows = 32;
 
 template <int D>
-__global__ __launch_bounds__(kThreads) void paged_f32_kernel(
+__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_pages, const float* __restrict__ v_pages, float* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int64_t row_bytes, int64_t q_token,
@@ -32,22 +33,21 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
   const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
 
   const PagedLine<kRows, kTile> line(batch);
-  long long pos = 0, end = 1, per_head = 1, length = 1;
+  unsigned pos = 0, end = 1;
   if (ranges) {
-    per_head = line.total;
-    length = paged_range(per_head * Hkv, gridDim.x, least);
-    pos = paged_cut(line, blockIdx.x, length, per_head * Hkv, per_head);
-    end = paged_cut(line, blockIdx.x + 1LL, length, per_head * Hkv, per_head);
+    const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
+    pos = paged_cut(line, blockIdx.x, length, total);
+    end = paged_cut(line, blockIdx.x + 1, length, total);
   }
   while (pos < end) {
     PagedUnit u;
     int head, t0, t1;
     if (ranges) {
-      head = (int)(pos / per_head);
-      const unsigned at = (unsigned)(pos - head * per_head);
+      head = (int)(pos / line.total);
+      const unsigned at = pos - (unsigned)head * line.total;
       if (!line.template find<false>(at, &u)) return;
       t0 = (int)(at - u.first);
-      t1 = (int)min((long long)u.tiles, t0 + (end - pos));
+      t1 = min(u.tiles, t0 + (int)(end - pos));
     } else {
       head = blockIdx.x % Hkv;
       if (!line.template find<true>(blockIdx.x / Hkv, &u)) return;
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
       t1 = u.tiles;
     }
     const bool whole = t0 == 0 && t1 == u.tiles;
-    pos += t1 - t0;
+    pos += (unsigned)(t1 - t0);
 
     const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);
     const int token = u.q0 + m_ld / group;
@@ -80,20 +80,53 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
 #pragma unroll
     for (int mb = 0; mb < NMB; ++mb) zero(oacc[mb]);
     float ref = -FLT_MAX, l_run = 0.0f;
-    PageWindow window = page_window(table, (t0 + wave) * kTile + lq, n_seen, page_size, n_pages, page_bytes, row_bytes);
-    for (int t = t0 + wave; t < t_end; t += kWaves) {
-      const PageWindow mine = window;   // of key t * 32 + lq
-      const uint64_t off = mine.lo | (uint64_t)mine.hi << 32;
-      window = page_window(table, (t + kWaves) * kTile + lq, n_seen, page_size, n_pages, page_bytes, row_bytes);
-      const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(mine.there != 0);
-      ChannelSum<HALF> chain;
+    // Lane lq of either half: where key tile * 32 + lq lies. K is loaded from there (of an absent key, the cache's first row), V by the two
+    // groups of 16 keys, which lie in a page each: rows that are absent come as zeros.
+    auto window_of = [&](int t) { return page_window(table, t * kTile + lq, n_seen, page_size, n_pages, page_bytes, row_bytes); };
+    float kv[HALF];
+    auto load_k = [&](const PageWindow& w) {
+      const char* at = k_base + (w.lo | (uint64_t)w.hi << 32) + hh * HALF * 4;
 #pragma unroll
       for (int s = 0; s < HALF; s += 4) {
-        const f32x4 x = *(const f32x4*)(k_base + off + (hh * HALF + s) * 4);   // (of an absent key the cache's first)
+        const f32x4 x = *(const f32x4*)(at + s * 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) chain.step(s + j, mine.there ? x[j] : 0.0f, qv[s + j]);
+        for (int j = 0; j < 4; ++j) kv[s + j] = w.there ? x[j] : 0.0f;
       }
+    };
+    int t = t0 + wave;
+    PageWindow now = window_of(t), next = window_of(t + kWaves);
+    if (t < t_end) load_k(now);
+    for (; t < t_end; t += kWaves) {
+      const uint32_t there = (uint32_t)__builtin_amdgcn_ballot_w64(now.there != 0);
+      float vv[16][NMB];   // V[key acc_row(i, hh)][channel lq * NMB + mb]
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const uint64_t off = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, 16 * g) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)now.hi, 16 * g) << 32;
+        const int rows = min(n_seen - (t * kTile + 16 * g), 16);
+        const unsigned bytes = there >> (16 * g) & 1 ? (unsigned)((rows - 1) * (int)row_bytes + D * 4) : 0u;
+        const __amdgpu_buffer_rsrc_t rsrc = head_rsrc(v_base + off, bytes);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int at = 4 * hh * (int)row_bytes + lq * NMB * 4, more = (8 * (j >> 2) + (j & 3)) * (int)row_bytes;
+          if constexpr (NMB == 4) {
+            const f32x4 x = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, more, 0));
+#pragma unroll
+            for (int mb = 0; mb < 4; ++mb) vv[8 * g + j][mb] = x[mb];
+          } else {
+            const f32x2 x = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, more, 0));
+            vv[8 * g + j][0] = x[0];
+            vv[8 * g + j][1] = x[1];
+          }
+        }
+      }
+      ChannelSum<HALF> chain;
+#pragma unroll
+      for (int s = 0; s < HALF; ++s) chain.step(s, kv[s], qv[s]);
       f32x16 sc = chain.sum();
+      now = next;
+      next = window_of(t + 2 * kWaves);
+      if (t + kWaves < t_end) load_k(now);
+      const bool some = t * kTile + kTile > all_see;
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (t * kTile + acc_row(i, hh) > lim || !(there >> acc_row(i, hh) & 1)) sc[i] = -INFINITY;
@@ -115,43 +148,40 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
         sc[i] = __builtin_amdgcn_exp2f((sc[i] - ref) * scale_log2e);
         l_run += sc[i];
       }
-      auto v_rows = [&](auto take) {   // take(i, mb, value of key acc_row(i, hh), channel 32 mb + lq)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int from = acc_row(i, hh) << 2;
-          const uint64_t row = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)mine.lo) | (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)mine.hi) << 32;
-          const bool is = there >> acc_row(i, hh) & 1;
-#pragma unroll
-          for (int mb = 0; mb < NMB; ++mb) {
-            const float x = *(const float*)(v_base + row + (32 * mb + lq) * 4);
-            take(i, mb, is ? x : 0.0f);
-          }
-        }
-      };
       bool odd = false;
-      if (t * kTile + kTile > all_see) v_rows([&](int, int, float x) { odd |= !(__builtin_fabsf(x) < INFINITY); });
+      if (some) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb) odd |= !(__builtin_fabsf(vv[i][mb]) < INFINITY);
+      }
       if (__builtin_amdgcn_ballot_w64(odd) == 0) {
-        v_rows([&](int i, int mb, float x) { oacc[mb] = mfma(x, sc[i], oacc[mb]); });
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+          for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma(vv[i][mb], sc[i], oacc[mb]);
         continue;
       }
       // An infinity or a NaN among values that not every row sees: it must not reach the rows with P = 0 (0 times it). The finite
       // values, then the weight with which a row sees either infinity or a NaN.
 #pragma unroll 1
       for (int kind = 0; kind < 4; ++kind) {
-        f32x16 z[NMB];
-#pragma unroll
-        for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) z[mb][i] = kind == 0 ? oacc[mb][i] : 0.0f;
-        v_rows([&](int i, int mb, float x) {
-          const int is = __builtin_fabsf(x) < INFINITY ? 0 : x != x ? 3 : x < 0.0f ? 2 : 1;
-          z[mb] = mfma(is != kind ? 0.0f : kind == 0 ? x : 1.0f, sc[i], z[mb]);
-        });
         const float what = kind == 1 ? INFINITY : kind == 2 ? -INFINITY : __builtin_nanf("");
 #pragma unroll
-        for (int mb = 0; mb < NMB; ++mb)
+        for (int mb = 0; mb < NMB; ++mb) {
+          f32x16 z;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) oacc[mb][i] = kind == 0 ? z[mb][i] : oacc[mb][i] + (z[mb][i] > 0.0f ? what : 0.0f);
+          for (int i = 0; i < 16; ++i) z[i] = kind == 0 ? oacc[mb][i] : 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float x = vv[i][mb];
+            const int is = __builtin_fabsf(x) < INFINITY ? 0 : x != x ? 3 : x < 0.0f ? 2 : 1;
+            z = mfma(is != kind ? 0.0f : kind == 0 ? x : 1.0f, sc[i], z);
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (a few operands' registers at a time)
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mb][i] = kind == 0 ? z[i] : oacc[mb][i] + (z[i] > 0.0f ? what : 0.0f);
+        }
       }
     }
 
@@ -165,11 +195,11 @@ __global__ __launch_bounds__(kThreads) void paged_f32_kernel(
     for (int j = 0; j < kWaves; ++j) l_all += stat_lds[j][lq][1] * __builtin_amdgcn_exp2f((stat_lds[j][lq][0] - ref_all) * scale_log2e);
     const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
 #pragma unroll
-    for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4)
-        *(f32x4*)&sums[wave][lq][32 * mb + 8 * i4 + 4 * hh] =
-            f32x4{oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
+    for (int i = 0; i < 16; ++i) {   // channels acc_row(i, hh) * NMB ..
+      float* to = &sums[wave][lq][acc_row(i, hh) * NMB];
+      if constexpr (NMB == 4) *(f32x4*)to = f32x4{oacc[0][i] * weight, oacc[1][i] * weight, oacc[2][i] * weight, oacc[3][i] * weight};
+      else *(f32x2*)to = f32x2{oacc[0][i] * weight, oacc[1][i] * weight};
+    }
     __syncthreads();
     const size_t slot = 2 * (size_t)blockIdx.x + (t0 == 0 ? 2 : 1);   // (the part in front of the next one's cut)
     for (int i = tid; i < kRows * (D / 4); i += kThreads) {
@@ -209,11 +239,14 @@ hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, voi
 
 }  // namespace
 
-size_t paged_f32_scratch_bytes(const da_paged& p) { return paged_launch_bytes(2 * kComputeUnits, kRows, p.d); }
+// Workgroups at a time (registers).
+static int resident(const da_paged& p) { return (p.d == 64 ? 2 : 1) * kComputeUnits; }
+
+size_t paged_f32_scratch_bytes(const da_paged& p) { return paged_launch_bytes(resident(p), kRows, p.d); }
 
 hipError_t launch_paged_f32(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                             size_t scratch_bytes, hipStream_t stream) {
-  const PagedLaunch l = paged_launch(p, kRows, kTile, 2 * kComputeUnits, scratch_bytes);
+  const PagedLaunch l = paged_launch(p, kRows, kTile, resident(p), scratch_bytes);
   return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
                    : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
 }

@@ -126,21 +126,22 @@ struct PagedLine {
   }
 };
 
+// (All kv heads' tiles stay below 2^31, by the call's checks.)
 // Length of a range: equal ones for `workgroups` of them, none shorter than `least` tiles.
-__device__ inline long long paged_range(long long total, int workgroups, int least) {
-  return max((total + workgroups - 1) / workgroups, (long long)least);
+__device__ inline unsigned paged_range(unsigned total, int workgroups, int least) {
+  return max((total + (unsigned)workgroups - 1) / (unsigned)workgroups, (unsigned)least);
 }
-__device__ inline int paged_snap(long long length) { return (int)min(max(length / 8, 1LL), 6LL); }
+__device__ inline unsigned paged_snap(unsigned length) { return min(max(length / 8, 1u), 6u); }
 // Where range w begins.
 template <typename LINE>
-__device__ inline long long paged_cut(const LINE& line, long long w, long long length, long long total, long long per_head) {
-  const long long at = w * length;
+__device__ inline unsigned paged_cut(const LINE& line, unsigned w, unsigned length, unsigned total) {
+  const unsigned at = w * length;
   if (at >= total) return total;
   PagedUnit u;
-  const long long head = at / per_head;
-  if (!line.template find<false>((unsigned)(at - head * per_head), &u)) return total;
-  const int in = (int)(at - head * per_head - u.first), snap = paged_snap(length);
-  return in < snap ? at - in : u.tiles - in < snap ? at - in + u.tiles : at;
+  const unsigned head = at / line.total;
+  if (!line.template find<false>(at - head * line.total, &u)) return total;
+  const unsigned in = at - head * line.total - u.first, snap = paged_snap(length);
+  return in < snap ? at - in : (unsigned)u.tiles - in < snap ? at - in + (unsigned)u.tiles : at;
 }
 
 // Where the keys of 16 successive places lie: a lane for each such group of a wave's next 64. The group's first row of
@@ -176,16 +177,16 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(
   const int group = H / Hkv;
   __shared__ f32x4 x_lds[256], stat_lds[256];
   const PagedLine<ROWS, KEYS> line(PagedBatch{q_start, kv_len, n_seq, n_tokens, Hkv, group, max_keys, 0});
-  const long long length = paged_range((long long)line.total * Hkv, workgroups, least);
-  const int snap = paged_snap(length);
+  const unsigned length = paged_range(line.total * (unsigned)Hkv, workgroups, least), snap = paged_snap(length);
   const unsigned each = line.units * (unsigned)Hkv;
   for (unsigned item = blockIdx.x; item < each * (ROWS / TAKE); item += gridDim.x) {
     const unsigned piece = item / each, of = item % each;
     const int head = (int)(of % (unsigned)Hkv);
     PagedUnit u;
     if (!line.template find<true>(of / (unsigned)Hkv, &u)) return;
-    const long long first = (long long)head * line.total + u.first;
-    const int w0 = (int)((first + snap + length - 1) / length), w1 = (int)((first + u.tiles - snap) / length);   // its cuts
+    const unsigned first = (unsigned)head * line.total + u.first;
+    if ((unsigned)u.tiles < snap) continue;
+    const int w0 = (int)((first + snap + length - 1) / length), w1 = (int)((first + (unsigned)u.tiles - snap) / length);   // its cuts
     const int rows = min(u.rows - u.m0 - (int)piece * TAKE, TAKE);
     if (w0 > w1 || rows <= 0) continue;
     int side = 1;   // lanes' rows side by side, a power of two
