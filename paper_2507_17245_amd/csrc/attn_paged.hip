@@ -24,7 +24,7 @@ namespace da {
 
 namespace {
 
-constexpr int kUnitRows = 128, kTileKeys = 64, kRW = 4, kHalves = 2, kThreads = kRW * kHalves * 64;
+constexpr int kUnitRows = 128, kTileKeys = 64, kRW = 4;   // rows and keys of the line's units and tiles, waves over the rows
 
 // Nothing is known of x from here on: what is computed of it stays where it is used, instead of in registers that the walk has not got.
 __device__ inline int here(int x) {
@@ -69,8 +69,10 @@ struct Places {
   }
 };
 
-template <int D, bool STATS>
-__global__ __launch_bounds__(kThreads, 2) void paged_kernel(
+// HALVES 2: one workgroup of eight waves a compute unit, for ranges and for units that are fewer than two a compute unit. HALVES 1: two of four, for whole
+// units, one beginning or ending beside the other's walk.
+template <int D, bool STATS, int HALVES>
+__global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
     const bf16* __restrict__ q, const bf16* __restrict__ k_pages, const bf16* __restrict__ v_pages, bf16* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int row_bytes, int64_t q_token,
@@ -80,17 +82,18 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
   constexpr int LPG = 16 * ROWB / 1024;   // direct loads of 16 keys
   constexpr float kSumTrigger = (BC / 2) * 256.0f;   // (as in attn_bf16_impl.h)
   // Two tiles of K and V for each half; or, with few rows, one of 8 KB for each wave.
-  constexpr int FEWB = 8192, FT = FEWB / ROWB, BUFB = 4 * FEWB;
-  static_assert(kHalves * TILEB <= BUFB, "a buffer holds the halves' tiles");
+  constexpr int WAVES = kRW * HALVES, kThreads = WAVES * 64;
+  constexpr int FEWB = 8192, FT = FEWB / ROWB, BUFB = WAVES / 2 * FEWB;
+  static_assert(HALVES * TILEB <= BUFB, "a buffer holds the halves' tiles");
   __shared__ __attribute__((aligned(1024))) char k_lds0[BUFB];
   __shared__ __attribute__((aligned(1024))) char k_lds1[BUFB];
   __shared__ __attribute__((aligned(1024))) char v_lds0[BUFB];
   __shared__ __attribute__((aligned(1024))) char v_lds1[BUFB];
-  __shared__ f32x4 few_stat[kRW * kHalves][32];
+  __shared__ f32x4 few_stat[WAVES][32];
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rw = wave % kRW, half = wave / kRW;
+  const int rw = wave % kRW, half = HALVES == 1 ? 0 : wave / kRW;
   const int group = H / Hkv;
   const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
   auto k_buf = [&](int par) -> char* { return (par ? k_lds1 : k_lds0) + half * TILEB; };
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
   const PagedLine<kUnitRows, BC> line(batch);
   unsigned pos = 0, end = 1;
   int wg = blockIdx.x;
-  if (ranges) {
+  if (HALVES == 2 && ranges) {
     // Ranges that follow each other on one XCD: their units read the same keys.
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
     const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
@@ -109,7 +112,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
   while (pos < end) {
     PagedUnit u;
     int head, t0, t1;
-    if (ranges) {
+    if (HALVES == 2 && ranges) {
       head = (int)(pos / line.total);
       const unsigned at = pos - (unsigned)head * line.total;
       if (!line.template find<false>(at, &u)) return;
@@ -123,7 +126,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
       t0 = 0;
       t1 = u.tiles;
     }
-    const bool whole = t0 == 0 && t1 == u.tiles;
+    const bool whole = HALVES == 1 || (t0 == 0 && t1 == u.tiles);
     pos += (unsigned)(t1 - t0);
 
     const int n_keys = min(u.len, batch.max_keys);
@@ -137,7 +140,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
       // ---- few rows: a wave has all of them, and every eighth tile of 8 KB. Bound: reading the keys and values. ----
       // Each wave has a softmax state of its own and no barrier; K of its next tile is asked for when the scores are
       // taken, V when it is multiplied, so that 128 KB a compute unit are on their way most of the time.
-      constexpr int GROUPS = FT / 16, FMB = FT / 32, FTT = FT / 16, CPT = FEWB / 1024, WINDOW = 64 / GROUPS, WAVES = kRW * kHalves;
+      constexpr int GROUPS = FT / 16, FMB = FT / 32, FTT = FT / 16, CPT = FEWB / 1024, WINDOW = 64 / GROUPS;
       const int lane = here(tid) & 63;
       const Places<D> at_lane(lane, row_bytes);
       const int lq = at_lane.lq, hh = at_lane.hh;
@@ -185,8 +188,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
       };
       const std::true_type of_k;
       const std::false_type of_v;
-      char* kb = (wave < 4 ? k_lds0 : k_lds1) + (wave & 3) * FEWB;
-      char* vb = (wave < 4 ? v_lds0 : v_lds1) + (wave & 3) * FEWB;
+      char* kb = (wave < WAVES / 2 ? k_lds0 : k_lds1) + wave % (WAVES / 2) * FEWB;
+      char* vb = (wave < WAVES / 2 ? v_lds0 : v_lds1) + wave % (WAVES / 2) * FEWB;
 #pragma unroll
       for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
       int there = 0;
@@ -317,8 +320,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
         f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < WAVES; ++j) {
-          const char* of = piece < 16 ? (j < 4 ? k_lds0 : k_lds1) : (j < 4 ? v_lds0 : v_lds1);
-          x += *(const f32x4*)(of + (j & 3) * FEWB + at);
+          const char* of = piece < 16 ? (j < WAVES / 2 ? k_lds0 : k_lds1) : (j < WAVES / 2 ? v_lds0 : v_lds1);
+          x += *(const f32x4*)(of + j % (WAVES / 2) * FEWB + at);
         }
         if (whole) {
           const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
     const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
     const int seen_tiles = (n_seen + BC - 1) / BC;
     // the halves' tiles; a half without any walks one behind the last key: zeros, masked out
-    const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + 1) / 2, 1);
+    const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + HALVES - 1) / HALVES, 1);
     const int n_tiles = half ? max(n_all - n_most, 1) : n_most;
     const int tile0 = half ? (n_all > 1 ? t0 + n_most : seen_tiles) : (n_all > 0 ? t0 : seen_tiles);
     const bool idle = u.m0 + rw * 32 >= u.rows;   // a wave without rows brings its part of the tiles in
@@ -578,48 +581,54 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
       advance(it);
       body(no, no, it, it & 1, s0, s1);
     }
-    if (n_tiles < n_most) __syncthreads();   // (the other half's last tile)
+    if (HALVES == 2 && n_tiles < n_most) __syncthreads();   // (the other half's last tile)
 
     // ---- the halves meet: each hands the other one half of the channels and finishes the rest ----------------
-    constexpr int OB = NMB / 2;
-    const int c0 = half * (D / 2);
+    constexpr int OB = NMB / HALVES;
+    const int c0 = HALVES == 2 ? half * (D / 2) : 0;
     float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
-    static_assert(kRW * OB * 4096 <= kHalves * TILEB && kThreads / 2 * 16 <= kHalves * TILEB, "the exchange fits the tile buffers");
-    f32x4* stat = (f32x4*)k_lds0;
-    f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
-    const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
+    float ref = -nref;
     f32x16 out[OB];
-    if (hh == 0) stat[wave * 32 + lq] = f32x4{-nref, l_tot, e_tot, 0.0f};
+    if constexpr (HALVES == 2) {
+      static_assert(kRW * OB * 4096 <= BUFB && WAVES * 512 <= BUFB, "the exchange fits the tile buffers");
+      f32x4* stat = (f32x4*)k_lds0;
+      f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
+      const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
+      if (hh == 0) stat[wave * 32 + lq] = f32x4{-nref, l_tot, e_tot, 0.0f};
 #pragma unroll
-    for (int mb = 0; mb < OB; ++mb) {
-      f32x16 theirs;
-      if (half) {
-        theirs = oacc[mb];
-        out[mb] = oacc[mb + OB];
-      } else {
-        theirs = oacc[mb + OB];
-        out[mb] = oacc[mb];
+      for (int mb = 0; mb < OB; ++mb) {
+        f32x16 theirs;
+        if (half) {
+          theirs = oacc[mb];
+          out[mb] = oacc[mb + OB];
+        } else {
+          theirs = oacc[mb + OB];
+          out[mb] = oacc[mb];
+        }
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) give[(mb * 4 + i4) * 64] = f32x4{theirs[4 * i4], theirs[4 * i4 + 1], theirs[4 * i4 + 2], theirs[4 * i4 + 3]};
       }
+      __syncthreads();
+      // (a half that saw nothing of a row has sum 0 and no reference; a NaN sum makes the row NaN)
+      const f32x4 st = stat[(wave ^ kRW) * 32 + lq];
+      const float mine_ref = l_tot == 0.0f ? -FLT_MAX : -nref, other_ref = st[1] == 0.0f ? -FLT_MAX : st[0];
+      ref = fmaxf(mine_ref, other_ref);
+      const float wm = __builtin_amdgcn_exp2f(mine_ref - ref), wo = __builtin_amdgcn_exp2f(other_ref - ref);
+      l_tot = __builtin_fmaf(wm, l_tot, wo * st[1]);
+      e_tot = __builtin_fmaf(wm, e_tot, wo * st[2]);
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) give[(mb * 4 + i4) * 64] = f32x4{theirs[4 * i4], theirs[4 * i4 + 1], theirs[4 * i4 + 2], theirs[4 * i4 + 3]};
+      for (int mb = 0; mb < OB; ++mb)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const f32x4 x = take[(mb * 4 + i4) * 64];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]);
+        }
+    } else {
+#pragma unroll
+      for (int mb = 0; mb < OB; ++mb) out[mb] = oacc[mb];
     }
-    __syncthreads();
-    // (a half that saw nothing of a row has sum 0 and no reference; a NaN sum makes the row NaN)
-    const f32x4 st = stat[(wave ^ kRW) * 32 + lq];
-    const float mine_ref = l_tot == 0.0f ? -FLT_MAX : -nref, other_ref = st[1] == 0.0f ? -FLT_MAX : st[0];
-    const float ref = fmaxf(mine_ref, other_ref);
-    const float wm = __builtin_amdgcn_exp2f(mine_ref - ref), wo = __builtin_amdgcn_exp2f(other_ref - ref);
-    l_tot = __builtin_fmaf(wm, l_tot, wo * st[1]);
-    e_tot = __builtin_fmaf(wm, e_tot, wo * st[2]);
     const float inv = !whole ? 1.0f : l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
-#pragma unroll
-    for (int mb = 0; mb < OB; ++mb)
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const f32x4 x = take[(mb * 4 + i4) * 64];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]) * inv;
-      }
     if (m < u.rows) {
       const int64_t row = (int64_t)token * H + q_of;
       const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows + rw * 32 + lq;
@@ -632,7 +641,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
           const int c = c0 + 32 * mb + 8 * i4 + 4 * hh;
-          const f32x4 x = {out[mb][4 * i4], out[mb][4 * i4 + 1], out[mb][4 * i4 + 2], out[mb][4 * i4 + 3]};
+          const f32x4 x = f32x4{out[mb][4 * i4], out[mb][4 * i4 + 1], out[mb][4 * i4 + 2], out[mb][4 * i4 + 3]} * inv;
           if (whole) *(bf16x4*)(o + row * D + c) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
           else *(f32x4*)(part_o + slot * D + c) = x;
         }
@@ -641,13 +650,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_kernel(
   }
 }
 
-template <int D>
-hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
-                    const PagedLaunch& l, hipStream_t stream) {
+template <int D, int HALVES>
+hipError_t launch_halves(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                         const PagedLaunch& l, hipStream_t stream) {
   const float scale_log2e = scale * 1.4426950408889634f;
   float* part_o = (float*)scratch;
   f32x4* part_stat = (f32x4*)((char*)scratch + paged_sum_bytes(l.workgroups, kUnitRows, D));
-  hipLaunchKernelGGL((p.lse_out ? paged_kernel<D, true> : paged_kernel<D, false>), dim3((unsigned)l.workgroups), dim3(kThreads), 0,
+  hipLaunchKernelGGL((p.lse_out ? paged_kernel<D, true, HALVES> : paged_kernel<D, false, HALVES>), dim3((unsigned)l.workgroups), dim3(kRW * HALVES * 64), 0,
                      stream, (const bf16*)q, (const bf16*)k_pages, (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H,
                      p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, p.page_stride * 2, p.head_stride * 2, (int)(p.row_stride * 2),
                      p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
@@ -670,9 +679,13 @@ hipError_t launch_paged(const void* q, const void* k_pages, const void* v_pages,
   if (p.dtype == DA_F32) return launch_paged_f32(q, k_pages, v_pages, o, p, scale, scratch, scratch_bytes, stream);
   PagedLaunch l = paged_launch(p, kUnitRows, kTileKeys, kComputeUnits, scratch_bytes);
   const long long units = (long long)p.n_tokens * (p.H / p.Hkv) / kUnitRows * p.Hkv;   // at least
-  if (units >= 2 * kComputeUnits) l = PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, l.least};
-  return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
-                   : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
+  const bool many = units >= 2 * kComputeUnits;
+  if (many) l = PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, l.least};
+  if (p.d == 64)
+    return many ? launch_halves<64, 1>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
+                : launch_halves<64, 2>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
+  return many ? launch_halves<128, 1>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
+              : launch_halves<128, 2>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
 }
 
 }  // namespace da
