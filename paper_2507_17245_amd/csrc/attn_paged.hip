@@ -130,523 +130,557 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
     pos += (unsigned)(t1 - t0);
 
     const int n_keys = min(u.len, batch.max_keys);
-    const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (min(u.m0 + kUnitRows, u.rows) - 1) / group + 1, 0)) : n_keys;   // no row sees more
-    const int all_see = causal ? min(max(u.len - u.nq + u.m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
     const int* table = page_table + (int64_t)u.seq * max_pages;
     const char* k_base = (const char*)k_pages + head * head_bytes;
     const char* v_base = (const char*)v_pages + head * head_bytes;
-
-    if (u.rows - u.m0 <= 32) {
-      // ---- few rows: a wave has all of them, and every eighth tile of 8 KB. Bound: reading the keys and values. ----
-      // Each wave has a softmax state of its own and no barrier; K of its next tile is asked for when the scores are
-      // taken, V when it is multiplied, so that 128 KB a compute unit are on their way most of the time.
-      constexpr int GROUPS = FT / 16, FMB = FT / 32, FTT = FT / 16, CPT = FEWB / 1024, WINDOW = 64 / GROUPS;
+    // The unit's rows: up to 128 at once, or 32 from m0 on.
+    bool few = u.rows - u.m0 <= 32;
+    for (int m0 = u.m0;;) {
+      const int m1 = min(m0 + (few ? 32 : kUnitRows), u.rows);
+      const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (m1 - 1) / group + 1, 0)) : n_keys;   // no row sees more
+      const int all_see = causal ? min(max(u.len - u.nq + m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
+      if (few) {
+        // ---- few rows: a wave has all of them, and every eighth tile of 8 KB. Bound: reading the keys and values. ----
+        // Each wave has a softmax state of its own and no barrier; K of its next tile is asked for when the scores are
+        // taken, V when it is multiplied, so that 128 KB a compute unit are on their way most of the time.
+        constexpr int GROUPS = FT / 16, FMB = FT / 32, FTT = FT / 16, CPT = FEWB / 1024, WINDOW = 64 / GROUPS;
+        const int lane = here(tid) & 63;
+        const Places<D> at_lane(lane, row_bytes);
+        const int lq = at_lane.lq, hh = at_lane.hh;
+        const int m = m0 + lq, m_ld = min(m, u.rows - 1);
+        const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
+        const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);
+        bf16x8 qop[KSTEPS];
+        const bf16* q_row = q + token * q_token + q_of * q_head;
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
+        int tile = t0 * (BC / FT) + wave;
+        const int t_end = min(t1 * (BC / FT), (n_seen + FT - 1) / FT);
+        // the window's lane for this wave's tile tile + 8 i is that of i * GROUPS, and of the groups of 16 keys behind it
+        auto window_of = [&](int first) {
+          const int t = first + (lane / GROUPS) * WAVES;
+          return page_window(table, t * FT + lane % GROUPS * 16, n_seen, page_size, n_pages, page_bytes, row_bytes);
+        };
+        // Every key is read once. Calls that read more than the caches hold (256 MB) leave them alone: B1 H16 100003 keys d128 171 -> 159 us, 64
+        // sequences of 5 on 4096 159 -> 144; smaller ones may find in them what a program read a step ago (14 sequences of 1100-3900 39, 41 so).
+        const bool once = (long long)line.total * Hkv * (2 * TILEB) > 256LL << 20;
+        // Two windows, the second from the middle of the first on; it takes the first's place when that half is asked for.
+        PageWindow now = window_of(tile), next = window_of(tile + WINDOW / 2 * WAVES);
+        int at = 0;   // place in the window of the tile that is asked for
+        auto ask = [&](auto of_k, const char* from, int t, char* to) -> int {
+          int there = 0;
+#pragma unroll
+          for (int g = 0; g < GROUPS; ++g) {
+            const int l = at * GROUPS + g;
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l);
+            const int is = __builtin_amdgcn_readlane(now.there, l);
+            const int rows = min(n_seen - (t * FT + 16 * g), 16);
+            const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
+            there |= is << g;
+            const char* rows_at = from + (lo | (uint64_t)hi << 32);
+            char* rows_to = to + g * LPG * 1024;
+            if constexpr (decltype(of_k)::value) {
+              if (once) at_lane.template load_k<true>(rows_at, bytes, row_bytes, rows_to);
+              else at_lane.load_k(rows_at, bytes, row_bytes, rows_to);
+            } else {
+              if (once) at_lane.template load_v<true>(rows_at, bytes, row_bytes, rows_to);
+              else at_lane.load_v(rows_at, bytes, row_bytes, rows_to);
+            }
+          }
+          return there;
+        };
+        const std::true_type of_k;
+        const std::false_type of_v;
+        char* kb = (wave < WAVES / 2 ? k_lds0 : k_lds1) + wave % (WAVES / 2) * FEWB;
+        char* vb = (wave < WAVES / 2 ? v_lds0 : v_lds1) + wave % (WAVES / 2) * FEWB;
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
+        int there = 0;
+        if (tile < t_end) {
+          there = ask(of_k, k_base, tile, kb);
+          ask(of_v, v_base, tile, vb);
+        }
+        f32x16 oacc[NMB];
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
+        // The reference is the largest score so far, unscaled (a scaled one is rounded, which shows on large scores).
+        float ref = -FLT_MAX, l_run = 0.0f, e_run = 0.0f;
+        for (; tile < t_end; tile += WAVES) {
+          const int seen = there;
+          asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // K is there
+          const int ka = here(at_lane.ka), va = here(at_lane.va);
+          f32x16 sc[FMB];
+#pragma unroll
+          for (int mb = 0; mb < FMB; ++mb) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[mb][i] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < KSTEPS; ++s) sc[mb] = mfma_32x32x16(at_lane.k_operand(kb, ka, mb, s), qop[s], sc[mb]);
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // and read
+          const bool more = tile + WAVES < t_end;
+          if (more) {
+            ++at;
+            there = ask(of_k, k_base, tile + WAVES, kb);
+          }
+          const int n0 = tile * FT;
+          const bool some = n0 + FT > all_see || seen != (1 << GROUPS) - 1;
+          if (some) {
+#pragma unroll
+            for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (n0 + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(seen >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
+          }
+          float mx = sc[0][0];
+#pragma unroll
+          for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[mb][i]);
+          const float ref_new = fmaxf(ref, half_swap_max(mx));
+          if (__builtin_amdgcn_ballot_w64(ref_new > ref) != 0) {
+            const float alpha = __builtin_amdgcn_exp2f((ref - ref_new) * scale_log2e);
+            l_run *= alpha;
+            if constexpr (STATS) e_run *= alpha;
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+            ref = ref_new;
+          }
+          // P rounded to bf16 as the operands of P.V; the row sum is taken over the rounded values, so that the rounding of a row's
+          // largest weights cancels
+          bf16x8 pop[FTT];
+          const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+#pragma unroll
+          for (int mb = 0; mb < FMB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float x0 = __builtin_amdgcn_exp2f((sc[mb][i] - ref) * scale_log2e), x1 = __builtin_amdgcn_exp2f((sc[mb][i + 1] - ref) * scale_log2e);
+              const bf16x2 pr = {(bf16)x0, (bf16)x1};
+              if constexpr (STATS) e_run += x0 + x1;
+              pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
+              pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
+              l_run = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run, false);
+            }
+          if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // V is there
+          else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
+          bool odd = false;
+          if (some) odd = any_odd<FTT, NMB>(v_operand);
+          if (odd) {
+            odd_values<FTT, NMB>(oacc, pop, v_operand);
+          } else {
+#pragma unroll
+            for (int tt = 0; tt < FTT; ++tt)
+#pragma unroll
+              for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(v_operand(tt, mb), pop[tt], oacc[mb]);
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (more) ask(of_v, v_base, tile + WAVES, vb);
+          if (at == WINDOW / 2) {   // (the next to be asked for is behind it)
+            at = 0;
+            now = next;
+            next = window_of(tile + (1 + WINDOW / 2) * WAVES);
+          }
+          // (the wait behind these products as in attn_bf16_few.hip)
+          __builtin_amdgcn_sched_barrier(0);
+          asm volatile("s_nop 1");
+        }
+        // the waves' states meet
+        const float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
+        if (hh == 0) few_stat[wave][lq] = f32x4{ref, l_tot, e_tot, 0.0f};
+        __syncthreads();
+        float ref_all = few_stat[0][lq][0], l_all = 0.0f, e_all = 0.0f;
+#pragma unroll
+        for (int j = 1; j < WAVES; ++j) ref_all = fmaxf(ref_all, few_stat[j][lq][0]);
+#pragma unroll
+        for (int j = 0; j < WAVES; ++j) {
+          const f32x4 st = few_stat[j][lq];
+          const float x = __builtin_amdgcn_exp2f((st[0] - ref_all) * scale_log2e);
+          l_all += st[1] * x;
+          e_all += st[2] * x;
+        }
+        // (a row that sees nothing has sum 0 and is 0)
+        const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
+        // wave w's sums: 32 rows of D floats in its own buffers (K at d = 64, K and V at d = 128), the 16-byte pieces exchanged by the row
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const int piece = 8 * mb + 2 * i4 + hh;   // channels 4*piece ..
+            float* dst = (float*)(mb < 2 ? kb : vb);
+            const f32x4 x = {oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
+            *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
+          }
+        __syncthreads();
+        const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows + (m0 - u.m0);
+        for (int i = tid; i < (m1 - m0) * (D / 4); i += kThreads) {
+          const int row = i / (D / 4), piece = i % (D / 4), mr = m0 + row;
+          const int at = row * 256 + (((piece & 15) ^ (row & 15)) << 4);
+          f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int j = 0; j < WAVES; ++j) {
+            const char* of = piece < 16 ? (j < WAVES / 2 ? k_lds0 : k_lds1) : (j < WAVES / 2 ? v_lds0 : v_lds1);
+            x += *(const f32x4*)(of + j % (WAVES / 2) * FEWB + at);
+          }
+          if (whole) {
+            const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+            *(bf16x4*)(o + ((int64_t)(u.q0 + mr / group) * H + head * group + mr % group) * D + piece * 4) = y;
+          } else {
+            *(f32x4*)(part_o + (slot + row) * D + piece * 4) = x;
+          }
+        }
+        if (wave == 0 && hh == 0 && m < m1) {
+          if (!whole) part_stat[slot + lq] = f32x4{ref_all * scale_log2e, l_all, e_all, 0.0f};
+          else if (STATS) lse[(int64_t)token * H + q_of] = row_statistic(ref_all * scale_log2e, e_all);
+        }
+        __syncthreads();   // (the next tiles take the place of the sums)
+        m0 += 32;
+        if (m0 >= min(u.m0 + kUnitRows, u.rows)) break;
+        continue;
+      }
       const int lane = here(tid) & 63;
       const Places<D> at_lane(lane, row_bytes);
       const int lq = at_lane.lq, hh = at_lane.hh;
-      const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);
+      const int m = u.m0 + rw * 32 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
       const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
-      const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);
+      const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
+      const int seen_tiles = (n_seen + BC - 1) / BC;
+      // the halves' tiles; a half without any walks one behind the last key: zeros, masked out
+      const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + HALVES - 1) / HALVES, 1);
+      const int n_tiles = half ? max(n_all - n_most, 1) : n_most;
+      const int tile0 = half ? (n_all > 1 ? t0 + n_most : seen_tiles) : (n_all > 0 ? t0 : seen_tiles);
+      const bool idle = u.m0 + rw * 32 >= u.rows;   // a wave without rows brings its part of the tiles in
+
       bf16x8 qop[KSTEPS];
-      const bf16* q_row = q + token * q_token + q_of * q_head;
+      {
+        const bf16* q_row = q + token * q_token + q_of * q_head;
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
-      int tile = t0 * (BC / FT) + wave;
-      const int t_end = min(t1 * (BC / FT), (n_seen + FT - 1) / FT);
-      // the window's lane for this wave's tile tile + 8 i is that of i * GROUPS, and of the groups of 16 keys behind it
-      auto window_of = [&](int first) {
-        const int t = first + (lane / GROUPS) * WAVES;
-        return page_window(table, t * FT + lane % GROUPS * 16, n_seen, page_size, n_pages, page_bytes, row_bytes);
-      };
-      // Every key is read once. Calls that read more than the caches hold (256 MB) leave them alone: B1 H16 100003 keys d128 171 -> 159 us, 64
-      // sequences of 5 on 4096 159 -> 144; smaller ones may find in them what a program read a step ago (14 sequences of 1100-3900 39, 41 so).
-      const bool once = (long long)line.total * Hkv * (2 * TILEB) > 256LL << 20;
-      // Two windows, the second from the middle of the first on; it takes the first's place when that half is asked for.
-      PageWindow now = window_of(tile), next = window_of(tile + WINDOW / 2 * WAVES);
-      int at = 0;   // place in the window of the tile that is asked for
-      auto ask = [&](auto of_k, const char* from, int t, char* to) -> int {
-        int there = 0;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-          const int l = at * GROUPS + g;
-          const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l);
-          const int is = __builtin_amdgcn_readlane(now.there, l);
-          const int rows = min(n_seen - (t * FT + 16 * g), 16);
-          const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
-          there |= is << g;
-          const char* rows_at = from + (lo | (uint64_t)hi << 32);
-          char* rows_to = to + g * LPG * 1024;
-          if constexpr (decltype(of_k)::value) {
-            if (once) at_lane.template load_k<true>(rows_at, bytes, row_bytes, rows_to);
-            else at_lane.load_k(rows_at, bytes, row_bytes, rows_to);
-          } else {
-            if (once) at_lane.template load_v<true>(rows_at, bytes, row_bytes, rows_to);
-            else at_lane.load_v(rows_at, bytes, row_bytes, rows_to);
-          }
-        }
-        return there;
-      };
-      const std::true_type of_k;
-      const std::false_type of_v;
-      char* kb = (wave < WAVES / 2 ? k_lds0 : k_lds1) + wave % (WAVES / 2) * FEWB;
-      char* vb = (wave < WAVES / 2 ? v_lds0 : v_lds1) + wave % (WAVES / 2) * FEWB;
+        for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
+      }
 #pragma unroll
       for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
-      int there = 0;
-      if (tile < t_end) {
-        there = ask(of_k, k_base, tile, kb);
-        ask(of_v, v_base, tile, vb);
-      }
+
+      // Lane i: where the wave's 16 keys of tile (first + i) of the half lie, and which of the tile's groups lie in the cache.
+      struct Window {
+        uint32_t lo, hi;
+        int there;
+      };
+      auto window_of = [&](int first) {
+        Window w = {0, 0, 0};
+        const int key = (tile0 + first + lane) * BC;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const PageWindow p = page_window(table, key + 16 * g, n_seen, page_size, n_pages, page_bytes, row_bytes);
+          w.there |= p.there << g;
+          if (g == rw) {
+            w.lo = p.lo;
+            w.hi = p.hi;
+          }
+        }
+        return w;
+      };
+      // Two windows, the second from the middle of the first on; it takes the first's place when that half is done with.
+      int base;
+      Window now, next;
+      auto advance = [&](int it) {   // tiles before `it` are done with: those up to it + 31 lie in the window from here on
+        if (it < base + 32) return;
+        base += 32;
+        now = next;
+        next = window_of(base + 32);
+      };
+      auto there_of = [&](int it) { return __builtin_amdgcn_readlane(now.there, it - base); };
+      const std::true_type yes;
+      const std::false_type no;
+      // The wave's 16 keys of a tile: where they lie, and how many bytes from there on. A tile's are taken when K is asked for and used for V, too.
+      struct Group {
+        uint32_t lo, hi;
+        unsigned bytes;
+      };
+      auto group_of = [&](int it) {
+        const int l = it - base, is = there_of(it) >> rw & 1, rows = min(n_seen - ((tile0 + it) * BC + 16 * rw), 16);
+        return Group{(uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l),
+                     is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u};
+      };
+      auto load_k = [&](const Group& g, int par) { at_lane.load_k(k_base + (g.lo | (uint64_t)g.hi << 32), g.bytes, row_bytes, k_buf(par) + rw * LPG * 1024); };
+      auto load_v = [&](const Group& g, int par) { at_lane.load_v(v_base + (g.lo | (uint64_t)g.hi << 32), g.bytes, row_bytes, v_buf(par) + rw * LPG * 1024); };
+      Group ahead1, ahead2;   // of tiles it + 1 and it + 2
+      // What tile `it` brings in: K(it + 2) where K(it) was, V(it + 1) where V(it - 1) was.
+      auto feed = [&](int it, int par) {
+        if (it + 2 < n_tiles) load_k(ahead2, par);
+        load_v(ahead1, par ^ 1);
+      };
+      auto fed = [&](int it) {
+        ahead1 = ahead2;
+        ahead2 = group_of(it + 3);
+      };
+      auto dma_wait = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+      auto masked = [&](int it) { return (tile0 + it) * BC + BC > all_see || there_of(it) != 15; };
+
       f32x16 oacc[NMB];
+      float nref, l_run, e_run;   // negated reference (exp2 domain), sums over this lane's half of the keys
+      float trigger;              // below zero until the row has met a score above -infinity: its first one becomes the reference
+
+      auto qk = [&](int par, f32x16 (&sacc)[MB]) {
+        const char* at = k_buf(par);
+        const int ka = here(at_lane.ka);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sacc[mb][i] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < KSTEPS; ++s) sacc[mb] = mfma_32x32x16(at_lane.k_operand(at, ka, mb, s), qop[s], sacc[mb]);
+        }
+      };
+      auto apply_mask = [&](int it, f32x16 (&sc)[MB]) {
+        const int there = there_of(it);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if ((tile0 + it) * BC + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(there >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
+      };
+      auto tile_max = [&](const f32x16 (&sc)[MB]) -> float {
+        float mt = sc[0][0];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[mb][i]);
+        return __builtin_fmaf(half_swap_max(mt), scale_log2e, nref);
+      };
+      auto exp_tile = [&](const f32x16 (&sc)[MB], bf16x8 (&pop)[TT]) -> float {   // -> sum before rounding, with STATS
+        float sum = 0.0f;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], scale_log2e, nref));
+            const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i + 1], scale_log2e, nref));
+            const bf16x2 pr = {(bf16)x0, (bf16)x1};
+            pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
+            pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
+            if constexpr (STATS) sum += x0 + x1;
+          }
+        return sum;
+      };
+      const RowSum row_sum(lane);
+      auto shift_reference = [&](float delta) {
+        nref -= delta;
+        const float alpha = __builtin_amdgcn_exp2f(fminf(-delta, 0.0f));   // (a first reference has no sums)
+        l_run *= alpha;
+        if constexpr (STATS) e_run *= alpha;
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+      };
+      // One tile, as in attn_bf16_impl.h. clean_c: neither it nor the next needs the mask.
+      auto body = [&](auto clean_c, auto next_c, int it, int par, f32x16 (&sc)[MB], f32x16 (&sn)[MB]) {
+        constexpr bool CLEAN = decltype(clean_c)::value, HAS_NEXT = decltype(next_c)::value;
+        if constexpr (HAS_NEXT) {
+          feed(it, par);
+          qk(par ^ 1, sn);
+          fed(it);
+        }
+        bf16x8 pop[TT];
+        float es = exp_tile(sc, pop);
+        float rs = row_sum(pop);
+        if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
+          const float mt = tile_max(sc);
+          const bool first = trigger < 0.0f && mt > -INFINITY;
+          if (first) trigger = kSumTrigger;
+          shift_reference(mt > kTau || first ? mt : 0.0f);
+          es = exp_tile(sc, pop);
+          rs = RowSum::by_lanes(pop);
+        }
+        l_run += rs;
+        if constexpr (STATS) e_run += es;
+        const char* vb = v_buf(par);
+        const int va = here(at_lane.va);
+        auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
+        {
+          constexpr int PF = (4 / NMB < TT) ? 4 / NMB : TT - 1;
+          bf16x8 va[PF + 1][NMB];
+#pragma unroll
+          for (int s = 0; s < PF; ++s)
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) va[s][mb] = v_operand(s, mb);
+#pragma unroll
+          for (int tt = 0; tt < TT; ++tt) {
+            if (tt + PF < TT) {
+#pragma unroll
+              for (int mb = 0; mb < NMB; ++mb) va[(tt + PF) % (PF + 1)][mb] = v_operand(tt + PF, mb);
+            }
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(va[tt % (PF + 1)][mb], pop[tt], oacc[mb]);
+          }
+          __builtin_amdgcn_sched_group_barrier(0x100, 2 * NMB * PF, 0);
+#pragma unroll
+          for (int i = 0; i < (TT - PF) * NMB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+          }
+          __builtin_amdgcn_sched_group_barrier(0x008, PF * NMB, 0);
+        }
+        if constexpr (!CLEAN) {   // (the wait behind these products as in attn_bf16_few.hip)
+          __builtin_amdgcn_sched_barrier(0);
+          asm volatile("s_nop 3");
+        }
+        if constexpr (HAS_NEXT) {
+          if constexpr (!CLEAN) {
+            if (masked(it + 1)) apply_mask(it + 1, sn);
+          }
+          dma_wait();
+        }
+        __syncthreads();
+      };
+
 #pragma unroll
       for (int mb = 0; mb < NMB; ++mb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
-      // The reference is the largest score so far, unscaled (a scaled one is rounded, which shows on large scores).
-      float ref = -FLT_MAX, l_run = 0.0f, e_run = 0.0f;
-      for (; tile < t_end; tile += WAVES) {
-        const int seen = there;
-        asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // K is there
-        const int ka = here(at_lane.ka), va = here(at_lane.va);
-        f32x16 sc[FMB];
-#pragma unroll
-        for (int mb = 0; mb < FMB; ++mb) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sc[mb][i] = 0.0f;
-#pragma unroll
-          for (int s = 0; s < KSTEPS; ++s) sc[mb] = mfma_32x32x16(at_lane.k_operand(kb, ka, mb, s), qop[s], sc[mb]);
+      nref = l_run = e_run = 0.0f;
+      trigger = kSumTrigger;
+      base = 0;
+      now = window_of(0);
+      next = window_of(32);
+      ahead2 = group_of(0);
+      load_v(ahead2, 0);
+      load_k(ahead2, 0);
+      ahead1 = group_of(1);
+      if (n_tiles > 1) load_k(ahead1, 1);
+      ahead2 = group_of(2);
+      dma_wait();
+      __syncthreads();
+      if (idle) {
+        __syncthreads();
+        for (int it = 0; it < n_tiles - 1; ++it) {
+          advance(it);
+          feed(it, it & 1);
+          fed(it);
+          dma_wait();
+          __syncthreads();
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // and read
-        const bool more = tile + WAVES < t_end;
-        if (more) {
-          ++at;
-          there = ask(of_k, k_base, tile + WAVES, kb);
-        }
-        const int n0 = tile * FT;
-        const bool some = n0 + FT > all_see || seen != (1 << GROUPS) - 1;
-        if (some) {
-#pragma unroll
-          for (int mb = 0; mb < FMB; ++mb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (n0 + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(seen >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
-        }
-        float mx = sc[0][0];
-#pragma unroll
-        for (int mb = 0; mb < FMB; ++mb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[mb][i]);
-        const float ref_new = fmaxf(ref, half_swap_max(mx));
-        if (__builtin_amdgcn_ballot_w64(ref_new > ref) != 0) {
-          const float alpha = __builtin_amdgcn_exp2f((ref - ref_new) * scale_log2e);
-          l_run *= alpha;
-          if constexpr (STATS) e_run *= alpha;
-#pragma unroll
-          for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
-          ref = ref_new;
-        }
-        // P rounded to bf16 as the operands of P.V; the row sum is taken over the rounded values, so that the rounding of a row's
-        // largest weights cancels
-        bf16x8 pop[FTT];
-        const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
-#pragma unroll
-        for (int mb = 0; mb < FMB; ++mb)
-#pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const float x0 = __builtin_amdgcn_exp2f((sc[mb][i] - ref) * scale_log2e), x1 = __builtin_amdgcn_exp2f((sc[mb][i + 1] - ref) * scale_log2e);
-            const bf16x2 pr = {(bf16)x0, (bf16)x1};
-            if constexpr (STATS) e_run += x0 + x1;
-            pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
-            pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
-            l_run = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, l_run, false);
+        __syncthreads();
+      } else {
+        f32x16 s0[MB], s1[MB];
+        qk(0, s0);
+        if (masked(0)) apply_mask(0, s0);
+        const float first_max = tile_max(s0);
+        if (first_max > -INFINITY) nref -= first_max;
+        else trigger = -1.0f;
+        __syncthreads();
+        const int n_full = min(max(all_see / BC - tile0, 0), n_tiles);   // tiles that need no mask for their place
+        int it = 0;
+        while (it < n_tiles - 1) {
+          advance(it);
+          if ((it & 1) == 0) {
+            // clean tiles of the window from `it` on
+            const uint64_t bad = __builtin_amdgcn_ballot_w64(now.there != 15) >> (it - base);
+            const int clean = min(min(n_full, it + (bad ? __builtin_ctzll(bad) : 64)), base + 61);   // (four tiles ahead are looked up)
+            if (it + 2 < clean) {
+              do {
+                body(yes, yes, it, 0, s0, s1);
+                body(yes, yes, it + 1, 1, s1, s0);
+                __builtin_amdgcn_sched_barrier(0);   // (as above, for the way out of this loop)
+                asm volatile("s_nop 3");
+                it += 2;
+              } while (it + 2 < clean);
+              continue;
+            }
           }
-        if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"i"(CPT) : "memory");   // V is there
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
-        bool odd = false;
-        if (some) odd = any_odd<FTT, NMB>(v_operand);
-        if (odd) {
-          odd_values<FTT, NMB>(oacc, pop, v_operand);
-        } else {
+          body(no, yes, it, it & 1, s0, s1);
 #pragma unroll
-          for (int tt = 0; tt < FTT; ++tt)
-#pragma unroll
-            for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(v_operand(tt, mb), pop[tt], oacc[mb]);
+          for (int mb = 0; mb < MB; ++mb) s0[mb] = s1[mb];
+          ++it;
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) ask(of_v, v_base, tile + WAVES, vb);
-        if (at == WINDOW / 2) {   // (the next to be asked for is behind it)
-          at = 0;
-          now = next;
-          next = window_of(tile + (1 + WINDOW / 2) * WAVES);
-        }
-        // (the wait behind these products as in attn_bf16_few.hip)
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 1");
+        advance(it);
+        body(no, no, it, it & 1, s0, s1);
       }
-      // the waves' states meet
-      const float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
-      if (hh == 0) few_stat[wave][lq] = f32x4{ref, l_tot, e_tot, 0.0f};
-      __syncthreads();
-      float ref_all = few_stat[0][lq][0], l_all = 0.0f, e_all = 0.0f;
+      if (HALVES == 2 && n_tiles < n_most) __syncthreads();   // (the other half's last tile)
+      // Where some rows do not see all keys of a tile, an infinity or a NaN among its values reaches their sums (0 times it). Sums that are no
+      // numbers have the unit's rows taken again as few rows, 32 at a time, which looks at the values of such tiles.
+      if (n_seen > all_see) {
+        float odd = 0.0f;
 #pragma unroll
-      for (int j = 1; j < WAVES; ++j) ref_all = fmaxf(ref_all, few_stat[j][lq][0]);
+        for (int mb = 0; mb < NMB; ++mb)
 #pragma unroll
-      for (int j = 0; j < WAVES; ++j) {
-        const f32x4 st = few_stat[j][lq];
-        const float x = __builtin_amdgcn_exp2f((st[0] - ref_all) * scale_log2e);
-        l_all += st[1] * x;
-        e_all += st[2] * x;
-      }
-      // (a row that sees nothing has sum 0 and is 0)
-      const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
-      // wave w's sums: 32 rows of D floats in its own buffers (K at d = 64, K and V at d = 128), the 16-byte pieces exchanged by the row
-#pragma unroll
-      for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const int piece = 8 * mb + 2 * i4 + hh;   // channels 4*piece ..
-          float* dst = (float*)(mb < 2 ? kb : vb);
-          const f32x4 x = {oacc[mb][4 * i4] * weight, oacc[mb][4 * i4 + 1] * weight, oacc[mb][4 * i4 + 2] * weight, oacc[mb][4 * i4 + 3] * weight};
-          *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
-        }
-      __syncthreads();
-      const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows;
-      for (int i = tid; i < min(u.rows - u.m0, 32) * (D / 4); i += kThreads) {
-        const int row = i / (D / 4), piece = i % (D / 4), mr = u.m0 + row;
-        const int at = row * 256 + (((piece & 15) ^ (row & 15)) << 4);
-        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < WAVES; ++j) {
-          const char* of = piece < 16 ? (j < WAVES / 2 ? k_lds0 : k_lds1) : (j < WAVES / 2 ? v_lds0 : v_lds1);
-          x += *(const f32x4*)(of + j % (WAVES / 2) * FEWB + at);
-        }
-        if (whole) {
-          const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
-          *(bf16x4*)(o + ((int64_t)(u.q0 + mr / group) * H + head * group + mr % group) * D + piece * 4) = y;
-        } else {
-          *(f32x4*)(part_o + (slot + row) * D + piece * 4) = x;
+          for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(oacc[mb][i], 0.0f, odd);
+        if (__syncthreads_or(odd != 0.0f)) {   // (NaN is)
+          few = true;
+          continue;
         }
       }
-      if (wave == 0 && hh == 0 && m < u.rows) {
-        if (!whole) part_stat[slot + lq] = f32x4{ref_all * scale_log2e, l_all, e_all, 0.0f};
-        else if (STATS) lse[(int64_t)token * H + q_of] = row_statistic(ref_all * scale_log2e, e_all);
+
+      // ---- the halves meet: each hands the other one half of the channels and finishes the rest ----------------
+      constexpr int OB = NMB / HALVES;
+      const int c0 = HALVES == 2 ? half * (D / 2) : 0;
+      float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
+      float ref = -nref;
+      f32x16 out[OB];
+      if constexpr (HALVES == 2) {
+        static_assert(kRW * OB * 4096 <= BUFB && WAVES * 512 <= BUFB, "the exchange fits the tile buffers");
+        f32x4* stat = (f32x4*)k_lds0;
+        f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
+        const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
+        if (hh == 0) stat[wave * 32 + lq] = f32x4{-nref, l_tot, e_tot, 0.0f};
+#pragma unroll
+        for (int mb = 0; mb < OB; ++mb) {
+          f32x16 theirs;
+          if (half) {
+            theirs = oacc[mb];
+            out[mb] = oacc[mb + OB];
+          } else {
+            theirs = oacc[mb + OB];
+            out[mb] = oacc[mb];
+          }
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) give[(mb * 4 + i4) * 64] = f32x4{theirs[4 * i4], theirs[4 * i4 + 1], theirs[4 * i4 + 2], theirs[4 * i4 + 3]};
+        }
+        __syncthreads();
+        // (a half that saw nothing of a row has sum 0 and no reference; a NaN sum makes the row NaN)
+        const f32x4 st = stat[(wave ^ kRW) * 32 + lq];
+        const float mine_ref = l_tot == 0.0f ? -FLT_MAX : -nref, other_ref = st[1] == 0.0f ? -FLT_MAX : st[0];
+        ref = fmaxf(mine_ref, other_ref);
+        const float wm = __builtin_amdgcn_exp2f(mine_ref - ref), wo = __builtin_amdgcn_exp2f(other_ref - ref);
+        l_tot = __builtin_fmaf(wm, l_tot, wo * st[1]);
+        e_tot = __builtin_fmaf(wm, e_tot, wo * st[2]);
+#pragma unroll
+        for (int mb = 0; mb < OB; ++mb)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const f32x4 x = take[(mb * 4 + i4) * 64];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]);
+          }
+      } else {
+#pragma unroll
+        for (int mb = 0; mb < OB; ++mb) out[mb] = oacc[mb];
+      }
+      const float inv = !whole ? 1.0f : l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
+      if (m < u.rows) {
+        const int64_t row = (int64_t)token * H + q_of;
+        const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows + rw * 32 + lq;
+        if (hh == 0 && half == 0) {
+          if (!whole) part_stat[slot] = f32x4{ref, l_tot, e_tot, 0.0f};
+          else if (STATS) lse[row] = row_statistic(ref, e_tot);
+        }
+#pragma unroll
+        for (int mb = 0; mb < OB; ++mb)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const int c = c0 + 32 * mb + 8 * i4 + 4 * hh;
+            const f32x4 x = f32x4{out[mb][4 * i4], out[mb][4 * i4 + 1], out[mb][4 * i4 + 2], out[mb][4 * i4 + 3]} * inv;
+            if (whole) *(bf16x4*)(o + row * D + c) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+            else *(f32x4*)(part_o + slot * D + c) = x;
+          }
       }
       __syncthreads();   // (the next unit's tiles take the place of the sums)
-      continue;
+      break;
     }
-    const int lane = here(tid) & 63;
-    const Places<D> at_lane(lane, row_bytes);
-    const int lq = at_lane.lq, hh = at_lane.hh;
-    const int m = u.m0 + rw * 32 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
-    const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
-    const int lim = min(causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
-    const int seen_tiles = (n_seen + BC - 1) / BC;
-    // the halves' tiles; a half without any walks one behind the last key: zeros, masked out
-    const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + HALVES - 1) / HALVES, 1);
-    const int n_tiles = half ? max(n_all - n_most, 1) : n_most;
-    const int tile0 = half ? (n_all > 1 ? t0 + n_most : seen_tiles) : (n_all > 0 ? t0 : seen_tiles);
-    const bool idle = u.m0 + rw * 32 >= u.rows;   // a wave without rows brings its part of the tiles in
-
-    bf16x8 qop[KSTEPS];
-    {
-      const bf16* q_row = q + token * q_token + q_of * q_head;
-#pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
-    }
-#pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(qop[s]));   // (here before the tiles are asked for)
-
-    // Lane i: where the wave's 16 keys of tile (first + i) of the half lie, and which of the tile's groups lie in the cache.
-    struct Window {
-      uint32_t lo, hi;
-      int there;
-    };
-    auto window_of = [&](int first) {
-      Window w = {0, 0, 0};
-      const int key = (tile0 + first + lane) * BC;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const PageWindow p = page_window(table, key + 16 * g, n_seen, page_size, n_pages, page_bytes, row_bytes);
-        w.there |= p.there << g;
-        if (g == rw) {
-          w.lo = p.lo;
-          w.hi = p.hi;
-        }
-      }
-      return w;
-    };
-    // Two windows, the second from the middle of the first on; it takes the first's place when that half is done with.
-    int base = 0;
-    Window now = window_of(0), next = window_of(32);
-    auto advance = [&](int it) {   // tiles before `it` are done with: those up to it + 31 lie in the window from here on
-      if (it < base + 32) return;
-      base += 32;
-      now = next;
-      next = window_of(base + 32);
-    };
-    auto there_of = [&](int it) { return __builtin_amdgcn_readlane(now.there, it - base); };
-    const std::true_type yes;
-    const std::false_type no;
-    auto load_group = [&](auto of_k, const char* from, int it, char* to) {
-      const int l = it - base;
-      const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)now.lo, l), hi = (uint32_t)__builtin_amdgcn_readlane((int)now.hi, l);
-      const int is = there_of(it) >> rw & 1;
-      const int rows = min(n_seen - ((tile0 + it) * BC + 16 * rw), 16);
-      const unsigned bytes = is ? (unsigned)((rows - 1) * row_bytes + ROWB) : 0u;
-      if constexpr (decltype(of_k)::value) at_lane.load_k(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + rw * LPG * 1024);
-      else at_lane.load_v(from + (lo | (uint64_t)hi << 32), bytes, row_bytes, to + rw * LPG * 1024);
-    };
-    // What tile `it` brings in: K(it + 2) where K(it) was, V(it + 1) where V(it - 1) was.
-    auto feed = [&](int it, int par) {
-      if (it + 2 < n_tiles) load_group(yes, k_base, it + 2, k_buf(par));
-      load_group(no, v_base, it + 1, v_buf(par ^ 1));
-    };
-    auto dma_wait = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
-    auto masked = [&](int it) { return (tile0 + it) * BC + BC > all_see || there_of(it) != 15; };
-
-    f32x16 oacc[NMB];
-#pragma unroll
-    for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
-    float nref = 0.0f, l_run = 0.0f, e_run = 0.0f;   // negated reference (exp2 domain), sums over this lane's half of the keys
-    // Below zero until the row has met a score above -infinity: its first one becomes the reference.
-    float trigger = kSumTrigger;
-
-    auto qk = [&](int par, f32x16 (&sacc)[MB]) {
-      const char* at = k_buf(par);
-      const int ka = here(at_lane.ka);
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sacc[mb][i] = 0.0f;
-#pragma unroll
-        for (int s = 0; s < KSTEPS; ++s) sacc[mb] = mfma_32x32x16(at_lane.k_operand(at, ka, mb, s), qop[s], sacc[mb]);
-      }
-    };
-    auto apply_mask = [&](int it, f32x16 (&sc)[MB]) {
-      const int there = there_of(it);
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if ((tile0 + it) * BC + 32 * mb + 8 * (i >> 2) + 4 * hh + (i & 3) > lim || !(there >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
-    };
-    auto tile_max = [&](const f32x16 (&sc)[MB]) -> float {
-      float mt = sc[0][0];
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[mb][i]);
-      return __builtin_fmaf(half_swap_max(mt), scale_log2e, nref);
-    };
-    auto exp_tile = [&](const f32x16 (&sc)[MB], bf16x8 (&pop)[TT]) -> float {   // -> sum before rounding, with STATS
-      float sum = 0.0f;
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], scale_log2e, nref));
-          const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i + 1], scale_log2e, nref));
-          const bf16x2 pr = {(bf16)x0, (bf16)x1};
-          pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
-          pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
-          if constexpr (STATS) sum += x0 + x1;
-        }
-      return sum;
-    };
-    const RowSum row_sum(lane);
-    auto shift_reference = [&](float delta) {
-      nref -= delta;
-      const float alpha = __builtin_amdgcn_exp2f(fminf(-delta, 0.0f));   // (a first reference has no sums)
-      l_run *= alpha;
-      if constexpr (STATS) e_run *= alpha;
-#pragma unroll
-      for (int mb = 0; mb < NMB; ++mb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
-    };
-    // One tile, as in attn_bf16_impl.h. clean_c: neither it nor the next needs the mask.
-    auto body = [&](auto clean_c, auto next_c, int it, int par, f32x16 (&sc)[MB], f32x16 (&sn)[MB]) {
-      constexpr bool CLEAN = decltype(clean_c)::value, HAS_NEXT = decltype(next_c)::value;
-      if constexpr (HAS_NEXT) {
-        feed(it, par);
-        qk(par ^ 1, sn);
-      }
-      bf16x8 pop[TT];
-      float es = exp_tile(sc, pop);
-      float rs = row_sum(pop);
-      if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
-        const float mt = tile_max(sc);
-        const bool first = trigger < 0.0f && mt > -INFINITY;
-        if (first) trigger = kSumTrigger;
-        shift_reference(mt > kTau || first ? mt : 0.0f);
-        es = exp_tile(sc, pop);
-        rs = RowSum::by_lanes(pop);
-      }
-      l_run += rs;
-      if constexpr (STATS) e_run += es;
-      const char* vb = v_buf(par);
-      const int va = here(at_lane.va);
-      auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
-      bool odd = false;
-      if constexpr (!CLEAN) {
-        if (masked(it)) odd = any_odd<TT, NMB>(v_operand);
-      }
-      if (!CLEAN && odd) {
-        odd_values<TT, NMB>(oacc, pop, v_operand);
-      } else {
-        constexpr int PF = (4 / NMB < TT) ? 4 / NMB : TT - 1;
-        bf16x8 va[PF + 1][NMB];
-#pragma unroll
-        for (int s = 0; s < PF; ++s)
-#pragma unroll
-          for (int mb = 0; mb < NMB; ++mb) va[s][mb] = v_operand(s, mb);
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt) {
-          if (tt + PF < TT) {
-#pragma unroll
-            for (int mb = 0; mb < NMB; ++mb) va[(tt + PF) % (PF + 1)][mb] = v_operand(tt + PF, mb);
-          }
-#pragma unroll
-          for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(va[tt % (PF + 1)][mb], pop[tt], oacc[mb]);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * NMB * PF, 0);
-#pragma unroll
-        for (int i = 0; i < (TT - PF) * NMB; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, PF * NMB, 0);
-      }
-      if constexpr (!CLEAN) {   // (the wait behind these products as in attn_bf16_few.hip)
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 3");
-      }
-      if constexpr (HAS_NEXT) {
-        if constexpr (!CLEAN) {
-          if (masked(it + 1)) apply_mask(it + 1, sn);
-        }
-        dma_wait();
-      }
-      __syncthreads();
-    };
-
-    load_group(no, v_base, 0, v_buf(0));
-    load_group(yes, k_base, 0, k_buf(0));
-    if (n_tiles > 1) load_group(yes, k_base, 1, k_buf(1));
-    dma_wait();
-    __syncthreads();
-    if (idle) {
-      __syncthreads();
-      for (int it = 0; it < n_tiles - 1; ++it) {
-        advance(it);
-        feed(it, it & 1);
-        dma_wait();
-        __syncthreads();
-      }
-      __syncthreads();
-    } else {
-      f32x16 s0[MB], s1[MB];
-      qk(0, s0);
-      if (masked(0)) apply_mask(0, s0);
-      const float first_max = tile_max(s0);
-      if (first_max > -INFINITY) nref -= first_max;
-      else trigger = -1.0f;
-      __syncthreads();
-      const int n_full = min(max(all_see / BC - tile0, 0), n_tiles);   // tiles that need no mask for their place
-      int it = 0;
-      while (it < n_tiles - 1) {
-        advance(it);
-        if ((it & 1) == 0) {
-          // clean tiles of the window from `it` on
-          const uint64_t bad = __builtin_amdgcn_ballot_w64(now.there != 15) >> (it - base);
-          const int clean = min(min(n_full, it + (bad ? __builtin_ctzll(bad) : 64)), base + 62);   // (loads run three tiles ahead)
-          for (; it + 2 < clean; it += 2) {
-            body(yes, yes, it, 0, s0, s1);
-            body(yes, yes, it + 1, 1, s1, s0);
-            __builtin_amdgcn_sched_barrier(0);   // (as above, for the way out of this loop)
-            asm volatile("s_nop 3");
-          }
-          if (it == n_tiles - 1) break;
-        }
-        body(no, yes, it, it & 1, s0, s1);
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) s0[mb] = s1[mb];
-        ++it;
-      }
-      advance(it);
-      body(no, no, it, it & 1, s0, s1);
-    }
-    if (HALVES == 2 && n_tiles < n_most) __syncthreads();   // (the other half's last tile)
-
-    // ---- the halves meet: each hands the other one half of the channels and finishes the rest ----------------
-    constexpr int OB = NMB / HALVES;
-    const int c0 = HALVES == 2 ? half * (D / 2) : 0;
-    float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
-    float ref = -nref;
-    f32x16 out[OB];
-    if constexpr (HALVES == 2) {
-      static_assert(kRW * OB * 4096 <= BUFB && WAVES * 512 <= BUFB, "the exchange fits the tile buffers");
-      f32x4* stat = (f32x4*)k_lds0;
-      f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
-      const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
-      if (hh == 0) stat[wave * 32 + lq] = f32x4{-nref, l_tot, e_tot, 0.0f};
-#pragma unroll
-      for (int mb = 0; mb < OB; ++mb) {
-        f32x16 theirs;
-        if (half) {
-          theirs = oacc[mb];
-          out[mb] = oacc[mb + OB];
-        } else {
-          theirs = oacc[mb + OB];
-          out[mb] = oacc[mb];
-        }
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) give[(mb * 4 + i4) * 64] = f32x4{theirs[4 * i4], theirs[4 * i4 + 1], theirs[4 * i4 + 2], theirs[4 * i4 + 3]};
-      }
-      __syncthreads();
-      // (a half that saw nothing of a row has sum 0 and no reference; a NaN sum makes the row NaN)
-      const f32x4 st = stat[(wave ^ kRW) * 32 + lq];
-      const float mine_ref = l_tot == 0.0f ? -FLT_MAX : -nref, other_ref = st[1] == 0.0f ? -FLT_MAX : st[0];
-      ref = fmaxf(mine_ref, other_ref);
-      const float wm = __builtin_amdgcn_exp2f(mine_ref - ref), wo = __builtin_amdgcn_exp2f(other_ref - ref);
-      l_tot = __builtin_fmaf(wm, l_tot, wo * st[1]);
-      e_tot = __builtin_fmaf(wm, e_tot, wo * st[2]);
-#pragma unroll
-      for (int mb = 0; mb < OB; ++mb)
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const f32x4 x = take[(mb * 4 + i4) * 64];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]);
-        }
-    } else {
-#pragma unroll
-      for (int mb = 0; mb < OB; ++mb) out[mb] = oacc[mb];
-    }
-    const float inv = !whole ? 1.0f : l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
-    if (m < u.rows) {
-      const int64_t row = (int64_t)token * H + q_of;
-      const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows + rw * 32 + lq;
-      if (hh == 0 && half == 0) {
-        if (!whole) part_stat[slot] = f32x4{ref, l_tot, e_tot, 0.0f};
-        else if (STATS) lse[row] = row_statistic(ref, e_tot);
-      }
-#pragma unroll
-      for (int mb = 0; mb < OB; ++mb)
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const int c = c0 + 32 * mb + 8 * i4 + 4 * hh;
-          const f32x4 x = f32x4{out[mb][4 * i4], out[mb][4 * i4 + 1], out[mb][4 * i4 + 2], out[mb][4 * i4 + 3]} * inv;
-          if (whole) *(bf16x4*)(o + row * D + c) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
-          else *(f32x4*)(part_o + slot * D + c) = x;
-        }
-    }
-    __syncthreads();   // (the next unit's tiles take the place of the sums)
   }
 }
 

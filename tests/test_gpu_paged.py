@@ -165,12 +165,15 @@ def test_values_that_later_tokens_alone_see(new, dtype):
     o, lse = _attention(b)
     clean = Batch([new + 70], [new], 4, 2, 64, dtype)
     oc, lc = _attention(clean)
-    assert torch.equal(lse, lc)
-    other = [c for c in range(64) if c != 5]
-    assert torch.equal(o[..., other], oc[..., other])
+    # What they do not reach is what it would be without them, to the bounds of any call (rows with such values may be summed in another order).
+    rest = o.clone()
+    rest[new // 2 if new > 1 else 0:, :, 5] = oc[new // 2 if new > 1 else 0:, :, 5]
+    some = [max(i, 0) for i in (0, 1, new // 2 - 1, new // 2, new - 2, new - 1)]
+    _check(clean, oc, lc, rows_of=some)
+    _check(clean, rest, lse, rows_of=some)
+    assert rest.isfinite().all() and ((rest - oc).abs() <= 4 * HALF_STEP[BF] * (clean.values[0].abs().max())).all()
     assert (o[-1, :, 5].isnan() if new > 1 else o[-1, :, 5] == float("inf")).all()   # (of one token, the second value stands)
     if new > 1:
-        assert torch.equal(o[:new // 2, :, 5], oc[:new // 2, :, 5])
         assert (o[new // 2:-1, :, 5] == float("inf")).all()
 
 
