@@ -426,7 +426,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
 
       auto qk = [&](int par, f32x16 (&sacc)[MB]) {
         const char* at = k_buf(par);
-        const int ka = here(at_lane.ka);
+        const int ka = at_lane.ka;
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
         l_run += rs;
         if constexpr (STATS) e_run += es;
         const char* vb = v_buf(par);
-        const int va = here(at_lane.va);
+        const int va = at_lane.va;
         auto v_operand = [&](int tt, int mb) { return at_lane.v_operand(vb, va, tt, mb); };
         {
           constexpr int PF = (4 / NMB < TT) ? 4 / NMB : TT - 1;
