@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
     const bf16* __restrict__ q, const bf16* __restrict__ k_pages, const bf16* __restrict__ v_pages, bf16* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int row_bytes, int64_t q_token,
-    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat) {
+    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat, PagedCut* __restrict__ cuts) {
   constexpr int BC = kTileKeys, ROWB = D * 2, TILEB = BC * ROWB;
   constexpr int MB = BC / 32, TT = BC / 16, KSTEPS = D / 16, NMB = D / 32;
   constexpr int LPG = 16 * ROWB / 1024;   // direct loads of 16 keys
@@ -108,6 +108,8 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
     const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
     pos = paged_cut(line, wg, length, total);
     end = paged_cut(line, wg + 1, length, total);
+    const PagedCut cut = paged_mark<kUnitRows>(line, pos, end, length, total);
+    if (tid == 0) cuts[wg] = cut;
   }
   while (pos < end) {
     PagedUnit u;
@@ -688,17 +690,15 @@ template <int D, int HALVES>
 hipError_t launch_halves(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                          const PagedLaunch& l, hipStream_t stream) {
   const float scale_log2e = scale * 1.4426950408889634f;
-  float* part_o = (float*)scratch;
-  f32x4* part_stat = (f32x4*)((char*)scratch + paged_sum_bytes(l.workgroups, kUnitRows, D));
+  const PagedScratch at(scratch, l.workgroups, kUnitRows, D);
   hipLaunchKernelGGL((p.lse_out ? paged_kernel<D, true, HALVES> : paged_kernel<D, false, HALVES>), dim3((unsigned)l.workgroups), dim3(kRW * HALVES * 64), 0,
                      stream, (const bf16*)q, (const bf16*)k_pages, (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H,
                      p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, p.page_stride * 2, p.head_stride * 2, (int)(p.row_stride * 2),
-                     p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, part_o, part_stat);
+                     p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, at.sums, at.stats, at.cuts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kUnitRows, kTileKeys>), dim3(paged_combine_grid(p, kUnitRows)), dim3(256), 0,
-                     stream, part_o, part_stat, (bf16*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens,
-                     p.max_pages * p.page_size, l.workgroups, l.least);
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kUnitRows>), dim3((unsigned)(l.workgroups * (kUnitRows * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
+                     at.cuts, (bf16*)o, p.lse_out, p.H, p.Hkv);
   return hipGetLastError();
 }
 

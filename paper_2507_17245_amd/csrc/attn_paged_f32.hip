@@ -23,7 +23,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_pages, const float* __restrict__ v_pages, float* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int64_t row_bytes, int64_t q_token,
-    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat) {
+    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat, PagedCut* __restrict__ cuts) {
   constexpr int NMB = D / 32, HALF = D / 2;
   __shared__ __attribute__((aligned(16))) float sums[kWaves][kRows][D + 4];
   __shared__ f32x2 stat_lds[kWaves][kRows];
@@ -38,6 +38,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
     const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
     pos = paged_cut(line, blockIdx.x, length, total);
     end = paged_cut(line, blockIdx.x + 1, length, total);
+    const PagedCut cut = paged_mark<kRows>(line, pos, end, length, total);
+    if (tid == 0) cuts[blockIdx.x] = cut;
   }
   while (pos < end) {
     PagedUnit u;
@@ -223,17 +225,15 @@ template <int D>
 hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                     const PagedLaunch& l, hipStream_t stream) {
   const float scale_log2e = scale * 1.4426950408889634f;
-  float* part_o = (float*)scratch;
-  f32x4* part_stat = (f32x4*)((char*)scratch + paged_sum_bytes(l.workgroups, kRows, D));
+  const PagedScratch at(scratch, l.workgroups, kRows, D);
   hipLaunchKernelGGL((paged_f32_kernel<D>), dim3((unsigned)l.workgroups), dim3(kThreads), 0, stream, (const float*)q, (const float*)k_pages,
                      (const float*)v_pages, (float*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.n_pages,
                      p.page_size, p.max_pages, p.page_stride * 4, p.head_stride * 4, p.row_stride * 4, p.q_stride[0], p.q_stride[1], p.causal,
-                     scale_log2e, l.ranges, l.least, part_o, part_stat);
+                     scale_log2e, l.ranges, l.least, at.sums, at.stats, at.cuts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows, kTile>), dim3(paged_combine_grid(p, kRows)), dim3(256), 0, stream, part_o,
-                     part_stat, (float*)o, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.max_pages * p.page_size,
-                     l.workgroups, l.least);
+  hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows>), dim3((unsigned)(l.workgroups * (kRows * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
+                     at.cuts, (float*)o, p.lse_out, p.H, p.Hkv);
   return hipGetLastError();
 }
 

@@ -167,69 +167,77 @@ __device__ inline PageWindow page_window(const int* __restrict__ table, int key,
 // log-sum-exp of a row from its reference (log2 units) and the sum relative to it
 __device__ inline float row_statistic(float ref, float sum) { return sum == 0.0f ? -INFINITY : 0.6931471805599453f * (ref + __builtin_log2f(sum)); }
 
-// Units that cuts fall into, from the sums of their parts; a workgroup takes 1024 / D rows of one at a time, first those of all
-// units that every unit has. Where there are fewer rows, lanes share a row's parts. E: type of o.
-template <typename E, int D, int ROWS, int KEYS>
+// What the combine kernel knows of a unit that cuts fall into, left by the workgroup of its first part (rows 0: there is none).
+struct PagedCut {
+  int rows, q0, m0, head;   // of the unit
+  int last;                 // its last cut; the first is the next workgroup's
+  int unused[3];
+};
+// The range from `begin` to `end`: whether a unit that begins in it is cut at its end.
+template <int ROWS, typename LINE>
+__device__ inline PagedCut paged_mark(const LINE& line, unsigned begin, unsigned end, unsigned length, unsigned total) {
+  PagedCut cut = {0, 0, 0, 0, 0, {0, 0, 0}};
+  PagedUnit u;
+  const unsigned head = end / line.total;
+  if (end >= total || !line.template find<false>(end - head * line.total, &u)) return cut;
+  const unsigned first = head * line.total + u.first;
+  if (first == end || first < begin) return cut;
+  return PagedCut{min(ROWS, u.rows - u.m0), u.q0, u.m0, (int)head, (int)((first + (unsigned)u.tiles - paged_snap(length)) / length), {0, 0, 0}};
+}
+
+// Units that cuts fall into, from the sums of their parts: a workgroup for every 1024 / D rows that a unit may have, behind every cut. Where
+// there are fewer rows, lanes share a row's parts. E: type of o.
+template <typename E, int D, int ROWS>
 __global__ __launch_bounds__(256) void paged_combine_kernel(
-    const float* __restrict__ part_o, const f32x4* __restrict__ part_stat, E* __restrict__ o, const int* __restrict__ q_start,
-    const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv, int n_seq, int n_tokens, int max_keys, int workgroups, int least) {
+    const float* __restrict__ part_o, const f32x4* __restrict__ part_stat, const PagedCut* __restrict__ cuts, E* __restrict__ o,
+    float* __restrict__ lse, int H, int Hkv) {
   constexpr int TAKE = 1024 / D, C4 = D / 4;
-  const int group = H / Hkv;
   __shared__ f32x4 x_lds[256], stat_lds[256];
-  const PagedLine<ROWS, KEYS> line(PagedBatch{q_start, kv_len, n_seq, n_tokens, Hkv, group, max_keys, 0});
-  const unsigned length = paged_range(line.total * (unsigned)Hkv, workgroups, least), snap = paged_snap(length);
-  const unsigned each = line.units * (unsigned)Hkv;
-  for (unsigned item = blockIdx.x; item < each * (ROWS / TAKE); item += gridDim.x) {
-    const unsigned piece = item / each, of = item % each;
-    const int head = (int)(of % (unsigned)Hkv);
-    PagedUnit u;
-    if (!line.template find<true>(of / (unsigned)Hkv, &u)) return;
-    const unsigned first = (unsigned)head * line.total + u.first;
-    if ((unsigned)u.tiles < snap) continue;
-    const int w0 = (int)((first + snap + length - 1) / length), w1 = (int)((first + (unsigned)u.tiles - snap) / length);   // its cuts
-    const int rows = min(u.rows - u.m0 - (int)piece * TAKE, TAKE);
-    if (w0 > w1 || rows <= 0) continue;
-    int side = 1;   // lanes' rows side by side, a power of two
-    while (side < rows) side *= 2;
-    const int c = threadIdx.x % C4 * 4, at_row = threadIdx.x / C4 % side, share = threadIdx.x / (C4 * side), shares = TAKE / side;
-    const int row = (int)piece * TAKE + min(at_row, rows - 1), parts = w1 - w0 + 2;
-    auto slot_of = [&](int i) { return (i == 0 ? 2 * (size_t)w0 : 2 * (size_t)(w0 + i - 1) + 1) * ROWS + row; };
-    f32x4 all = {-FLT_MAX, 0.0f, 0.0f, 0.0f}, x = {0.0f, 0.0f, 0.0f, 0.0f};   // reference, sum, sum before rounding
-    auto add = [&](f32x4 st, f32x4 y) {
-      const float ref = fmaxf(all[0], st[0]);
-      const float a = __builtin_amdgcn_exp2f(all[0] - ref), b = __builtin_amdgcn_exp2f(st[0] - ref);
-      all = f32x4{ref, __builtin_fmaf(b, st[1], a * all[1]), __builtin_fmaf(b, st[2], a * all[2]), 0.0f};
+  constexpr int PIECES = ROWS / TAKE;
+  // (pieces shifted by the cut: neither one cut's pieces nor the first pieces of all cuts end up on one XCD)
+  const int group = H / Hkv, wg = blockIdx.x / PIECES, piece = (blockIdx.x + wg) % PIECES;
+  const PagedCut u = cuts[wg];
+  const int rows = min(u.rows - piece * TAKE, TAKE);
+  if (rows <= 0) return;
+  int side = 1;   // lanes' rows side by side, a power of two
+  while (side < rows) side *= 2;
+  const int c = threadIdx.x % C4 * 4, at_row = threadIdx.x / C4 % side, share = threadIdx.x / (C4 * side), shares = TAKE / side;
+  const int row = piece * TAKE + min(at_row, rows - 1), first = wg + 1, parts = u.last - first + 2;
+  auto slot_of = [&](int i) { return (i == 0 ? 2 * (size_t)first : 2 * (size_t)(first + i - 1) + 1) * ROWS + row; };
+  f32x4 all = {-FLT_MAX, 0.0f, 0.0f, 0.0f}, x = {0.0f, 0.0f, 0.0f, 0.0f};   // reference, sum, sum before rounding
+  auto add = [&](f32x4 st, f32x4 y) {
+    const float ref = fmaxf(all[0], st[0]);
+    const float a = __builtin_amdgcn_exp2f(all[0] - ref), b = __builtin_amdgcn_exp2f(st[0] - ref);
+    all = f32x4{ref, __builtin_fmaf(b, st[1], a * all[1]), __builtin_fmaf(b, st[2], a * all[2]), 0.0f};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(b, y[i], a * x[i]);
-    };
-    for (int i = share; i < parts; i += 4 * shares) {   // four parts in flight
-      f32x4 st[4], y[4];
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_fmaf(b, y[i], a * x[i]);
+  };
+  for (int i = share; i < parts; i += 4 * shares) {   // four parts in flight
+    f32x4 st[4], y[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const size_t slot = slot_of(min(i + j * shares, parts - 1));
-        st[j] = part_stat[slot];
-        y[j] = *(const f32x4*)(part_o + slot * D + c);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (i + j * shares < parts) add(st[j], y[j]);
+    for (int j = 0; j < 4; ++j) {
+      const size_t slot = slot_of(min(i + j * shares, parts - 1));
+      st[j] = part_stat[slot];
+      y[j] = *(const f32x4*)(part_o + slot * D + c);
     }
-    if (shares > 1) {
-      x_lds[threadIdx.x] = x;
-      stat_lds[threadIdx.x] = all;
-      __syncthreads();
-      if (share == 0)
-        for (int j = 1; j < shares; ++j) add(stat_lds[threadIdx.x + j * C4 * side], x_lds[threadIdx.x + j * C4 * side]);
-      __syncthreads();
-    }
-    if (share != 0 || at_row >= rows) continue;
-    const int mr = u.m0 + row;
-    const int64_t at = (int64_t)(u.q0 + mr / group) * H + head * group + mr % group;
-    x *= all[1] == 0.0f ? 0.0f : 1.0f / all[1];
-    typedef __attribute__((ext_vector_type(4))) E Four;
-    *(Four*)(o + at * D + c) = Four{(E)x[0], (E)x[1], (E)x[2], (E)x[3]};
-    if (lse && c == 0) lse[at] = row_statistic(all[0], all[2]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j * shares < parts) add(st[j], y[j]);
   }
+  if (shares > 1) {
+    x_lds[threadIdx.x] = x;
+    stat_lds[threadIdx.x] = all;
+    __syncthreads();
+    if (share == 0)
+      for (int j = 1; j < shares; ++j) add(stat_lds[threadIdx.x + j * C4 * side], x_lds[threadIdx.x + j * C4 * side]);
+  }
+  if (share != 0 || at_row >= rows) return;
+  const int mr = u.m0 + row;
+  const int64_t at = (int64_t)(u.q0 + mr / group) * H + u.head * group + mr % group;
+  x *= all[1] == 0.0f ? 0.0f : 1.0f / all[1];
+  typedef __attribute__((ext_vector_type(4))) E Four;
+  *(Four*)(o + at * D + c) = Four{(E)x[0], (E)x[1], (E)x[2], (E)x[3]};
+  if (lse && c == 0) lse[at] = row_statistic(all[0], all[2]);
 }
 
 // How a call is launched: units dealt out whole, or ranges with sums of their parts in scratch.
@@ -238,12 +246,18 @@ struct PagedLaunch {
 };
 // (no more units than this, whatever the sequences' shares of the tokens are)
 inline long long paged_units(const da_paged& p, int rows) { return (long long)p.n_tokens * (p.H / p.Hkv) / rows + std::min(p.n_seq, p.n_tokens); }
-inline size_t paged_sum_bytes(int workgroups, int rows, int d) { return (size_t)2 * workgroups * rows * d * 4; }
-inline size_t paged_launch_bytes(int workgroups, int rows, int d) { return (size_t)2 * workgroups * rows * (d + 4) * 4; }
-// Workgroups of the combine kernel: no more than are resident at a time, which find their sequences once.
-inline unsigned paged_combine_grid(const da_paged& p, int rows) {
-  return (unsigned)std::min(paged_units(p, rows) * p.Hkv * (rows * p.d / 1024), (long long)4 * kComputeUnits);
-}
+// Scratch: sums [2 * workgroups][rows][d], their statistics [2 * workgroups][rows][4], cuts [workgroups].
+inline size_t paged_launch_bytes(int workgroups, int rows, int d) { return (size_t)workgroups * (2 * (size_t)rows * (d + 4) * 4 + sizeof(PagedCut)); }
+struct PagedScratch {
+  float* sums;
+  f32x4* stats;
+  PagedCut* cuts;
+  PagedScratch(void* at, int workgroups, int rows, int d) {
+    sums = (float*)at;
+    stats = (f32x4*)(sums + (size_t)2 * workgroups * rows * d);
+    cuts = (PagedCut*)(stats + (size_t)2 * workgroups * rows);
+  }
+};
 // `most` workgroups are resident at a time. Ranges, unless no sequence is long enough for two of them, with what fits the scratch.
 inline PagedLaunch paged_launch(const da_paged& p, int rows, int keys, int most, size_t scratch_bytes) {
   const long long room = ((long long)p.max_pages * p.page_size + keys - 1) / keys;
