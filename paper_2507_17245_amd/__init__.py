@@ -413,11 +413,13 @@ def _fill_rotary(r, d, heads, norm, eps, weights, rope, cos, sin):
         r.cos_table, r.sin_table = cos.data_ptr(), sin.data_ptr()
 
 
-def _fill_workspace(p, workspace):
+def _fill_workspace(p, workspace, device):
     _check_buffer(workspace, "workspace", 0)
     if workspace is not None:
         p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     p.stream = _current_stream().value
+    import torch
+    p.device, p.current_device = device.index, torch.cuda.current_device
 
 
 def make_qk_params(q, k, q_out, k_out, norm=False, eps=1e-6, q_weight=None, k_weight=None, rope="none", cos=None, sin=None,
@@ -447,11 +449,21 @@ def make_qk_params(q, k, q_out, k_out, norm=False, eps=1e-6, q_weight=None, k_we
     if positions is not None:
         _check_index(positions, (B, N), "positions")
         p.positions = positions.data_ptr()
-    _fill_workspace(p, workspace)
+    _fill_workspace(p, workspace, q.device)
     p.layouts = {"q": _layout(q), "q_out": _layout(q_out), "k": k if k is None else _layout(k), "k_out": k if k is None else _layout(k_out)}
     p.weights = {"q": q_weight, "k": k_weight}
     p.held = (cos, sin, positions, workspace)
     return p
+
+
+def _run(name, params, *args):
+    """The call, on the stream and the device that params were made for."""
+    if params.current_device() != params.device:
+        raise ValueError(f"params were made for cuda:{params.device}, the current device is cuda:{params.current_device()}")
+    L = _lib or lib()
+    if params.stream is None:      # (the null stream: not what a short form has set since)
+        L.distr_attn_set_stream(None)
+    _check(getattr(L, name)(*args, ctypes.byref(params)))
 
 
 def _check_qk(params, tensors):
@@ -466,14 +478,13 @@ def _check_qk(params, tensors):
 def distr_attn_qk_norm_rope(q, k, q_out, k_out, params):
     """q_out, k_out = rotation(norm(q)), rotation(norm(k)), in one launch. -> (q_out, k_out)"""
     _check_qk(params, ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out")))
-    _check(lib().distr_attn_qk_norm_rope(_at(q), _at(k), _at(q_out), _at(k_out), ctypes.byref(params)))
+    _run("distr_attn_qk_norm_rope", params, _at(q), _at(k), _at(q_out), _at(k_out))
     return q_out, k_out
 
 
 def distr_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, params, dq_weight=None, dk_weight=None):
     """Gradient of distr_attn_qk_norm_rope: dq, dk (laid out like q, k) from dq_out, dk_out (like q_out, k_out) and the forward's
     inputs; dq_weight, dk_weight float32 in the weights' shapes ([d] where there is none), or None. -> (dq, dk)"""
-    import torch
     _check_qk(params, ((q, "q"), (k, "k"), (dq_out, "q_out"), (dk_out, "k_out"), (dq, "q"), (dk, "k")))
     for t, of in ((dq_weight, "q"), (dk_weight, "k")):
         if t is None:
@@ -482,10 +493,9 @@ def distr_attn_qk_norm_rope_bwd(q, k, dq_out, dk_out, dq, dk, params, dq_weight=
             raise ValueError("dk_weight without keys")
         w = params.weights[of]
         shape = (params.H if of == "q" else params.Hkv, params.d) if params.rotary.weight_heads else (params.d,)
-        if t.dtype != torch.float32 or tuple(t.shape) != (tuple(w.shape) if w is not None else shape) or not t.is_contiguous() or t.device != dq.device:
+        if _dtype_code(t) != DA_F32 or tuple(t.shape) != (tuple(w.shape) if w is not None else shape) or not t.is_contiguous() or t.device != dq.device:
             raise ValueError(f"d{of}_weight must be contiguous float32 of the weight's shape")
-    _check(lib().distr_attn_qk_norm_rope_bwd(_at(q), _at(k), _at(dq_out), _at(dk_out), _at(dq), _at(dk), _at(dq_weight), _at(dk_weight),
-                                             ctypes.byref(params)))
+    _run("distr_attn_qk_norm_rope_bwd", params, _at(q), _at(k), _at(dq_out), _at(dk_out), _at(dq), _at(dk), _at(dq_weight), _at(dk_weight))
     return dq, dk
 
 
@@ -539,7 +549,7 @@ def make_paged_params(k_pages, v_pages, page_table, kv_len, q_start, q=None, k=N
         if lse_out.dtype != torch.float32 or q is None or tuple(lse_out.shape) != tuple(q.shape[:2]) or not lse_out.is_contiguous():
             raise ValueError("lse_out must be contiguous float32 [tokens, H]")
         p.lse_out = lse_out.data_ptr()
-    _fill_workspace(p, workspace)
+    _fill_workspace(p, workspace, k_pages.device)
     p.layouts = {"pages": _layout(k_pages), "q": q if q is None else _layout(q), "k": k if k is None else _layout(k), "v": v if v is None else _layout(v)}
     p.held = (page_table, kv_len, q_start, lse_out, k_weight, cos, sin, positions, workspace)
     return p
@@ -558,7 +568,7 @@ def distr_attn_cache_append(k, v, k_pages, v_pages, params):
     _check_layout(k, params.layouts["k"], "k")
     _check_layout(v, params.layouts["v"], "v")
     _check_pages(k_pages, v_pages, params)
-    _check(lib().distr_attn_cache_append(_at(k), _at(v), _at(k_pages), _at(v_pages), ctypes.byref(params)))
+    _run("distr_attn_cache_append", params, _at(k), _at(v), _at(k_pages), _at(v_pages))
     return k_pages, v_pages
 
 
@@ -570,7 +580,7 @@ def distr_attn_paged_fwd(q, k_pages, v_pages, o, params):
     if o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or not o.is_contiguous():
         raise ValueError("o must be contiguous, of q's shape and dtype, on its device")
     _check_pages(k_pages, v_pages, params)
-    _check(lib().distr_attn_paged_fwd(_at(q), _at(k_pages), _at(v_pages), _at(o), ctypes.byref(params)))
+    _run("distr_attn_paged_fwd", params, _at(q), _at(k_pages), _at(v_pages), _at(o))
     return o
 
 

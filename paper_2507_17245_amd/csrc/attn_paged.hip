@@ -95,11 +95,12 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % kRW, half = HALVES == 1 ? 0 : wave / kRW;
   const int group = H / Hkv;
-  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
+  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size};
   auto k_buf = [&](int par) -> char* { return (par ? k_lds1 : k_lds0) + half * TILEB; };
   auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
 
-  const PagedLine<kUnitRows, BC> line(batch);
+  __shared__ PagedLds line_lds;
+  const PagedLine<kUnitRows, BC> line(batch, &line_lds, wave, WAVES);
   unsigned pos = 0, end = 1;
   int wg = blockIdx.x;
   if (HALVES == 2 && ranges) {

@@ -30,9 +30,10 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, hh = lane >> 5;
   const int group = H / Hkv;
-  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, Hkv, group, max_pages * page_size, causal};
+  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size};
 
-  const PagedLine<kRows, kTile> line(batch);
+  __shared__ PagedLds line_lds;
+  const PagedLine<kRows, kTile> line(batch, &line_lds, wave, kWaves);
   unsigned pos = 0, end = 1;
   if (ranges) {
     const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);

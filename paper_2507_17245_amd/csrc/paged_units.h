@@ -22,10 +22,9 @@ namespace {
 struct PagedBatch {
   const int* __restrict__ q_start;
   const int* __restrict__ kv_len;
-  int n_seq, n_tokens, n_heads_kv;
+  int n_seq, n_tokens;
   int group;       // query heads of a kv head
   int max_keys;    // that a row of the page table has room for
-  int causal;
 };
 
 struct PagedUnit {
@@ -49,6 +48,11 @@ __device__ inline unsigned wave_scan(unsigned x) {   // sums over the lanes up t
   return dpp_add<0x143, 0xc>(x);   // row_bcast 31: the second row's last lane to the upper two
 }
 
+struct PagedLds {   // of a workgroup
+  int seq[7][64];                     // the first 64 sequences
+  unsigned tiles[64], units[64];      // of each 64 sequences, up to 4096 of them
+};
+
 template <int ROWS, int KEYS>
 struct PagedSequence {   // what a lane knows of its sequence
   int q0, nq, len, units, tiles;
@@ -66,52 +70,78 @@ struct PagedSequence {   // what a lane knows of its sequence
     sum = wave_scan((unsigned)units * (unsigned)tiles);
     unit_sum = wave_scan((unsigned)units);
   }
+  __device__ PagedSequence(const PagedLds* lds, int lane)
+      : q0(lds->seq[0][lane]), nq(lds->seq[1][lane]), len(lds->seq[2][lane]), units(lds->seq[3][lane]), tiles(lds->seq[4][lane]),
+        sum((unsigned)lds->seq[5][lane]), unit_sum((unsigned)lds->seq[6][lane]) {}
+  __device__ void store(PagedLds* lds, int lane) const {
+    const int x[7] = {q0, nq, len, units, tiles, (int)sum, (int)unit_sum};
+#pragma unroll
+    for (int i = 0; i < 7; ++i) lds->seq[i][lane] = x[i];
+  }
   __device__ unsigned all_tiles() const { return (unsigned)__builtin_amdgcn_readlane((int)sum, 63); }
   __device__ unsigned all_units() const { return (unsigned)__builtin_amdgcn_readlane((int)unit_sum, 63); }
 };
 
-// The line of a kv head. The first 64 sequences stay in registers, a lane each; others are loaded again where they are asked for.
+// The line of a kv head. The first 64 sequences stay in LDS. Of more, up to 4096, LDS has the sums of each 64, which the waves
+// take a share of, and the 64 that are asked for are loaded again; beyond, the sums are taken again, too.
 template <int ROWS, int KEYS>
 struct PagedLine {
   typedef PagedSequence<ROWS, KEYS> Sequence;
   const PagedBatch b;
-  const Sequence head;
-  unsigned total, units;   // its tiles and units
-  __device__ explicit PagedLine(const PagedBatch& batch) : b(batch), head(batch, threadIdx.x & 63) {
+  PagedLds* const lds;
+  unsigned total;   // its tiles
+  // (called by all threads of the workgroup)
+  __device__ PagedLine(const PagedBatch& batch, PagedLds* to, int wave, int waves) : b(batch), lds(to) {
+    const int lane = threadIdx.x & 63, n = (b.n_seq + 63) / 64;
+    const Sequence head(b, lane);
+    if (wave == 0) head.store(lds, lane);
     total = head.all_tiles();
-    units = head.all_units();
-    for (int s0 = 64; s0 < b.n_seq; s0 += 64) {
-      const Sequence q(b, s0 + (threadIdx.x & 63));
-      total += q.all_tiles();
-      units += q.all_units();
+    if (n > 64) {
+      for (int c = 1; c < n; ++c) total += Sequence(b, c * 64 + lane).all_tiles();
+    } else if (n > 1) {
+      for (int c = wave; c < n; c += waves) {
+        const Sequence q(b, c * 64 + lane);
+        if (lane == 63) {
+          lds->tiles[c] = q.sum;
+          lds->units[c] = q.unit_sum;
+        }
+      }
     }
+    __syncthreads();
+    if (n > 1 && n <= 64) total = (unsigned)__builtin_amdgcn_readlane((int)wave_scan(lane < n ? lds->tiles[lane] : 0u), 63);
   }
   // The unit that holds place `x` (BY_UNIT: the x-th unit); false behind the last one.
   template <bool BY_UNIT>
   __device__ bool find(unsigned x, PagedUnit* out) const {
-    unsigned before = 0;
-    if (in<BY_UNIT>(head, 0, x, &before, out)) return true;
-    unsigned units_before = head.all_units();
-    for (int s0 = 64; s0 < b.n_seq; s0 += 64) {
-      const Sequence q(b, s0 + (threadIdx.x & 63));
-      if (in<BY_UNIT>(q, s0, BY_UNIT ? x - units_before : x, &before, out)) return true;
-      units_before += q.all_units();
+    const int lane = threadIdx.x & 63, n = (b.n_seq + 63) / 64;
+    if (n == 1) return in<BY_UNIT>(Sequence(lds, lane), 0, x, 0, out);
+    if (n <= 64) {
+      const unsigned t = lane < n ? lds->tiles[lane] : 0u, u = lane < n ? lds->units[lane] : 0u, ts = wave_scan(t), us = wave_scan(u);
+      const uint64_t past = __builtin_amdgcn_ballot_w64((BY_UNIT ? us : ts) > x);
+      if (past == 0) return false;
+      const int c = __builtin_ctzll(past);
+      const unsigned tiles = (unsigned)__builtin_amdgcn_readlane((int)(ts - t), c), units = (unsigned)__builtin_amdgcn_readlane((int)(us - u), c);
+      return in<BY_UNIT>(Sequence(b, c * 64 + lane), c * 64, x - (BY_UNIT ? units : tiles), tiles, out);
+    }
+    unsigned tiles = 0, units = 0;
+    for (int c = 0; c < n; ++c) {
+      const Sequence q(b, c * 64 + lane);
+      if (in<BY_UNIT>(q, c * 64, x - (BY_UNIT ? units : tiles), tiles, out)) return true;
+      tiles += q.all_tiles();
+      units += q.all_units();
     }
     return false;
   }
 
  private:
+  // among 64 sequences from s0 on, with `before` tiles in front of them
   template <bool BY_UNIT>
-  __device__ bool in(const Sequence& q, int s0, unsigned x, unsigned* before, PagedUnit* out) const {
-    const unsigned w = (unsigned)q.units * (unsigned)q.tiles;
-    const uint64_t past = __builtin_amdgcn_ballot_w64((BY_UNIT ? q.unit_sum : *before + q.sum) > x);
-    if (past == 0) {
-      *before += q.all_tiles();
-      return false;
-    }
+  __device__ bool in(const Sequence& q, int s0, unsigned x, unsigned before, PagedUnit* out) const {
+    const uint64_t past = __builtin_amdgcn_ballot_w64((BY_UNIT ? q.unit_sum : q.sum) > x);
+    if (past == 0) return false;
     const int i = __builtin_ctzll(past);
     auto of = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
-    const unsigned first = *before + (unsigned)of((int)(q.sum - w));
+    const unsigned first = (unsigned)of((int)(q.sum - (unsigned)q.units * (unsigned)q.tiles));
     const int tiles = of(q.tiles);
     const int unit = BY_UNIT ? (int)(x - (unsigned)of((int)(q.unit_sum - (unsigned)q.units))) : (int)((x - first) / (unsigned)tiles);
     out->seq = s0 + i;
@@ -121,7 +151,7 @@ struct PagedLine {
     out->m0 = unit * ROWS;
     out->rows = out->nq * b.group;
     out->tiles = tiles;
-    out->first = first + (unsigned)unit * (unsigned)tiles;
+    out->first = before + first + (unsigned)unit * (unsigned)tiles;
     return true;
   }
 };

@@ -25,15 +25,15 @@ def _attention(b, causal=True, scale=None, lse=True, workspace=True, q=None):
     return o.cpu(), row.cpu() if lse else None
 
 
-def _check(b, o, lse, causal=True, scale=None, seen=None, rows_of=None):
-    """Every row of every sequence (rows_of: some of its new tokens) and that no others were written."""
+def _check(b, o, lse, causal=True, scale=None, seen=None, rows_of=None, only=None):
+    """Every row of every sequence (rows_of: some of its new tokens; only: some sequences) and that no others were written."""
     scale = b.d ** -0.5 if scale is None else scale
     left = torch.ones(b.T, dtype=torch.bool)
     for s, (n, fresh) in enumerate(zip(b.lens, b.new)):
         r0 = int(b.start[s])
         left[r0:r0 + fresh] = False
         at = list(range(fresh)) if rows_of is None else sorted({i for i in rows_of if i < fresh})
-        if not at:
+        if not at or (only is not None and s not in only):
             continue
         places = [n - fresh + i if causal else n - 1 for i in at]
         rows = [r0 + i for i in at]
@@ -106,6 +106,60 @@ def test_many_sequences(n_seq, dtype):
     b = Batch(lens, new, 4, 2, 64, dtype, pad_back=1)
     o, lse = _attention(b)
     _check(b, o, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n_seq", [300, 4096, 4200])
+def test_very_many_sequences(n_seq, dtype):
+    """More than a wave's lanes of them, and more than the sums of 64 that a workgroup keeps; with and without ranges."""
+    g = torch.Generator().manual_seed(n_seq)
+    lens = torch.randint(0, 40, (n_seq,), generator=g).tolist()
+    lens[n_seq - 2] = 1500
+    new = [min(int(x), n) for x, n in zip(torch.randint(0, 3, (n_seq,), generator=g), lens)]
+    new[n_seq - 2], new[70] = 33, 0
+    b = Batch(lens, new, 2, 1, 64, dtype)
+    only = [0, 1, 63, 64, 65, 69, 70, 71, 127, 128, 255, 256, n_seq - 3, n_seq - 2, n_seq - 1] + list(range(200, 210))
+    for workspace in (True, 256):
+        o, lse = _attention(b, workspace=workspace)
+        _check(b, o, lse, only=only, rows_of=[0, 1, 31, 32])
+        assert o.isfinite().all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompts_that_fill_the_chip(d):
+    """Enough units for workgroups of their own: whole prompts, one behind a prefix, a single token and none beside them."""
+    lens, new = [1100, 700, 65, 130, 40], [1000, 140, 65, 1, 0]
+    b = Batch(lens, new, 64, 64, d, BF, page=64, order="tokens")
+    o, lse = _attention(b)
+    _check(b, o, lse, rows_of=[0, 63, 64, 127, 128, 139, 512, 999])
+    o, _ = _attention(b, causal=False, lse=False)
+    _check(b, o, None, causal=False, rows_of=[0, 64, 139, 999])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("new", [2, 150])
+def test_scores_that_are_no_numbers(new, dtype):
+    """A NaN or an infinity in one query row, and in one key, reaches the rows of its scores and no others."""
+    n = new + 90
+    b, clean = (Batch([n], [new], 4, 2, 64, dtype) for _ in range(2))
+    b.dev["q"][1, 2, 7] = float("nan")
+    place = n - 1                                    # a key that the last token alone sees
+    b.k_pages[int(b.table[0, place // 16]), 1, place % 16, 3] = float("inf")
+    (o, lse), (oc, lc) = _attention(b), _attention(clean)
+    odd = torch.zeros(new, 4, dtype=torch.bool)
+    odd[1, 2] = True
+    # an infinite score: NaN where it is the largest, nothing where the smallest
+    high = b.q[-1, 2:].float()[:, 3] > 0
+    odd[-1, 2:] |= high
+    low = torch.zeros_like(odd)
+    low[-1, 2:] = ~high
+    low &= ~odd
+    assert o[odd].isnan().all() and lse[odd].isnan().all() and o[~odd].isfinite().all() and lse[~odd].isfinite().all()
+    same = ~odd & ~low
+    _check(clean, oc, lc, rows_of=[0, 1, new // 2, new - 1])
+    o[odd | low], lse[odd | low] = oc[odd | low], lc[odd | low]
+    _check(clean, o, lse, rows_of=[0, 1, new // 2, new - 1])
+    assert same.sum() >= 4 * new - 3
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
@@ -395,6 +449,35 @@ def test_serving_steps(captured, dtype):
                 assert (err <= (bound + extra)[0]).all(), (step, s)
                 worst = max(worst, err.max().item())
         assert worst > 0
+
+
+def test_the_null_stream_is_the_null_stream():
+    """Calls of the short forms on another stream do not send the null stream's calls there."""
+    b = Batch([300], [2], 4, 2, 64, BF)
+    want, _ = _attention(b, lse=False)
+    p = da.make_paged_params(*b.cache(), q=b.dev["q"])
+    x = torch.randn(1, 2, 5, 64, device="cuda", dtype=BF)
+    y, rotated = torch.empty_like(x), torch.empty_like(x)
+    rows = da.make_qk_params(x, None, rotated, None, norm=True)
+    da.distr_attn_qk_norm_rope(x, None, rotated, None, rows)
+    expected = rotated.clone()
+    o = torch.zeros(b.T, b.H, b.d, dtype=BF, device="cuda")
+    rotated.zero_()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        da.distr_attn_exact_fwd(x, x, x, y, 64, 64)
+        torch.cuda._sleep(400_000_000)               # the side stream is busy for a while
+    da.distr_attn_paged_fwd(b.dev["q"], b.k_pages, b.v_pages, o, p)
+    da.distr_attn_qk_norm_rope(x, None, rotated, None, rows)
+    done = torch.cuda.Event()
+    done.record()
+    done.synchronize()
+    busy = not side.query()
+    got, turned = o.cpu(), rotated.cpu()
+    torch.cuda.synchronize()
+    if busy:                                         # (else nothing is shown)
+        assert torch.equal(got, want) and torch.equal(turned, expected.cpu())
 
 
 def test_streams_and_their_scratch():
