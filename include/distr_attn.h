@@ -253,7 +253,8 @@ typedef struct {
   da_rotary rotary;
   const int32_t *positions;  /* device [B][N]; null: row n of every batch is at position n                */
   void *stream;          /* as in da_params                                                              */
-  void *workspace;       /* backward with weight gradients: as in da_params, distr_attn_qk_bwd_workspace_bytes() */
+  void *workspace;       /* backward with weight gradients: as in da_params, distr_attn_qk_bwd_workspace_bytes();
+                            one call's until the call has ended */
   size_t workspace_bytes;
 } da_qk;
 
@@ -305,7 +306,9 @@ typedef struct {
   void *stream;          /* as in da_params                                                              */
   void *workspace;       /* attention: distr_attn_paged_workspace_bytes(), 256-byte aligned, for the partial sums of keys that are dealt
                             out: with less of it they go to fewer workgroups, with too little stay together; NULL: a
-                            library-owned buffer as in da_params, or, where there is none to have, keys stay together */
+                            library-owned buffer of 32 MB as in da_params, or, where there is none to have, keys stay
+                            together. A workspace is one call's until the call has ended: calls that may overlap in time, and
+                            graphs that may be replayed so, bring one each */
   size_t workspace_bytes;
 } da_paged;
 

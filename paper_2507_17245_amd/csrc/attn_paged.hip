@@ -2,17 +2,18 @@
 //
 //   O = softmax(scale Q K^T) V over the keys that a row sees, one pass: running maximum and sum of every row.
 //
-// A unit is up to 128 query rows of a sequence and a kv head, all of its query heads together, so that grouped heads share every tile. One workgroup of
-// eight waves per compute unit (its tiles take the LDS), two to a SIMD, one exponentiating while the other multiplies.
-//   more than 32 rows: four wave pairs own 32 rows each, and each wave of a pair walks half of the unit's tiles (64 keys) in buffers
-//     of its half's own. Bound: the matrix products (at d = 64 the exponentials beside them). Loop, layouts, online softmax and
+// A unit is up to 128 query rows of a sequence and a kv head, all of its query heads together, so that grouped heads share every tile; of calls
+// with single tokens up to 32 rows, by a kernel with the second walk alone. Eight waves a compute unit (their tiles take the LDS), two to a
+// SIMD, one exponentiating while the other multiplies, in one workgroup or several (paged_form).
+//   more than 32 rows: waves own 32 rows each, and of eight waves each of a pair with the same rows walks half of the unit's tiles (64 keys)
+//     in buffers of its half's own. Bound: the matrix products (at d = 64 the exponentials beside them). Loop, layouts, online softmax and
 //     the exchange of the halves are those of attn_bf16_impl.h.
-//   up to 32 rows (decoding): every wave has all rows and every eighth tile of 8 KB. Bound: reading the keys and values.
+//   up to 32 rows (decoding): every wave has all rows and tiles of 8 KB in turn. Bound: reading the keys and values.
 // Tiles come 16 keys at a time, which lie in one page, by a scalar base and limit: rows behind the sequence's end, and keys on
 // pages that are none of the cache's, are never read. The page table's entries are held for the tiles ahead, a lane for each, with a bit for
 // those that lie in the cache.
-// Measured, us: 64 sequences of up to 8192 tokens, H32 Hkv8 d64 109 (5.8 TB/s); one of 100003, H16 d128 158 (5.2 TB/s); 2048 tokens on 16384,
-// H32 Hkv8, d64 293 (880 TFLOP/s), d128 514 (1000); two chunks of 250 beside 14 single tokens d128 80.
+// Measured, us: 64 sequences of up to 8192 tokens, H32 Hkv8 d64 107 (5.9 TB/s); one of 100003, H16 d128 144 (5.7 TB/s); 2048 tokens on 16384,
+// H32 Hkv8, d64 289 (890 TFLOP/s), d128 488 (1055); two chunks of 250 beside 14 single tokens d128 78.
 #include <cfloat>
 
 #include "attn_bf16_impl.h"
@@ -24,7 +25,10 @@ namespace da {
 
 namespace {
 
-constexpr int kUnitRows = 128, kTileKeys = 64, kRW = 4;   // rows and keys of the line's units and tiles, waves over the rows
+constexpr int kUnitRows = 128, kFewRows = 32, kTileKeys = 64, kRW = 4;   // rows and keys of the line's units and tiles, waves over the rows
+
+// Places of the line for what beginning and ending a unit takes, in tiles (paged_units.h).
+constexpr int paged_pad(int rows, int waves) { return rows != kFewRows ? 8 : waves == 8 ? 6 : 3; }
 
 // Nothing is known of x from here on: what is computed of it stays where it is used, instead of in registers that the walk has not got.
 __device__ inline int here(int x) {
@@ -69,10 +73,11 @@ struct Places {
   }
 };
 
-// HALVES 2: one workgroup of eight waves a compute unit, for ranges and for units that are fewer than two a compute unit. HALVES 1: two of four, for whole
-// units, one beginning or ending beside the other's walk.
-template <int D, bool STATS, int HALVES>
-__global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
+// ROWS: 128, or 32 for single tokens: without the loop for more rows, whose code and registers are in the way of a short call. WAVES: 8, one
+// workgroup a compute unit; 4 (and 2 with 32 rows): two (four), one beginning or ending its units beside the others' walks.
+// CUT: whether there may be ranges (without, prompts of H16 d128 with row statistics 114 -> 109 us: fewer registers in memory).
+template <int D, bool STATS, int ROWS, int WAVES, bool CUT>
+__global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
     const bf16* __restrict__ q, const bf16* __restrict__ k_pages, const bf16* __restrict__ v_pages, bf16* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int row_bytes, int64_t q_token,
@@ -82,9 +87,9 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
   constexpr int LPG = 16 * ROWB / 1024;   // direct loads of 16 keys
   constexpr float kSumTrigger = (BC / 2) * 256.0f;   // (as in attn_bf16_impl.h)
   // Two tiles of K and V for each half; or, with few rows, one of 8 KB for each wave.
-  constexpr int WAVES = kRW * HALVES, kThreads = WAVES * 64;
+  constexpr int kThreads = WAVES * 64, HALVES = WAVES == 2 * kRW ? 2 : 1;
   constexpr int FEWB = 8192, FT = FEWB / ROWB, BUFB = WAVES / 2 * FEWB;
-  static_assert(HALVES * TILEB <= BUFB, "a buffer holds the halves' tiles");
+  static_assert(ROWS == kFewRows || HALVES * TILEB <= BUFB, "a buffer holds the halves' tiles");
   __shared__ __attribute__((aligned(1024))) char k_lds0[BUFB];
   __shared__ __attribute__((aligned(1024))) char k_lds1[BUFB];
   __shared__ __attribute__((aligned(1024))) char v_lds0[BUFB];
@@ -100,36 +105,36 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
   auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
 
   __shared__ PagedLds line_lds;
-  const PagedLine<kUnitRows, BC> line(batch, &line_lds, wave, WAVES);
+  const PagedLine<ROWS, BC, paged_pad(ROWS, WAVES)> line(batch, &line_lds, wave, WAVES);
   unsigned pos = 0, end = 1;
   int wg = blockIdx.x;
-  if (HALVES == 2 && ranges) {
+  if (CUT && ranges) {
     // Ranges that follow each other on one XCD: their units read the same keys.
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
     const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
     pos = paged_cut(line, wg, length, total);
     end = paged_cut(line, wg + 1, length, total);
-    const PagedCut cut = paged_mark<kUnitRows>(line, pos, end, length, total);
+    const PagedCut cut = paged_mark<ROWS>(line, pos, end, length, total);
     if (tid == 0) cuts[wg] = cut;
   }
   while (pos < end) {
     PagedUnit u;
     int head, t0, t1;
-    if (HALVES == 2 && ranges) {
+    if (CUT && ranges) {
       head = (int)(pos / line.total);
       const unsigned at = pos - (unsigned)head * line.total;
       if (!line.template find<false>(at, &u)) return;
       t0 = (int)(at - u.first);
-      t1 = min(u.tiles, t0 + (int)(end - pos));
+      t1 = min(u.places, t0 + (int)(end - pos));
     } else {
       // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
       head = wg % Hkv;
       if (!line.template find<true>(wg / Hkv, &u)) return;
-      u.m0 = (u.rows - 1) / kUnitRows * kUnitRows - u.m0;
+      u.m0 = (u.rows - 1) / ROWS * ROWS - u.m0;
       t0 = 0;
-      t1 = u.tiles;
+      t1 = u.places;
     }
-    const bool whole = HALVES == 1 || (t0 == 0 && t1 == u.tiles);
+    const bool whole = !CUT || (t0 == 0 && t1 == u.places);
     pos += (unsigned)(t1 - t0);
 
     const int n_keys = min(u.len, batch.max_keys);
@@ -137,13 +142,13 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
     const char* k_base = (const char*)k_pages + head * head_bytes;
     const char* v_base = (const char*)v_pages + head * head_bytes;
     // The unit's rows: up to 128 at once, or 32 from m0 on.
-    bool few = u.rows - u.m0 <= 32;
+    bool few = ROWS == kFewRows || u.rows - u.m0 <= 32;
     for (int m0 = u.m0;;) {
-      const int m1 = min(m0 + (few ? 32 : kUnitRows), u.rows);
+      const int m1 = min(m0 + (few ? 32 : ROWS), u.rows);
       const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (m1 - 1) / group + 1, 0)) : n_keys;   // no row sees more
       const int all_see = causal ? min(max(u.len - u.nq + m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
       if (few) {
-        // ---- few rows: a wave has all of them, and every eighth tile of 8 KB. Bound: reading the keys and values. ----
+        // ---- few rows: a wave has all of them, and every eighth (fourth, second) tile of 8 KB. Bound: reading the keys and values. ----
         // Each wave has a softmax state of its own and no barrier; K of its next tile is asked for when the scores are
         // taken, V when it is multiplied, so that 128 KB a compute unit are on their way most of the time.
         constexpr int GROUPS = FT / 16, FMB = FT / 32, FTT = FT / 16, CPT = FEWB / 1024, WINDOW = 64 / GROUPS;
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
         };
         // Every key is read once. Calls that read more than the caches hold (256 MB) leave them alone: B1 H16 100003 keys d128 171 -> 159 us, 64
         // sequences of 5 on 4096 159 -> 144; smaller ones may find in them what a program read a step ago (14 sequences of 1100-3900 39, 41 so).
-        const bool once = (long long)line.total * Hkv * (2 * TILEB) > 256LL << 20;
+        const bool once = (long long)line.tiles * Hkv * (2 * TILEB) > 256LL << 20;
         // Two windows, the second from the middle of the first on; it takes the first's place when that half is asked for.
         PageWindow now = window_of(tile), next = window_of(tile + WINDOW / 2 * WAVES);
         int at = 0;   // place in the window of the tile that is asked for
@@ -319,7 +324,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
             *(f32x4*)&dst[lq * 64 + (((piece & 15) ^ (lq & 15)) << 2)] = x;
           }
         __syncthreads();
-        const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows + (m0 - u.m0);
+        const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * ROWS + (m0 - u.m0);
         for (int i = tid; i < (m1 - m0) * (D / 4); i += kThreads) {
           const int row = i / (D / 4), piece = i % (D / 4), mr = m0 + row;
           const int at = row * 256 + (((piece & 15) ^ (row & 15)) << 4);
@@ -342,7 +347,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
         }
         __syncthreads();   // (the next tiles take the place of the sums)
         m0 += 32;
-        if (m0 >= min(u.m0 + kUnitRows, u.rows)) break;
+        if (m0 >= min(u.m0 + ROWS, u.rows)) break;
         continue;
       }
       const int lane = here(tid) & 63;
@@ -625,7 +630,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
       float ref = -nref;
       f32x16 out[OB];
       if constexpr (HALVES == 2) {
-        static_assert(kRW * OB * 4096 <= BUFB && WAVES * 512 <= BUFB, "the exchange fits the tile buffers");
+        static_assert(ROWS == kFewRows || (kRW * OB * 4096 <= BUFB && WAVES * 512 <= BUFB), "the exchange fits the tile buffers");
         f32x4* stat = (f32x4*)k_lds0;
         f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
         const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
@@ -666,7 +671,7 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
       const float inv = !whole ? 1.0f : l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
       if (m < u.rows) {
         const int64_t row = (int64_t)token * H + q_of;
-        const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * kUnitRows + rw * 32 + lq;
+        const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * ROWS + rw * 32 + lq;
         if (hh == 0 && half == 0) {
           if (!whole) part_stat[slot] = f32x4{ref, l_tot, e_tot, 0.0f};
           else if (STATS) lse[row] = row_statistic(ref, e_tot);
@@ -687,40 +692,71 @@ __global__ __launch_bounds__(kRW * HALVES * 64, 2) void paged_kernel(
   }
 }
 
-template <int D, int HALVES>
-hipError_t launch_halves(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
-                         const PagedLaunch& l, hipStream_t stream) {
+template <int D, int ROWS, int WAVES, bool CUT>
+hipError_t launch_as(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                     const PagedLaunch& l, hipStream_t stream) {
   const float scale_log2e = scale * 1.4426950408889634f;
-  const PagedScratch at(scratch, l.workgroups, kUnitRows, D);
-  hipLaunchKernelGGL((p.lse_out ? paged_kernel<D, true, HALVES> : paged_kernel<D, false, HALVES>), dim3((unsigned)l.workgroups), dim3(kRW * HALVES * 64), 0,
-                     stream, (const bf16*)q, (const bf16*)k_pages, (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H,
+  const PagedScratch at(scratch, l.workgroups, ROWS, D);
+  hipLaunchKernelGGL((p.lse_out ? paged_kernel<D, true, ROWS, WAVES, CUT> : paged_kernel<D, false, ROWS, WAVES, CUT>), dim3((unsigned)l.workgroups), dim3(WAVES * 64),
+                     0, stream, (const bf16*)q, (const bf16*)k_pages, (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H,
                      p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, p.page_stride * 2, p.head_stride * 2, (int)(p.row_stride * 2),
                      p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, at.sums, at.stats, at.cuts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kUnitRows>), dim3((unsigned)(l.workgroups * (kUnitRows * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, ROWS>), dim3((unsigned)(l.workgroups * (ROWS * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
                      at.cuts, (bf16*)o, p.lse_out, p.H, p.Hkv);
   return hipGetLastError();
+}
+
+// How a call is launched. us:
+//   units of 32 rows for no more new tokens than sequences (units of 128 | of 32, both with eight waves): H32 Hkv8 one of 777 d64 12.8 | 11.5, 32 of up
+//     to 8000 d128 123 | 112. Tokens that are all one sequence's take longer: 250 on 2000 among 256 places 25 | 30, 500 on 4000 among 512 d128 61 | 101.
+//   workgroups of eight, four, two waves by the units that there are at least, so that as many begin at once as compute units hold (eight | four |
+//     two waves; H32 Hkv8 d64): 16 of 8000 42 | 44 | 44, one of 100003 49 | 54 | 61; 48 of up to 1000 23 | 19 | 25; 128 of up to 300 34 | 23 | 18.
+//     With 128 rows eight | four: 1024 on 4096 49 | 59; 64 of 8 new tokens H16 71 | 65.
+//   whole units where the full ones alone are more than compute units (ranges | whole): a prompt of 1400, H32 Hkv8 d64 42 | 26, 1900 on 6000 122 | 105; of
+//     fewer it is not known whether they fill the chip: 1000 on 16000 165 | 200.
+struct PagedForm {
+  int rows, waves;   // of a unit, of a workgroup
+  PagedLaunch launch;
+};
+PagedForm paged_form(const da_paged& p, size_t scratch_bytes) {
+  const int group = p.H / p.Hkv;
+  const long long heads = (long long)p.n_seq * p.Hkv, full = (long long)p.n_tokens * group / kUnitRows * p.Hkv;
+  auto form = [&](int rows, int waves) {
+    return PagedForm{rows, waves, paged_launch(p, rows, kTileKeys, paged_pad(rows, waves), kComputeUnits * 8 / waves, 4, scratch_bytes)};
+  };
+  if (p.n_tokens <= p.n_seq && group <= kFewRows) return form(kFewRows, heads <= kComputeUnits ? 8 : heads <= 2 * kComputeUnits ? 4 : 2);
+  if (full > kComputeUnits) return PagedForm{kUnitRows, 4, PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, 0}};
+  if (heads > kComputeUnits) {
+    const PagedForm f = form(kUnitRows, 4);
+    if (!f.launch.ranges || f.launch.workgroups > kComputeUnits) return f;   // (a smaller scratch: one workgroup a compute unit)
+  }
+  return form(kUnitRows, 8);
+}
+
+template <int D>
+hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
+                    size_t scratch_bytes, hipStream_t stream) {
+  const PagedForm f = paged_form(p, scratch_bytes);
+  const auto launch = f.rows == kFewRows ? (f.waves == 2 ? launch_as<D, kFewRows, 2, true> : f.waves == 4 ? launch_as<D, kFewRows, 4, true> : launch_as<D, kFewRows, 8, true>)
+                      : f.waves == 8     ? launch_as<D, kUnitRows, 8, true>
+                      : f.launch.ranges  ? launch_as<D, kUnitRows, 4, true>
+                                         : launch_as<D, kUnitRows, 4, false>;
+  return launch(q, k_pages, v_pages, o, p, scale, scratch, f.launch, stream);
 }
 
 }  // namespace
 
 size_t paged_scratch_bytes(const da_paged& p) {
-  return p.dtype == DA_F32 ? paged_f32_scratch_bytes(p) : paged_launch_bytes(kComputeUnits, kUnitRows, p.d);
+  return p.dtype == DA_F32 ? paged_f32_scratch_bytes(p) : paged_launch_bytes(2 * kComputeUnits, kUnitRows, p.d);
 }
 
 hipError_t launch_paged(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                         size_t scratch_bytes, hipStream_t stream) {
   if (p.dtype == DA_F32) return launch_paged_f32(q, k_pages, v_pages, o, p, scale, scratch, scratch_bytes, stream);
-  PagedLaunch l = paged_launch(p, kUnitRows, kTileKeys, kComputeUnits, scratch_bytes);
-  const long long units = (long long)p.n_tokens * (p.H / p.Hkv) / kUnitRows * p.Hkv;   // at least
-  const bool many = units >= 2 * kComputeUnits;
-  if (many) l = PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, l.least};
-  if (p.d == 64)
-    return many ? launch_halves<64, 1>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
-                : launch_halves<64, 2>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
-  return many ? launch_halves<128, 1>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
-              : launch_halves<128, 2>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
+  return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, scratch_bytes, stream)
+                   : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, scratch_bytes, stream);
 }
 
 }  // namespace da

@@ -16,7 +16,7 @@ namespace da {
 
 namespace {
 
-constexpr int kWaves = 4, kThreads = kWaves * 64, kRows = 32;
+constexpr int kPad = 3, kWaves = 4, kThreads = kWaves * 64, kRows = 32;
 
 template <int D>
 __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
   const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size};
 
   __shared__ PagedLds line_lds;
-  const PagedLine<kRows, kTile> line(batch, &line_lds, wave, kWaves);
+  const PagedLine<kRows, kTile, kPad> line(batch, &line_lds, wave, kWaves);
   unsigned pos = 0, end = 1;
   if (ranges) {
     const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
@@ -50,14 +50,14 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
       const unsigned at = pos - (unsigned)head * line.total;
       if (!line.template find<false>(at, &u)) return;
       t0 = (int)(at - u.first);
-      t1 = min(u.tiles, t0 + (int)(end - pos));
+      t1 = min(u.places, t0 + (int)(end - pos));
     } else {
       head = blockIdx.x % Hkv;
       if (!line.template find<true>(blockIdx.x / Hkv, &u)) return;
       t0 = 0;
-      t1 = u.tiles;
+      t1 = u.places;
     }
-    const bool whole = t0 == 0 && t1 == u.tiles;
+    const bool whole = t0 == 0 && t1 == u.places;
     pos += (unsigned)(t1 - t0);
 
     const int m = u.m0 + lq, m_ld = min(m, u.rows - 1);
@@ -247,7 +247,7 @@ size_t paged_f32_scratch_bytes(const da_paged& p) { return paged_launch_bytes(re
 
 hipError_t launch_paged_f32(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                             size_t scratch_bytes, hipStream_t stream) {
-  const PagedLaunch l = paged_launch(p, kRows, kTile, resident(p), scratch_bytes);
+  const PagedLaunch l = paged_launch(p, kRows, kTile, kPad, resident(p), kWaves, scratch_bytes);
   return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
                    : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
 }

@@ -5,10 +5,14 @@
 // units and tiles of the sequences, 64 at a time, a lane for each.
 //   whole units   workgroup w takes unit w / Hkv of kv head w % Hkv.
 //   ranges        all tiles, unit after unit and kv head after kv head, are one line, which is cut into equal ranges, one a workgroup:
-//                 each has the same walk whatever the lengths are. A cut less than `snap` tiles from an end of its unit moves
-//                 there (beginning and ending a unit costs as much as several tiles). A unit that cuts fall into is put together by the
+//                 each has the same walk whatever the lengths are. Beginning and ending a unit costs as much as several
+//                 tiles: behind its tiles a unit has PAD places without one, and a cut on them or less than `snap` tiles from
+//                 either end of the tiles moves to the end. A unit that cuts fall into is put together by the
 //                 combine kernel from the sums of its parts: those of the part in front of its first cut, which workgroup w begins
 //                 at, at 2 w, those of a part that begins with workgroup w's cut at 2 w + 1.
+//                 PAD 0 | as it is, us: three chunks of up to 48 on 700, float H8 d64 24.0 | 18.2; decoding H32 Hkv8 d64, 16 sequences of up
+//                 to 2000 25.5 | 19.9, one of 8000 18.6 | 15.6; 60 and one new token each of four of up to 4000, d128 40.7 | 35.7. (One
+//                 prompt of 512 on 4096, whose units half a range fits without, 34.6 | 36.3.) Places spread over the tiles, more snap: 5-20 % more.
 #pragma once
 #include <cfloat>
 
@@ -31,8 +35,8 @@ struct PagedUnit {
   int seq, q0, nq;     // sequence, its first new token and their number
   int len;             // its keys (as told, not cut to the table's room)
   int m0, rows;        // first query row of the unit (token * group + head), rows of the sequence
-  int tiles;           // of the sequence's keys: those that the line counts for the unit
-  unsigned first;      // place of the unit's first tile among a kv head's
+  int places;          // the line's for it: a tile each for the sequence's keys and PAD behind them
+  unsigned first;      // the unit's first place among a kv head's
 };
 
 template <int CTRL, int ROWS>
@@ -50,65 +54,75 @@ __device__ inline unsigned wave_scan(unsigned x) {   // sums over the lanes up t
 
 struct PagedLds {   // of a workgroup
   int seq[7][64];                     // the first 64 sequences
-  unsigned tiles[64], units[64];      // of each 64 sequences, up to 4096 of them
+  unsigned places[64], units[64];     // of each 64 sequences, up to 4096 of them
 };
 
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, int PAD>
 struct PagedSequence {   // what a lane knows of its sequence
-  int q0, nq, len, units, tiles;
-  unsigned sum, unit_sum;   // tiles and units of the sequences up to it, in its 64
+  int q0, nq, len, units, places;   // (places of a unit)
+  unsigned sum, unit_sum;   // places and units of the sequences up to it, in its 64
   __device__ PagedSequence(const PagedBatch& b, int s) {
-    q0 = nq = len = units = tiles = 0;
+    q0 = nq = len = units = places = 0;
     if (s < b.n_seq) {
       const int at = b.q_start[s], to = b.q_start[s + 1], keys = b.kv_len[s];
       q0 = min(max(at, 0), b.n_tokens);
       nq = max(min(max(to, 0), b.n_tokens) - q0, 0);
       len = max(keys, 0);
       units = (int)(((unsigned)nq * (unsigned)b.group + (ROWS - 1)) / ROWS);
-      tiles = max((min(len, b.max_keys) + KEYS - 1) / KEYS, 1);
+      places = max((min(len, b.max_keys) + KEYS - 1) / KEYS, 1) + PAD;
     }
-    sum = wave_scan((unsigned)units * (unsigned)tiles);
+    sum = wave_scan((unsigned)units * (unsigned)places);
     unit_sum = wave_scan((unsigned)units);
   }
   __device__ PagedSequence(const PagedLds* lds, int lane)
-      : q0(lds->seq[0][lane]), nq(lds->seq[1][lane]), len(lds->seq[2][lane]), units(lds->seq[3][lane]), tiles(lds->seq[4][lane]),
+      : q0(lds->seq[0][lane]), nq(lds->seq[1][lane]), len(lds->seq[2][lane]), units(lds->seq[3][lane]), places(lds->seq[4][lane]),
         sum((unsigned)lds->seq[5][lane]), unit_sum((unsigned)lds->seq[6][lane]) {}
   __device__ void store(PagedLds* lds, int lane) const {
-    const int x[7] = {q0, nq, len, units, tiles, (int)sum, (int)unit_sum};
+    const int x[7] = {q0, nq, len, units, places, (int)sum, (int)unit_sum};
 #pragma unroll
     for (int i = 0; i < 7; ++i) lds->seq[i][lane] = x[i];
   }
-  __device__ unsigned all_tiles() const { return (unsigned)__builtin_amdgcn_readlane((int)sum, 63); }
+  __device__ unsigned all_places() const { return (unsigned)__builtin_amdgcn_readlane((int)sum, 63); }
   __device__ unsigned all_units() const { return (unsigned)__builtin_amdgcn_readlane((int)unit_sum, 63); }
 };
 
 // The line of a kv head. The first 64 sequences stay in LDS. Of more, up to 4096, LDS has the sums of each 64, which the waves
 // take a share of, and the 64 that are asked for are loaded again; beyond, the sums are taken again, too.
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, int PAD>
 struct PagedLine {
-  typedef PagedSequence<ROWS, KEYS> Sequence;
+  typedef PagedSequence<ROWS, KEYS, PAD> Sequence;
+  static constexpr unsigned kPad = PAD;
   const PagedBatch b;
   PagedLds* const lds;
-  unsigned total;   // its tiles
+  unsigned total, tiles;   // its places, those of them that are tiles
   // (called by all threads of the workgroup)
   __device__ PagedLine(const PagedBatch& batch, PagedLds* to, int wave, int waves) : b(batch), lds(to) {
     const int lane = threadIdx.x & 63, n = (b.n_seq + 63) / 64;
     const Sequence head(b, lane);
     if (wave == 0) head.store(lds, lane);
-    total = head.all_tiles();
+    total = head.all_places();
+    unsigned units = head.all_units();
     if (n > 64) {
-      for (int c = 1; c < n; ++c) total += Sequence(b, c * 64 + lane).all_tiles();
+      for (int c = 1; c < n; ++c) {
+        const Sequence q(b, c * 64 + lane);
+        total += q.all_places();
+        units += q.all_units();
+      }
     } else if (n > 1) {
       for (int c = wave; c < n; c += waves) {
         const Sequence q(b, c * 64 + lane);
         if (lane == 63) {
-          lds->tiles[c] = q.sum;
+          lds->places[c] = q.sum;
           lds->units[c] = q.unit_sum;
         }
       }
     }
     __syncthreads();
-    if (n > 1 && n <= 64) total = (unsigned)__builtin_amdgcn_readlane((int)wave_scan(lane < n ? lds->tiles[lane] : 0u), 63);
+    if (n > 1 && n <= 64) {
+      total = (unsigned)__builtin_amdgcn_readlane((int)wave_scan(lane < n ? lds->places[lane] : 0u), 63);
+      units = (unsigned)__builtin_amdgcn_readlane((int)wave_scan(lane < n ? lds->units[lane] : 0u), 63);
+    }
+    tiles = total - units * (unsigned)PAD;
   }
   // The unit that holds place `x` (BY_UNIT: the x-th unit); false behind the last one.
   template <bool BY_UNIT>
@@ -116,47 +130,47 @@ struct PagedLine {
     const int lane = threadIdx.x & 63, n = (b.n_seq + 63) / 64;
     if (n == 1) return in<BY_UNIT>(Sequence(lds, lane), 0, x, 0, out);
     if (n <= 64) {
-      const unsigned t = lane < n ? lds->tiles[lane] : 0u, u = lane < n ? lds->units[lane] : 0u, ts = wave_scan(t), us = wave_scan(u);
+      const unsigned t = lane < n ? lds->places[lane] : 0u, u = lane < n ? lds->units[lane] : 0u, ts = wave_scan(t), us = wave_scan(u);
       const uint64_t past = __builtin_amdgcn_ballot_w64((BY_UNIT ? us : ts) > x);
       if (past == 0) return false;
       const int c = __builtin_ctzll(past);
-      const unsigned tiles = (unsigned)__builtin_amdgcn_readlane((int)(ts - t), c), units = (unsigned)__builtin_amdgcn_readlane((int)(us - u), c);
-      return in<BY_UNIT>(Sequence(b, c * 64 + lane), c * 64, x - (BY_UNIT ? units : tiles), tiles, out);
+      const unsigned places = (unsigned)__builtin_amdgcn_readlane((int)(ts - t), c), units = (unsigned)__builtin_amdgcn_readlane((int)(us - u), c);
+      return in<BY_UNIT>(Sequence(b, c * 64 + lane), c * 64, x - (BY_UNIT ? units : places), places, out);
     }
-    unsigned tiles = 0, units = 0;
+    unsigned places = 0, units = 0;
     for (int c = 0; c < n; ++c) {
       const Sequence q(b, c * 64 + lane);
-      if (in<BY_UNIT>(q, c * 64, x - (BY_UNIT ? units : tiles), tiles, out)) return true;
-      tiles += q.all_tiles();
+      if (in<BY_UNIT>(q, c * 64, x - (BY_UNIT ? units : places), places, out)) return true;
+      places += q.all_places();
       units += q.all_units();
     }
     return false;
   }
 
  private:
-  // among 64 sequences from s0 on, with `before` tiles in front of them
+  // among 64 sequences from s0 on, with `before` places in front of them
   template <bool BY_UNIT>
   __device__ bool in(const Sequence& q, int s0, unsigned x, unsigned before, PagedUnit* out) const {
     const uint64_t past = __builtin_amdgcn_ballot_w64((BY_UNIT ? q.unit_sum : q.sum) > x);
     if (past == 0) return false;
     const int i = __builtin_ctzll(past);
     auto of = [&](int v) { return __builtin_amdgcn_readlane(v, i); };
-    const unsigned first = (unsigned)of((int)(q.sum - (unsigned)q.units * (unsigned)q.tiles));
-    const int tiles = of(q.tiles);
-    const int unit = BY_UNIT ? (int)(x - (unsigned)of((int)(q.unit_sum - (unsigned)q.units))) : (int)((x - first) / (unsigned)tiles);
+    const unsigned first = (unsigned)of((int)(q.sum - (unsigned)q.units * (unsigned)q.places));
+    const int places = of(q.places);
+    const int unit = BY_UNIT ? (int)(x - (unsigned)of((int)(q.unit_sum - (unsigned)q.units))) : (int)((x - first) / (unsigned)places);
     out->seq = s0 + i;
     out->q0 = of(q.q0);
     out->nq = of(q.nq);
     out->len = of(q.len);
     out->m0 = unit * ROWS;
     out->rows = out->nq * b.group;
-    out->tiles = tiles;
-    out->first = before + first + (unsigned)unit * (unsigned)tiles;
+    out->places = places;
+    out->first = before + first + (unsigned)unit * (unsigned)places;
     return true;
   }
 };
 
-// (All kv heads' tiles stay below 2^31, by the call's checks.)
+// (All kv heads' places stay below 2^32, by the call's checks: 2e9 tiles and 2.5e8 units of up to 8 places more.)
 // Length of a range: equal ones for `workgroups` of them, none shorter than `least` tiles.
 __device__ inline unsigned paged_range(unsigned total, int workgroups, int least) {
   return max((total + (unsigned)workgroups - 1) / (unsigned)workgroups, (unsigned)least);
@@ -171,7 +185,7 @@ __device__ inline unsigned paged_cut(const LINE& line, unsigned w, unsigned leng
   const unsigned head = at / line.total;
   if (!line.template find<false>(at - head * line.total, &u)) return total;
   const unsigned in = at - head * line.total - u.first, snap = paged_snap(length);
-  return in < snap ? at - in : (unsigned)u.tiles - in < snap ? at - in + (unsigned)u.tiles : at;
+  return in < snap ? at - in : (unsigned)u.places - in < snap + LINE::kPad ? at - in + (unsigned)u.places : at;
 }
 
 // Where the keys of 16 successive places lie: a lane for each such group of a wave's next 64. The group's first row of
@@ -212,7 +226,7 @@ __device__ inline PagedCut paged_mark(const LINE& line, unsigned begin, unsigned
   if (end >= total || !line.template find<false>(end - head * line.total, &u)) return cut;
   const unsigned first = head * line.total + u.first;
   if (first == end || first < begin) return cut;
-  return PagedCut{min(ROWS, u.rows - u.m0), u.q0, u.m0, (int)head, (int)((first + (unsigned)u.tiles - paged_snap(length)) / length), {0, 0, 0}};
+  return PagedCut{min(ROWS, u.rows - u.m0), u.q0, u.m0, (int)head, (int)((first + (unsigned)u.places - LINE::kPad - paged_snap(length)) / length), {0, 0, 0}};
 }
 
 // Units that cuts fall into, from the sums of their parts: a workgroup for every 1024 / D rows that a unit may have, behind every cut. Where
@@ -288,11 +302,11 @@ struct PagedScratch {
     cuts = (PagedCut*)(stats + (size_t)2 * workgroups * rows);
   }
 };
-// `most` workgroups are resident at a time. Ranges, unless no sequence is long enough for two of them, with what fits the scratch.
-inline PagedLaunch paged_launch(const da_paged& p, int rows, int keys, int most, size_t scratch_bytes) {
-  const long long room = ((long long)p.max_pages * p.page_size + keys - 1) / keys;
-  const int least = 4;
-  const int n = (int)std::min((long long)most, (long long)(scratch_bytes / paged_launch_bytes(1, rows, p.d)));
+// `most` workgroups are resident at a time. Ranges of `least` tiles or more, unless no sequence is long enough for two of them, as many as the cache
+// has tiles for and the scratch has room for.
+inline PagedLaunch paged_launch(const da_paged& p, int rows, int keys, int pad, int most, int least, size_t scratch_bytes) {
+  const long long room = ((long long)p.max_pages * p.page_size + keys - 1) / keys, places = (room + pad) * paged_units(p, rows) * p.Hkv;
+  const int n = (int)std::min({(long long)most, (places + least - 1) / least, (long long)(scratch_bytes / paged_launch_bytes(1, rows, p.d))});
   if (n >= 2 && room >= 20) return PagedLaunch{n, 1, least};
   return PagedLaunch{(int)(paged_units(p, rows) * p.Hkv), 0, least};
 }

@@ -136,6 +136,75 @@ def test_prompts_that_fill_the_chip(d):
     _check(b, o, None, causal=False, rows_of=[0, 64, 139, 999])
 
 
+FORMS = [  # sequences, H, Hkv, d, longest, page: kv heads of the sequences beside 256, 512 compute units' worth; ranges and whole units
+    (40, 8, 2, 64, 1500, 16, "heads"),
+    (9, 32, 1, 128, 2300, 64, "tokens"),
+    (100, 8, 4, 64, 1500, 16, "tokens"),
+    (70, 12, 4, 128, 900, 16, "heads"),
+    (100, 8, 4, 128, 1500, 32, "heads"),
+    (150, 8, 4, 64, 1400, 16, "heads"),
+    (150, 4, 4, 128, 1400, 16, "tokens"),
+    (600, 2, 1, 64, 150, 16, "heads"),
+    (300, 64, 2, 64, 100, 16, "heads"),
+]
+
+
+@pytest.mark.parametrize("case", FORMS)
+@pytest.mark.parametrize("workspace", [True, None, 4 << 20])
+def test_single_tokens_of_many_sequences(case, workspace):
+    """One new token each (none for some): workgroups of eight, four and two waves, many units to a range and many ranges to a unit."""
+    n_seq, H, Hkv, d, most, page, order = case
+    g = torch.Generator().manual_seed(n_seq + d)
+    lens = torch.randint(0, most // 2, (n_seq,), generator=g).tolist()
+    lens[1], lens[n_seq // 2], lens[n_seq - 1], lens[3] = most, most - 1, 64, 0
+    new = [1 if n else 0 for n in lens]
+    new[5] = 0
+    b = Batch(lens, new, H, Hkv, d, BF, page=page, order=order, pad_back=1)
+    assert b.T <= n_seq and H // Hkv <= 32
+    only = [0, 1, 2, 3, 4, 5, 6, n_seq // 2, n_seq - 2, n_seq - 1] + list(range(n_seq // 3, n_seq // 3 + 6))
+    o, lse = _attention(b, workspace=workspace)
+    _check(b, o, lse, only=only)
+    assert o[:-1].isfinite().all()
+    plain, _ = _attention(b, workspace=workspace, lse=False, causal=False)
+    _check(b, plain, None, causal=False, only=only)
+
+
+@pytest.mark.parametrize("n_seq,Hkv", [(100, 1), (100, 4), (150, 4)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_prompt_among_places_without_new_tokens(n_seq, Hkv, d):
+    """No more new tokens than sequences, most of them one sequence's: more rows than a unit of single tokens has. A NaN in a value that
+    the last token alone sees reaches it alone."""
+    lens, new = [30] * n_seq, [0] * n_seq
+    lens[7], new[7], lens[50], new[50] = 700, 90, 1300, 1
+    H = 3 * Hkv
+    b, clean = (Batch(lens, new, H, Hkv, d, BF, page=16) for _ in range(2))
+    b.v_pages[int(b.table[7, 699 // 16]), :, 699 % 16, 9] = float("nan")
+    for workspace in (True, 256):
+        o, lse = _attention(b, workspace=workspace)
+        assert o[89, :, 9].isnan().all()
+        o[89, :, 9] = _attention(clean, workspace=workspace)[0][89, :, 9]
+        assert o.isfinite().all()
+        _check(clean, o, lse, only=[7, 50], rows_of=[0, 1, 9, 10, 11, 20, 21, 22, 42, 43, 63, 64, 88, 89])
+
+
+@pytest.mark.parametrize("workspace", [True, None, 3 << 20])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_few_tokens_of_many_sequences(workspace, d):
+    """Up to five new tokens each beside a prompt: ranges for two workgroups a compute unit, for one, and what a small scratch has room for."""
+    g = torch.Generator().manual_seed(d)
+    n_seq, Hkv = 75, 4
+    lens = torch.randint(5, 900, (n_seq,), generator=g).tolist()
+    new = torch.randint(1, 6, (n_seq,), generator=g).tolist()
+    lens[20], new[20], lens[21], lens[74], new[74] = 1500, 150, 1400, 1400, 33
+    b = Batch(lens, new, 8, Hkv, d, BF, page=32, order="tokens")
+    assert n_seq * Hkv > 256
+    o, lse = _attention(b, workspace=workspace)
+    only = [0, 1, 19, 20, 21, 22, 40, 63, 64, 65, 73, 74]
+    _check(b, o, lse, only=only, rows_of=[0, 1, 2, 3, 4, 31, 32, 63, 64, 149])
+    again, lse2 = _attention(b, workspace=workspace)
+    assert torch.equal(o, again) and torch.equal(lse, lse2) and o.isfinite().all()
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("new", [2, 150])
 def test_scores_that_are_no_numbers(new, dtype):

@@ -138,7 +138,7 @@ def test_paged_pointers():
 
 def test_workspace_does_not_depend_on_lengths():
     want = da.distr_attn_paged_workspace_bytes(_paged())
-    assert 0 < want == da.distr_attn_paged_workspace_bytes(_paged(n_seq=1000, max_pages=1 << 16)) <= 32 << 20
+    assert 0 < want == da.distr_attn_paged_workspace_bytes(_paged(n_seq=1000, max_pages=1 << 16)) <= 128 << 20
 
 
 def test_binding_wants_gpu_tensors():
