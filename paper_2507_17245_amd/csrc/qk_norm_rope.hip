@@ -7,6 +7,8 @@
 // keys: the rotation's angles, as many bytes as a bf16 row, are loaded once for all of them, and all their rows are asked
 // for before the first is worked on. Weight gradients are summed over a workgroup's rows in registers and LDS, then over workgroups by
 // a second kernel: no atomics.
+// Measured, us: B1 N4096 H32 Hkv8 d64 bf16 forward 10.5 (42 MB, launch and ramp 2-3 of it); B4 N8192 H16 Hkv16 d128 bf16 forward and gradient 252
+// (5.35 TB/s); N2047 H8 Hkv8 d64 float, a weight a head, 18 (7.0, 8.5 and the weights' sums 2.5); 64 single tokens, a kernel of 3.5.
 #include "paged.h"
 #include "token_rows.h"
 
