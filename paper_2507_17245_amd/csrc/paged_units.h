@@ -226,7 +226,9 @@ __device__ inline PagedCut paged_mark(const LINE& line, unsigned begin, unsigned
   if (end >= total || !line.template find<false>(end - head * line.total, &u)) return cut;
   const unsigned first = head * line.total + u.first;
   if (first == end || first < begin) return cut;
-  return PagedCut{min(ROWS, u.rows - u.m0), u.q0, u.m0, (int)head, (int)((first + (unsigned)u.places - LINE::kPad - paged_snap(length)) / length), {0, 0, 0}};
+  // (starts that do not ascend may count more places than there are: no cut behind the last workgroup's)
+  const unsigned last = min((first + (unsigned)u.places - LINE::kPad - paged_snap(length)) / length, gridDim.x - 1);
+  return PagedCut{min(ROWS, u.rows - u.m0), u.q0, u.m0, (int)head, (int)last, {0, 0, 0}};
 }
 
 // Units that cuts fall into, from the sums of their parts: a workgroup for every 1024 / D rows that a unit may have, behind every cut. Where
