@@ -715,7 +715,10 @@ hipError_t launch_as(const void* q, const void* k_pages, const void* v_pages, vo
 //     two waves; H32 Hkv8 d64): 16 of 8000 42 | 44 | 44, one of 100003 49 | 54 | 61; 48 of up to 1000 23 | 19 | 25; 128 of up to 300 34 | 23 | 18.
 //     With 128 rows eight | four: 1024 on 4096 49 | 59; 64 of 8 new tokens H16 71 | 65.
 //   whole units where the full ones alone are more than compute units (ranges | whole): a prompt of 1400, H32 Hkv8 d64 42 | 26, 1900 on 6000 122 | 105; of
-//     fewer it is not known whether they fill the chip: 1000 on 16000 165 | 200.
+//     fewer it is not known whether they fill the chip: 1000 on 16000 165 | 200. And where the table has no room for more tiles of a sequence than beginning,
+//     ending and joining units take, the more the better the units fill the chip by themselves: single tokens H32 Hkv8 d64 of one sequence of 1200
+//     13.6 | 12.1, 2000 13.0 | 16.2, of 16 of up to 2000 20.1 | 17.4, 4000 25.1 | 25.9; d128 of one of 1000 14.3 | 15.6, 1300 14.3 | 17.2, of 16 of up to
+//     1300 23.0 | 19.9; 60 new of two of 16 of up to 1300 d64 25.0 | 21.0, 3200 31.2 | 34.6.
 struct PagedForm {
   int rows, waves;   // of a unit, of a workgroup
   PagedLaunch launch;
@@ -723,8 +726,10 @@ struct PagedForm {
 PagedForm paged_form(const da_paged& p, size_t scratch_bytes) {
   const int group = p.H / p.Hkv;
   const long long heads = (long long)p.n_seq * p.Hkv, full = (long long)p.n_tokens * group / kUnitRows * p.Hkv;
+  const int units = (int)std::min(std::max(heads, full), (long long)kComputeUnits);   // that there are at least
   auto form = [&](int rows, int waves) {
-    return PagedForm{rows, waves, paged_launch(p, rows, kTileKeys, paged_pad(rows, waves), kComputeUnits * 8 / waves, 4, scratch_bytes)};
+    const int from = rows == kUnitRows ? 16 + units / 6 : p.d == 64 ? 20 + std::min(units, kComputeUnits / 2) / 4 : 12 + std::min(units, kComputeUnits / 2) / 6;
+    return PagedForm{rows, waves, paged_launch(p, rows, kTileKeys, paged_pad(rows, waves), kComputeUnits * 8 / waves, from, scratch_bytes)};
   };
   if (p.n_tokens <= p.n_seq && group <= kFewRows) return form(kFewRows, heads <= kComputeUnits ? 8 : heads <= 2 * kComputeUnits ? 4 : 2);
   if (full > kComputeUnits) return PagedForm{kUnitRows, 4, PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, 0}};

@@ -248,7 +248,11 @@ size_t paged_f32_scratch_bytes(const da_paged& p) { return paged_launch_bytes(re
 
 hipError_t launch_paged_f32(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                             size_t scratch_bytes, hipStream_t stream) {
-  const PagedLaunch l = paged_launch(p, kRows, kTile, kPad, resident(p), kWaves, scratch_bytes);
+  // Ranges where the table has room for more tiles than a workgroup takes in two rounds (one at d = 128), and the more the better units fill the chip by
+  // themselves (units whole | ranges, us): H8 Hkv8 d64 one of 300 17.0 | 14.7, 600 24.4 | 14.8, 40 tokens each of 16 of up to 400 22.8 | 31.1, 620 28.6 |
+  // 36.5; d128 one of 150 21.5 | 18.5, of 600 44.6 | 19.7.
+  const int from = (p.d == 64 ? 8 : 5) + (int)std::min(paged_units(p, kRows) * p.Hkv, (long long)kComputeUnits) / 16;
+  const PagedLaunch l = paged_launch(p, kRows, kTile, kPad, resident(p), from, scratch_bytes);
   return p.d == 64 ? launch_d<64>(q, k_pages, v_pages, o, p, scale, scratch, l, stream)
                    : launch_d<128>(q, k_pages, v_pages, o, p, scale, scratch, l, stream);
 }

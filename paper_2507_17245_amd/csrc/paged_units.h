@@ -304,12 +304,13 @@ struct PagedScratch {
     cuts = (PagedCut*)(stats + (size_t)2 * workgroups * rows);
   }
 };
-// `most` workgroups are resident at a time. Ranges of `least` tiles or more, unless no sequence is long enough for two of them, as many as the cache
-// has tiles for and the scratch has room for.
-inline PagedLaunch paged_launch(const da_paged& p, int rows, int keys, int pad, int most, int least, size_t scratch_bytes) {
+// `most` workgroups are resident at a time. Ranges of `least` places or more, as many as there are places in all and the scratch has room for, where
+// the table has room for `from` tiles of a sequence.
+inline PagedLaunch paged_launch(const da_paged& p, int rows, int keys, int pad, int most, int from, size_t scratch_bytes) {
+  constexpr int least = 4;
   const long long room = ((long long)p.max_pages * p.page_size + keys - 1) / keys, places = (room + pad) * paged_units(p, rows) * p.Hkv;
   const int n = (int)std::min({(long long)most, (places + least - 1) / least, (long long)(scratch_bytes / paged_launch_bytes(1, rows, p.d))});
-  if (n >= 2 && room >= 20) return PagedLaunch{n, 1, least};
+  if (n >= 2 && room >= from) return PagedLaunch{n, 1, least};
   return PagedLaunch{(int)(paged_units(p, rows) * p.Hkv), 0, least};
 }
 

@@ -10,6 +10,10 @@ pytestmark = pytest.mark.gpu
 BF, F = torch.bfloat16, torch.float32
 
 
+# Tokens that a row of the page table has room for beyond the longest sequence: with few the units of a call stay whole, with many they go by ranges.
+ROOMY = [0, 5000]
+
+
 def _attention(b, causal=True, scale=None, lse=True, workspace=True, q=None):
     """-> o, lse of one call on the batch; o is NaN where nothing is written"""
     q = b.dev["q"] if q is None else q
@@ -65,9 +69,10 @@ RAGGED = [  # lens, new, H, Hkv, d, page, order
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("case", RAGGED)
-def test_ragged_batches(case, dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_ragged_batches(case, dtype, roomy):
     lens, new, H, Hkv, d, page, order = case
-    b = Batch(lens, new, H, Hkv, d, dtype, page=page, order=order, pad_front=1, pad_back=2, room=1)
+    b = Batch(lens, new, H, Hkv, d, dtype, page=page, order=order, pad_front=1, pad_back=2, room=1 + roomy // page)
     some = [0, 1, 2, 3, 7, 8, 30, 31, 32, 33, 63, 64, 69, 127, 128, 129, 149, 199, 259]
     for causal in (True, False):
         o, lse = _attention(b, causal=causal)
@@ -99,25 +104,27 @@ def test_without_row_statistics(dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("n_seq", [63, 64, 65, 200])
-def test_many_sequences(n_seq, dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_many_sequences(n_seq, dtype, roomy):
     g = torch.Generator().manual_seed(n_seq)
     lens = torch.randint(0, 120, (n_seq,), generator=g).tolist()
     new = [min(int(x), n) for x, n in zip(torch.randint(0, 4, (n_seq,), generator=g), lens)]
-    b = Batch(lens, new, 4, 2, 64, dtype, pad_back=1)
+    b = Batch(lens, new, 4, 2, 64, dtype, pad_back=1, room=roomy // 16)
     o, lse = _attention(b)
     _check(b, o, lse)
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("n_seq", [300, 4096, 4200])
-def test_very_many_sequences(n_seq, dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_very_many_sequences(n_seq, dtype, roomy):
     """More than a wave's lanes of them, and more than the sums of 64 that a workgroup keeps; with and without ranges."""
     g = torch.Generator().manual_seed(n_seq)
     lens = torch.randint(0, 40, (n_seq,), generator=g).tolist()
     lens[n_seq - 2] = 1500
     new = [min(int(x), n) for x, n in zip(torch.randint(0, 3, (n_seq,), generator=g), lens)]
     new[n_seq - 2], new[70] = 33, 0
-    b = Batch(lens, new, 2, 1, 64, dtype)
+    b = Batch(lens, new, 2, 1, 64, dtype, room=roomy // 16)
     only = [0, 1, 63, 64, 65, 69, 70, 71, 127, 128, 255, 256, n_seq - 3, n_seq - 2, n_seq - 1] + list(range(200, 210))
     for workspace in (True, 256):
         o, lse = _attention(b, workspace=workspace)
@@ -151,7 +158,8 @@ FORMS = [  # sequences, H, Hkv, d, longest, page: kv heads of the sequences besi
 
 @pytest.mark.parametrize("case", FORMS)
 @pytest.mark.parametrize("workspace", [True, None, 4 << 20])
-def test_single_tokens_of_many_sequences(case, workspace):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_single_tokens_of_many_sequences(case, workspace, roomy):
     """One new token each (none for some): workgroups of eight, four and two waves, many units to a range and many ranges to a unit."""
     n_seq, H, Hkv, d, most, page, order = case
     g = torch.Generator().manual_seed(n_seq + d)
@@ -159,7 +167,7 @@ def test_single_tokens_of_many_sequences(case, workspace):
     lens[1], lens[n_seq // 2], lens[n_seq - 1], lens[3] = most, most - 1, 64, 0
     new = [1 if n else 0 for n in lens]
     new[5] = 0
-    b = Batch(lens, new, H, Hkv, d, BF, page=page, order=order, pad_back=1)
+    b = Batch(lens, new, H, Hkv, d, BF, page=page, order=order, pad_back=1, room=roomy // page)
     assert b.T <= n_seq and H // Hkv <= 32
     only = [0, 1, 2, 3, 4, 5, 6, n_seq // 2, n_seq - 2, n_seq - 1] + list(range(n_seq // 3, n_seq // 3 + 6))
     o, lse = _attention(b, workspace=workspace)
@@ -171,13 +179,14 @@ def test_single_tokens_of_many_sequences(case, workspace):
 
 @pytest.mark.parametrize("n_seq,Hkv", [(100, 1), (100, 4), (150, 4)])
 @pytest.mark.parametrize("d", [64, 128])
-def test_a_prompt_among_places_without_new_tokens(n_seq, Hkv, d):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_a_prompt_among_places_without_new_tokens(n_seq, Hkv, d, roomy):
     """No more new tokens than sequences, most of them one sequence's: more rows than a unit of single tokens has. A NaN in a value that
     the last token alone sees reaches it alone."""
     lens, new = [30] * n_seq, [0] * n_seq
     lens[7], new[7], lens[50], new[50] = 700, 90, 1300, 1
     H = 3 * Hkv
-    b, clean = (Batch(lens, new, H, Hkv, d, BF, page=16) for _ in range(2))
+    b, clean = (Batch(lens, new, H, Hkv, d, BF, page=16, room=roomy // 16) for _ in range(2))
     b.v_pages[int(b.table[7, 699 // 16]), :, 699 % 16, 9] = float("nan")
     for workspace in (True, 256):
         o, lse = _attention(b, workspace=workspace)
@@ -189,14 +198,15 @@ def test_a_prompt_among_places_without_new_tokens(n_seq, Hkv, d):
 
 @pytest.mark.parametrize("workspace", [True, None, 3 << 20])
 @pytest.mark.parametrize("d", [64, 128])
-def test_a_few_tokens_of_many_sequences(workspace, d):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_a_few_tokens_of_many_sequences(workspace, d, roomy):
     """Up to five new tokens each beside a prompt: ranges for two workgroups a compute unit, for one, and what a small scratch has room for."""
     g = torch.Generator().manual_seed(d)
     n_seq, Hkv = 75, 4
     lens = torch.randint(5, 900, (n_seq,), generator=g).tolist()
     new = torch.randint(1, 6, (n_seq,), generator=g).tolist()
     lens[20], new[20], lens[21], lens[74], new[74] = 1500, 150, 1400, 1400, 33
-    b = Batch(lens, new, 8, Hkv, d, BF, page=32, order="tokens")
+    b = Batch(lens, new, 8, Hkv, d, BF, page=32, order="tokens", room=roomy // 32)
     assert n_seq * Hkv > 256
     o, lse = _attention(b, workspace=workspace)
     only = [0, 1, 19, 20, 21, 22, 40, 63, 64, 65, 73, 74]
@@ -207,10 +217,11 @@ def test_a_few_tokens_of_many_sequences(workspace, d):
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("new", [2, 150])
-def test_scores_that_are_no_numbers(new, dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_scores_that_are_no_numbers(new, dtype, roomy):
     """A NaN or an infinity in one query row, and in one key, reaches the rows of its scores and no others."""
     n = new + 90
-    b, clean = (Batch([n], [new], 4, 2, 64, dtype) for _ in range(2))
+    b, clean = (Batch([n], [new], 4, 2, 64, dtype, room=roomy // 16) for _ in range(2))
     b.dev["q"][1, 2, 7] = float("nan")
     place = n - 1                                    # a key that the last token alone sees
     b.k_pages[int(b.table[0, place // 16]), 1, place % 16, 3] = float("inf")
@@ -233,10 +244,11 @@ def test_scores_that_are_no_numbers(new, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("new", [1, 40, 200])
-def test_rows_that_see_no_key(new, dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_rows_that_see_no_key(new, dtype, roomy):
     """More new tokens than the sequence has tokens: the first see nothing. A length of none: no row sees any."""
     lens, fresh = [max(new - 7, 0), 0, 50], [new, 2, 1]
-    b = Batch(lens, fresh, 4, 2, 64, dtype, room=2)
+    b = Batch(lens, fresh, 4, 2, 64, dtype, room=2 + roomy // 16)
     o, lse = _attention(b)
     _check(b, o, lse, rows_of=[0, 1, 5, 6, 7, 8, 30, 32, 39, 40, 150, 199])
     assert (o[new:new + 2] == 0).all() and (lse[new:new + 2] == -float("inf")).all()
@@ -244,9 +256,10 @@ def test_rows_that_see_no_key(new, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("new", [1, 140])
-def test_pages_that_are_none_of_the_cache(new, dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_pages_that_are_none_of_the_cache(new, dtype, roomy):
     lens = [400, 90, 16]
-    b = Batch(lens, [new, 1, 1], 4, 1, 64, dtype, page=16)
+    b = Batch(lens, [new, 1, 1], 4, 1, 64, dtype, page=16, room=roomy // 16)
     n_pages = b.k_pages.shape[0]
     seen = [[True] * n for n in lens]
     for s, i, value in ((0, 3, -1), (0, 7, n_pages), (0, 24, 2 ** 31 - 1), (1, 0, -2 ** 31), (2, 0, n_pages + 5)):
@@ -277,16 +290,17 @@ def test_lengths_beyond_the_table_and_starts_out_of_order(dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("new", [1, 100, 300])
-def test_values_that_later_tokens_alone_see(new, dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_values_that_later_tokens_alone_see(new, dtype, roomy):
     """An infinity or a NaN in a value (and a key) reaches the rows that see it and no others."""
-    b = Batch([new + 70], [new], 4, 2, 64, dtype)
+    b = Batch([new + 70], [new], 4, 2, 64, dtype, room=roomy // 16)
     last, mid = new + 69, 70 + new // 2
     for place, what in ((last, float("nan")), (mid, float("inf"))):
         page, row = int(b.table[0, place // 16]), place % 16
         b.v_pages[page, :, row, 5] = what
         b.values[0][:, place, 5] = what
     o, lse = _attention(b)
-    clean = Batch([new + 70], [new], 4, 2, 64, dtype)
+    clean = Batch([new + 70], [new], 4, 2, 64, dtype, room=roomy // 16)
     oc, lc = _attention(clean)
     # What they do not reach is what it would be without them, to the bounds of any call (rows with such values may be summed in another order).
     rest = o.clone()
@@ -301,9 +315,10 @@ def test_values_that_later_tokens_alone_see(new, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
-def test_large_scores(dtype):
+@pytest.mark.parametrize("roomy", ROOMY)
+def test_large_scores(dtype, roomy):
     """Scores of thousands: one key takes a row's whole weight."""
-    b = Batch([600, 40], [5, 40], 4, 2, 64, dtype, scale=1000.0)
+    b = Batch([600, 40], [5, 40], 4, 2, 64, dtype, scale=1000.0, room=roomy // 16)
     o, lse = _attention(b)
     _check(b, o, lse)
     o, lse = _attention(b, scale=1e-3)
