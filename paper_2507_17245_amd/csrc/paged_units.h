@@ -10,7 +10,7 @@
 //                 either end of the tiles moves to the end. A unit that cuts fall into is put together by the
 //                 combine kernel from the sums of its parts: those of the part in front of its first cut, which workgroup w begins
 //                 at, at 2 w, those of a part that begins with workgroup w's cut at 2 w + 1.
-//                 PAD 0 | as it is, us: three chunks of up to 48 on 700, float H8 d64 24.0 | 18.2; decoding H32 Hkv8 d64, 16 sequences of up
+//                 PAD 0 | as it is (ranges, us): three chunks of up to 48 on 700, float H8 d64 24.0 | 18.2; decoding H32 Hkv8 d64, 16 sequences of up
 //                 to 2000 25.5 | 19.9, one of 8000 18.6 | 15.6; 60 and one new token each of four of up to 4000, d128 40.7 | 35.7. (One
 //                 prompt of 512 on 4096, whose units half a range fits without, 34.6 | 36.3.) Places spread over the tiles, more snap: 5-20 % more.
 #pragma once
