@@ -665,6 +665,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
             for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]);
           }
       } else {
+        if (l_tot == 0.0f) ref = -FLT_MAX;   // (as above, for the unit's other parts: a row that saw nothing has no reference)
 #pragma unroll
         for (int mb = 0; mb < OB; ++mb) out[mb] = oacc[mb];
       }
