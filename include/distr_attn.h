@@ -70,7 +70,8 @@ typedef struct {
   float softmax_scale;  /* multiplies S before softmax; 0 means 1/sqrt(d)                           */
   int gray_mode;        /* Gray map of the sign word (Sec. 3.2): 0 = position of the word in the Gray
                            sequence, 1 = Gray code of the word                                     */
-  void *stream;         /* hipStream_t; NULL = the stream set by distr_attn_set_stream (default: null stream) */
+  void *stream;         /* hipStream_t; NULL = the stream set by distr_attn_set_stream (default: null stream);
+                           hipStreamLegacy = the null stream, whatever is set                        */
   void *workspace;      /* device scratch of >= distr_attn_workspace_bytes(), 256-byte aligned; NULL =
                            library-owned, one per device, grown on demand (hipMalloc on first use /
                            growth; outgrown buffers are kept until distr_attn_release; growing
@@ -328,7 +329,7 @@ int distr_attn_cache_append(const void *k, const void *v, void *k_pages, void *v
 int distr_attn_paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *o, const da_paged *p);
 size_t distr_attn_paged_workspace_bytes(const da_paged *p);
 
-/* Stream used when da_params.stream is NULL and by the short-form entry points (process-wide). */
+/* Stream used when the stream of a call's parameters is NULL and by the short-form entry points (process-wide). */
 int distr_attn_set_stream(void *hip_stream);
 
 /* Frees the library-owned device workspace (synchronises the device first). */

@@ -348,6 +348,7 @@ def distr_attn_version():
 # ---- around attention: norms and rotation of queries and keys, a cache in pages --------------------------
 
 ROPE = {"none": 0, "halves": 1, "neighbours": 2}
+NULL_STREAM = 1   # hipStreamLegacy: the null stream itself, not what a short form or a program has set for calls without one
 
 
 def _at(t):
@@ -417,7 +418,7 @@ def _fill_workspace(p, workspace, device):
     _check_buffer(workspace, "workspace", 0)
     if workspace is not None:
         p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    p.stream = _current_stream().value
+    p.stream = _current_stream().value or NULL_STREAM
     import torch
     p.device, p.current_device = device.index, torch.cuda.current_device
 
@@ -460,10 +461,7 @@ def _run(name, params, *args):
     """The call, on the stream and the device that params were made for."""
     if params.current_device() != params.device:
         raise ValueError(f"params were made for cuda:{params.device}, the current device is cuda:{params.current_device()}")
-    L = _lib or lib()
-    if params.stream is None:      # (the null stream: not what a short form has set since)
-        L.distr_attn_set_stream(None)
-    _check(getattr(L, name)(*args, ctypes.byref(params)))
+    _check(getattr(_lib or lib(), name)(*args, ctypes.byref(params)))
 
 
 def _check_qk(params, tensors):

@@ -81,6 +81,12 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
+// The stream of a call's parameters. hipStreamLegacy names the null stream whatever is set.
+hipStream_t stream_of(void* stream) {
+  const hipStream_t s = (hipStream_t)(stream ? stream : g_stream.load());
+  return s == hipStreamLegacy ? nullptr : s;
+}
+
 struct Resolved {
   da::Problem pb;
   int dtype;
@@ -138,7 +144,7 @@ int resolve(const da_params* p, bool need_groups, Resolved* out) {
   out->dtype = p->dtype;
   out->Tq = (p->N + p->Br - 1) / p->Br;
   out->Tk_side = (Nk + p->Bc - 1) / p->Bc;
-  out->stream = (hipStream_t)(p->stream ? p->stream : g_stream.load());
+  out->stream = stream_of(p->stream);
   return DA_OK;
 }
 
@@ -470,8 +476,6 @@ int attention_bwd(const void* q, const void* k, const void* v, const void* o, co
 }
 
 // ---- around attention: norms and rotation, paged cache ------------------------------------------------
-
-hipStream_t stream_of(void* stream) { return (hipStream_t)(stream ? stream : g_stream.load()); }
 
 int check_shape(int d, int dtype) {
   if (dtype != DA_BF16 && dtype != DA_F32) return fail(DA_ERR_INVALID_ARG, "unknown dtype %d", dtype);
