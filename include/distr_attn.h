@@ -285,7 +285,8 @@ size_t distr_attn_qk_bwd_workspace_bytes(const da_qk *p);
  * the rows of q, k, v and o, one sequence after the other: rows q_start[s] .. q_start[s + 1] - 1 are the last ones of sequence
  * s. Rows before q_start[0] and from q_start[n_seq] on belong to none and are left as they are. The three index arrays are read on the
  * device, at the time of the call's kernels (a captured call sees what they hold at each replay): what they hold is not
- * checked by the call, but no access leaves the buffers whatever it is. Lengths count up to max_pages * page_size; pages
+ * checked by the call, but no access leaves the buffers whatever it is (starts that do not ascend leave rows of o unwritten, or
+ * rows of which it is not known whose they are). Lengths count up to max_pages * page_size; pages
  * outside the cache hold nothing: a token whose page is none of 0 .. n_pages - 1 is not stored, and keys of such a page are
  * not seen.
  */

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
     const bf16* __restrict__ q, const bf16* __restrict__ k_pages, const bf16* __restrict__ v_pages, bf16* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int row_bytes, int64_t q_token,
-    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat, PagedCut* __restrict__ cuts) {
+    int64_t q_head, int causal, float scale_log2e, int ranges, int least, unsigned most, float* __restrict__ part_o, f32x4* __restrict__ part_stat, PagedCut* __restrict__ cuts) {
   constexpr int BC = kTileKeys, ROWB = D * 2, TILEB = BC * ROWB;
   constexpr int MB = BC / 32, TT = BC / 16, KSTEPS = D / 16, NMB = D / 32;
   constexpr int LPG = 16 * ROWB / 1024;   // direct loads of 16 keys
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % kRW, half = HALVES == 1 ? 0 : wave / kRW;
   const int group = H / Hkv;
-  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size};
+  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size, most};
   auto k_buf = [&](int par) -> char* { return (par ? k_lds1 : k_lds0) + half * TILEB; };
   auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
 
@@ -701,7 +701,7 @@ hipError_t launch_as(const void* q, const void* k_pages, const void* v_pages, vo
   hipLaunchKernelGGL((p.lse_out ? paged_kernel<D, true, ROWS, WAVES, CUT> : paged_kernel<D, false, ROWS, WAVES, CUT>), dim3((unsigned)l.workgroups), dim3(WAVES * 64),
                      0, stream, (const bf16*)q, (const bf16*)k_pages, (const bf16*)v_pages, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H,
                      p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, p.page_stride * 2, p.head_stride * 2, (int)(p.row_stride * 2),
-                     p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, at.sums, at.stats, at.cuts);
+                     p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, l.most, at.sums, at.stats, at.cuts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
   hipLaunchKernelGGL((paged_combine_kernel<bf16, D, ROWS>), dim3((unsigned)(l.workgroups * (ROWS * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
@@ -733,7 +733,7 @@ PagedForm paged_form(const da_paged& p, size_t scratch_bytes) {
     return PagedForm{rows, waves, paged_launch(p, rows, kTileKeys, paged_pad(rows, waves), kComputeUnits * 8 / waves, from, scratch_bytes)};
   };
   if (p.n_tokens <= p.n_seq && group <= kFewRows) return form(kFewRows, heads <= kComputeUnits ? 8 : heads <= 2 * kComputeUnits ? 4 : 2);
-  if (full > kComputeUnits) return PagedForm{kUnitRows, 4, PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, 0}};
+  if (full > kComputeUnits) return PagedForm{kUnitRows, 4, PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, 0, 0}};
   if (heads > kComputeUnits) {
     const PagedForm f = form(kUnitRows, 4);
     if (!f.launch.ranges || f.launch.workgroups > kComputeUnits) return f;   // (a smaller scratch: one workgroup a compute unit)

@@ -24,14 +24,14 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void paged_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_pages, const float* __restrict__ v_pages, float* __restrict__ o,
     const int* __restrict__ page_table, const int* __restrict__ q_start, const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv,
     int n_seq, int n_tokens, int n_pages, int page_size, int max_pages, int64_t page_bytes, int64_t head_bytes, int64_t row_bytes, int64_t q_token,
-    int64_t q_head, int causal, float scale_log2e, int ranges, int least, float* __restrict__ part_o, f32x4* __restrict__ part_stat, PagedCut* __restrict__ cuts) {
+    int64_t q_head, int causal, float scale_log2e, int ranges, int least, unsigned most, float* __restrict__ part_o, f32x4* __restrict__ part_stat, PagedCut* __restrict__ cuts) {
   constexpr int NMB = D / 32, HALF = D / 2;
   __shared__ __attribute__((aligned(16))) float sums[kWaves][kRows][D + 4];
   __shared__ f32x2 stat_lds[kWaves][kRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, hh = lane >> 5;
   const int group = H / Hkv;
-  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size};
+  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size, most};
 
   __shared__ PagedLds line_lds;
   const PagedLine<kRows, kTile, kPad> line(batch, &line_lds, wave, kWaves);
@@ -231,7 +231,7 @@ hipError_t launch_d(const void* q, const void* k_pages, const void* v_pages, voi
   hipLaunchKernelGGL((paged_f32_kernel<D>), dim3((unsigned)l.workgroups), dim3(kThreads), 0, stream, (const float*)q, (const float*)k_pages,
                      (const float*)v_pages, (float*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.n_pages,
                      p.page_size, p.max_pages, p.page_stride * 4, p.head_stride * 4, p.row_stride * 4, p.q_stride[0], p.q_stride[1], p.causal,
-                     scale_log2e, l.ranges, l.least, at.sums, at.stats, at.cuts);
+                     scale_log2e, l.ranges, l.least, l.most, at.sums, at.stats, at.cuts);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
   hipLaunchKernelGGL((paged_combine_kernel<float, D, kRows>), dim3((unsigned)(l.workgroups * (kRows * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,

@@ -29,6 +29,7 @@ struct PagedBatch {
   int n_seq, n_tokens;
   int group;       // query heads of a kv head
   int max_keys;    // that a row of the page table has room for
+  unsigned most;   // places of a kv head's line that starts in ascending order may make
 };
 
 struct PagedUnit {
@@ -50,6 +51,11 @@ __device__ inline unsigned wave_scan(unsigned x) {   // sums over the lanes up t
   x = dpp_add<0x118, 0xf>(x);
   x = dpp_add<0x142, 0xa>(x);   // row_bcast 15: a row's last lane to the next row
   return dpp_add<0x143, 0xc>(x);   // row_bcast 31: the second row's last lane to the upper two
+}
+
+// The sum of all lanes' x, given wave_scan(x); the largest number where it is beyond 32 bits.
+__device__ inline unsigned wave_total(unsigned x, unsigned scan) {
+  return __builtin_amdgcn_ballot_w64(scan < x) == 0 ? (unsigned)__builtin_amdgcn_readlane((int)scan, 63) : ~0u;
 }
 
 struct PagedLds {   // of a workgroup
@@ -82,12 +88,14 @@ struct PagedSequence {   // what a lane knows of its sequence
 #pragma unroll
     for (int i = 0; i < 7; ++i) lds->seq[i][lane] = x[i];
   }
-  __device__ unsigned all_places() const { return (unsigned)__builtin_amdgcn_readlane((int)sum, 63); }
+  __device__ unsigned all_places() const { return wave_total((unsigned)units * (unsigned)places, sum); }
   __device__ unsigned all_units() const { return (unsigned)__builtin_amdgcn_readlane((int)unit_sum, 63); }
 };
 
 // The line of a kv head. The first 64 sequences stay in LDS. Of more, up to 4096, LDS has the sums of each 64, which the waves
 // take a share of, and the 64 that are asked for are loaded again; beyond, the sums are taken again, too.
+// Starts out of order may count the same tokens many times, more than 32 bits hold and than the parts of units have scratch for: sums stay at the
+// largest number then, and a line of more places than ascending starts can make is taken as empty (no range has work).
 template <int ROWS, int KEYS, int PAD>
 struct PagedLine {
   typedef PagedSequence<ROWS, KEYS, PAD> Sequence;
@@ -105,24 +113,28 @@ struct PagedLine {
     if (n > 64) {
       for (int c = 1; c < n; ++c) {
         const Sequence q(b, c * 64 + lane);
-        total += q.all_places();
+        const unsigned more = q.all_places();
+        total = total + more < more ? ~0u : total + more;
         units += q.all_units();
       }
     } else if (n > 1) {
       for (int c = wave; c < n; c += waves) {
         const Sequence q(b, c * 64 + lane);
+        const unsigned all = q.all_places();
         if (lane == 63) {
-          lds->places[c] = q.sum;
+          lds->places[c] = all;
           lds->units[c] = q.unit_sum;
         }
       }
     }
     __syncthreads();
     if (n > 1 && n <= 64) {
-      total = (unsigned)__builtin_amdgcn_readlane((int)wave_scan(lane < n ? lds->places[lane] : 0u), 63);
+      const unsigned all = lane < n ? lds->places[lane] : 0u;
+      total = wave_total(all, wave_scan(all));
       units = (unsigned)__builtin_amdgcn_readlane((int)wave_scan(lane < n ? lds->units[lane] : 0u), 63);
     }
     tiles = total - units * (unsigned)PAD;
+    if (total > b.most) total = 0;
   }
   // The unit that holds place `x` (BY_UNIT: the x-th unit); false behind the last one.
   template <bool BY_UNIT>
@@ -222,12 +234,12 @@ template <int ROWS, typename LINE>
 __device__ inline PagedCut paged_mark(const LINE& line, unsigned begin, unsigned end, unsigned length, unsigned total) {
   PagedCut cut = {0, 0, 0, 0, 0, {0, 0, 0}};
   PagedUnit u;
+  if (end >= total) return cut;
   const unsigned head = end / line.total;
-  if (end >= total || !line.template find<false>(end - head * line.total, &u)) return cut;
+  if (!line.template find<false>(end - head * line.total, &u)) return cut;
   const unsigned first = head * line.total + u.first;
   if (first == end || first < begin) return cut;
-  // (starts that do not ascend may count more places than there are: no cut behind the last workgroup's)
-  const unsigned last = min((first + (unsigned)u.places - LINE::kPad - paged_snap(length)) / length, gridDim.x - 1);
+  const unsigned last = (first + (unsigned)u.places - LINE::kPad - paged_snap(length)) / length;   // (in front of the line's end, which the last range has)
   return PagedCut{min(ROWS, u.rows - u.m0), u.q0, u.m0, (int)head, (int)last, {0, 0, 0}};
 }
 
@@ -289,6 +301,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(
 // How a call is launched: units dealt out whole, or ranges with sums of their parts in scratch.
 struct PagedLaunch {
   int workgroups, ranges, least;
+  unsigned most;   // places of a kv head's line
 };
 // (no more units than this, whatever the sequences' shares of the tokens are)
 inline long long paged_units(const da_paged& p, int rows) { return (long long)p.n_tokens * (p.H / p.Hkv) / rows + std::min(p.n_seq, p.n_tokens); }
@@ -308,10 +321,10 @@ struct PagedScratch {
 // the table has room for `from` tiles of a sequence.
 inline PagedLaunch paged_launch(const da_paged& p, int rows, int keys, int pad, int most, int from, size_t scratch_bytes) {
   constexpr int least = 4;
-  const long long room = ((long long)p.max_pages * p.page_size + keys - 1) / keys, places = (room + pad) * paged_units(p, rows) * p.Hkv;
+  const long long room = ((long long)p.max_pages * p.page_size + keys - 1) / keys, line = (room + pad) * paged_units(p, rows), places = line * p.Hkv;
   const int n = (int)std::min({(long long)most, (places + least - 1) / least, (long long)(scratch_bytes / paged_launch_bytes(1, rows, p.d))});
-  if (n >= 2 && room >= from) return PagedLaunch{n, 1, least};
-  return PagedLaunch{(int)(paged_units(p, rows) * p.Hkv), 0, least};
+  if (n >= 2 && room >= from) return PagedLaunch{n, 1, least, (unsigned)line};
+  return PagedLaunch{(int)(paged_units(p, rows) * p.Hkv), 0, least, (unsigned)line};
 }
 
 }  // namespace
