@@ -269,8 +269,8 @@ int distr_attn_qk_norm_rope(const void *q, const void *k, void *q_out, void *k_o
 /*
  * Its gradient. q, k: the forward's inputs (read with norm = 1 alone, null else allowed); dq_out, dk_out: gradients of the loss with
  * respect to its outputs. Written: dq, dk, in the types and strides of q and k (dq may be dq_out where the strides are the
- * same, dk likewise), and, where not null, dq_weight ([d] or [H][d]) and dk_weight ([d] or [Hkv][d]), float: the sums over
- * all rows that a weight scales (norm = 1 alone). No atomics: results are the same on every run. With a weight gradient the call
+ * same, dk likewise; otherwise neither may overlap an input or the other), and, where not null, dq_weight ([d] or [H][d]) and
+ * dk_weight ([d] or [Hkv][d]; not dq_weight's place), float: the sums over all rows that a weight scales (norm = 1 alone). No atomics: results are the same on every run. With a weight gradient the call
  * needs distr_attn_qk_bwd_workspace_bytes(p) of scratch, found as in da_params.
  */
 int distr_attn_qk_norm_rope_bwd(const void *q, const void *k, const void *dq_out, const void *dk_out, void *dq, void *dk,

@@ -726,7 +726,9 @@ int distr_attn_qk_norm_rope_bwd(const void* q, const void* k, const void* dq_out
     return fail(DA_ERR_INVALID_ARG, "q, k must be non-null and 16-byte aligned where norm = 1");
   if (!norm && (dq_weight || dk_weight)) return fail(DA_ERR_INVALID_ARG, "weight gradients without a norm");
   if (((uintptr_t)dq_weight & 3u) != 0 || ((uintptr_t)dk_weight & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "dq_weight, dk_weight must be 4-byte aligned");
-  if (dq == q || dq == dk || dq == dk_out || (keys && (dk == k || dk == dq_out))) return fail(DA_ERR_INVALID_ARG, "dq and dk must not alias q, k or each other's gradients");
+  if (dq == q || dq == k || dq == dk || dq == dk_out || (keys && (dk == q || dk == k || dk == dq_out)))
+    return fail(DA_ERR_INVALID_ARG, "dq and dk must not alias q, k or each other's gradients");
+  if (dq_weight && dq_weight == dk_weight) return fail(DA_ERR_INVALID_ARG, "dq_weight and dk_weight must not alias");
   const int nq[] = {p->B, p->H, p->N}, nk[] = {p->B, p->Hkv, p->N};
   rc = check_in_place(dq_out, dq, p->q_out_stride, p->q_stride, nq, "dq");
   if (!rc && keys) rc = check_in_place(dk_out, dk, p->k_out_stride, p->k_stride, nk, "dk");
