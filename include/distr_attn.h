@@ -308,7 +308,7 @@ typedef struct {
   void *stream;          /* as in da_params                                                              */
   void *workspace;       /* attention: distr_attn_paged_workspace_bytes(), 256-byte aligned, for the partial sums of keys that are dealt
                             out: with less of it they go to fewer workgroups, with too little stay together; NULL: a
-                            library-owned buffer of 32 MB as in da_params, or, where there is none to have, keys stay
+                            library-owned buffer of 32 MB as in da_params (less than the full amount at d = 128), or, where there is none to have, keys stay
                             together. A workspace is one call's until the call has ended: calls that may overlap in time, and
                             graphs that may be replayed so, bring one each */
   size_t workspace_bytes;

@@ -6,7 +6,9 @@
 // acc_row(i, 0 / 1) in step i of the second, where P already is, with channels r * d / 32 + mb as row r of block mb (a lane takes consecutive
 // ones of a row of V). Bound: the float products, 1/16 of the bf16 rate; V of a tile is asked for before its scores are taken and K of
 // the next one behind them. Operands do not pass through LDS.
-// Measured, us: three chunks of up to 48 on up to 700, H8 d64 17.1 (latency: 13, and the combine kernel's 4.2); 100 tokens on 2000, H16 Hkv4 d128 53.
+// Measured, us: three chunks of up to 48 on up to 700, H8 d64 17.1 (latency: 13, and the combine kernel's 4.2); 100 tokens on 2000, H16 Hkv4 d128 53;
+// 16 chunks of 40 on up to 2000, H8 d64 61 (28 % of the products' rate: each unit reads the keys again, K one tile ahead); 64 single tokens of up to
+// 8192, H32 Hkv8 d64 339 (3.7 TB/s).
 #include <cfloat>
 
 #include "f32_tiles.h"

@@ -3,7 +3,7 @@
 // Bound: reading k and v and writing their places once. Lanes are dealt to (token, head) pairs, heads fastest: a wave's
 // reads are one run of k and of v, and lanes of one token load the same angles. A token finds its sequence by counting the starts up
 // to its wave's first token, 64 at a time, then its place, its page and the row in it.
-// Measured, us: five prompts of up to 4096, Hkv16 d128 bf16 27.7 (5.4 TB/s); 64 single tokens, a kernel of 4.2 (that chain of loads).
+// Measured, us: five prompts of up to 4096, Hkv16 d128 bf16 27.7 (5.4 TB/s), float 62 (4.7 TB/s); 64 single tokens, a kernel of 4.2 (that chain of loads).
 #include "paged.h"
 #include "token_rows.h"
 
