@@ -256,7 +256,7 @@ int run() {
     std::vector<int> fresh;
     int T = 0;
     for (int s = 0; s < n_seq; ++s) {
-      fresh.push_back(in(0, 3) == 0 ? in(0, most_new) : 1);
+      fresh.push_back(n_seq > 1000 && in(0, 20) ? 0 : in(0, 3) == 0 ? in(0, most_new) : 1);
       T += fresh.back();
     }
     Batch b = make(8, 2, 64, n_seq, T + 3, 16, n_seq > 1000 ? 40 : 300);
