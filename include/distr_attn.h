@@ -330,6 +330,46 @@ int distr_attn_cache_append(const void *k, const void *v, void *k_pages, void *v
 int distr_attn_paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *o, const da_paged *p);
 size_t distr_attn_paged_workspace_bytes(const da_paged *p);
 
+/*
+ * The same cache held in 4 bits: 32 consecutive channels of a key or value share a scale byte e (the scale is 2^(e - 127); 255: the 32 are
+ * NaN), and each has a code of 4 bits: the sign above the number of one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, by which the scale is
+ * multiplied. Codes are [n_pages][Hkv][page_size][d / 2] bytes (channel 2 j in the low bits of byte j), scales
+ * [n_pages][Hkv][page_size][d / 32] bytes, both by strides in bytes.
+ */
+typedef struct {
+  void *k_codes, *k_scales, *v_codes, *v_scales;  /* device; codes 16-byte aligned, scales 4-byte aligned, none another's place */
+  int64_t code_stride[3];   /* of a page, a head and a row of k_codes and v_codes: multiples of 16, rows at least d / 2 apart  */
+  int64_t scale_stride[3];  /* of k_scales and v_scales: multiples of d / 32, at least d / 32                               */
+} da_cache4;
+
+/*
+ * The calls below take the sequences, the page table and the new tokens as da_paged gives them; its page_stride, head_stride and row_stride
+ * are not read, its dtype is that of q, k, v and o. What it says of the index arrays, of absent pages, streams and workspaces holds
+ * here, too.
+ *
+ * append: k and v ([n_tokens][Hkv][d] by strides) into the cache, the keys normed and rotated on the way if p->rotary says so. The scale of 32 channels
+ * is the smallest from 2^-126 to 2^125 that leaves none beyond 7 times it (the largest where there is none), or 255 where one is an infinity or a
+ * NaN; a channel goes to the nearest value, at the same distance from two to the one of the even code, beyond 6 to 6. Norm and
+ * rotation are taken in 64 bits where 32 leave a code in doubt: the codes are those of the exact rows. Places that two tokens
+ * share receive either of them, channels of one beside the other's.
+ */
+int distr_attn_cache4_append(const void *k, const void *v, const da_cache4 *cache, const da_paged *p);
+
+/*
+ * The way back: rows q_start[s] .. q_start[s + 1] - 1 of k and v ([n_tokens][Hkv][d] by strides, at least d) receive what the cache holds of the last
+ * tokens of sequence s (all of them where there are kv_len[s]). Values are exact in either dtype, but for what exceeds its range (infinite) or falls below it. Rows of
+ * tokens that have no place in the cache are left as they are.
+ */
+int distr_attn_cache4_read(void *k, void *v, const da_cache4 *cache, const da_paged *p);
+
+/*
+ * distr_attn_paged_fwd over it. q, o, lse_out, causal, softmax_scale as there. bf16: matrix cores, keys and values as bf16 (exact), P rounded to
+ * bf16, sums in float; float tensors: float arithmetic. A key of NaN makes the rows that see it NaN, a value's 32 channels of
+ * NaN those of the rows that see it.
+ */
+int distr_attn_paged4_fwd(const void *q, void *o, const da_cache4 *cache, const da_paged *p);
+size_t distr_attn_paged4_workspace_bytes(const da_paged *p);
+
 /* Stream used when the stream of a call's parameters is NULL and by the short-form entry points (process-wide). */
 int distr_attn_set_stream(void *hip_stream);
 

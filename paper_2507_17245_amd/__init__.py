@@ -22,6 +22,7 @@ EXPORTS = (
     "distr_attn_workspace_bytes", "distr_attn_bwd_workspace_bytes", "distr_attn_hyperplanes",
     "distr_attn_qk_norm_rope", "distr_attn_qk_norm_rope_bwd", "distr_attn_qk_bwd_workspace_bytes",
     "distr_attn_cache_append", "distr_attn_paged_fwd", "distr_attn_paged_workspace_bytes",
+    "distr_attn_cache4_append", "distr_attn_cache4_read", "distr_attn_paged4_fwd", "distr_attn_paged4_workspace_bytes",
     "distr_attn_set_stream", "distr_attn_release", "distr_attn_last_error", "distr_attn_version",
 )
 
@@ -74,6 +75,14 @@ class DaPaged(ctypes.Structure):
     ]
 
 
+class DaCache4(ctypes.Structure):
+    """Mirror of da_cache4."""
+    _fields_ = [
+        ("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+        ("code_stride", ctypes.c_int64 * 3), ("scale_stride", ctypes.c_int64 * 3),
+    ]
+
+
 class DistrAttnError(RuntimeError):
     def __init__(self, code, message):
         super().__init__(f"distr_attn error {code}: {message}")
@@ -107,7 +116,10 @@ def lib():
         L.distr_attn_qk_norm_rope_bwd.argtypes = [vp] * 8 + [ctypes.POINTER(DaQk)]
         for name in ("distr_attn_cache_append", "distr_attn_paged_fwd"):
             getattr(L, name).argtypes = [vp] * 4 + [ctypes.POINTER(DaPaged)]
-        for name, params in (("distr_attn_qk_bwd_workspace_bytes", DaQk), ("distr_attn_paged_workspace_bytes", DaPaged)):
+        for name in ("distr_attn_cache4_append", "distr_attn_cache4_read", "distr_attn_paged4_fwd"):
+            getattr(L, name).argtypes = [vp, vp, ctypes.POINTER(DaCache4), ctypes.POINTER(DaPaged)]
+        for name, params in (("distr_attn_qk_bwd_workspace_bytes", DaQk), ("distr_attn_paged_workspace_bytes", DaPaged),
+                             ("distr_attn_paged4_workspace_bytes", DaPaged)):
             getattr(L, name).argtypes = [ctypes.POINTER(params)]
             getattr(L, name).restype = ctypes.c_size_t
         L.distr_attn_hyperplanes.argtypes = [u64, ci, ci, ctypes.POINTER(ctypes.c_float)]
@@ -511,29 +523,40 @@ def make_paged_params(k_pages, v_pages, page_table, kv_len, q_start, q=None, k=N
     the next step's into them and calls again. norm, rope and the rest: of the keys on their way into the cache, as in make_qk_params (positions
     int32 [tokens]; None: a token's place in its sequence). lse_out: float32 [tokens, H]. workspace: of
     distr_attn_paged_workspace_bytes, which a captured call needs for the keys of a row to be dealt out to several workgroups."""
-    import torch
     if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or _strides(k_pages, "k_pages") != _strides(v_pages, "v_pages"):
         raise ValueError("k_pages and v_pages must be [pages, Hkv, page size, d] of the same strides")
-    n_pages, Hkv, page_size, d = k_pages.shape
+    if any(t is not None and t.dtype != k_pages.dtype for t in (v_pages, q, k, v)):
+        raise TypeError("q, k, v and the pages must share a dtype")
+    p = _paged_params(k_pages.shape, (k_pages, v_pages), page_table, kv_len, q_start, q, k, v, causal, softmax_scale, lse_out, norm, eps, k_weight,
+                      rope, cos, sin, positions, workspace)
+    p.page_stride, p.head_stride, p.row_stride = _strides(k_pages, "k_pages")
+    p.layouts["pages"] = _layout(k_pages)
+    return p
+
+
+def _paged_params(shape, cache, page_table, kv_len, q_start, q, k, v, causal, softmax_scale, lse_out, norm, eps, k_weight, rope, cos, sin, positions,
+                  workspace):
+    """What calls over pages of `shape` [pages, Hkv, page size, d] share: all but the pages' strides. cache: its tensors."""
+    import torch
+    n_pages, Hkv, page_size, d = shape
     new = [t for t in (q, k, v) if t is not None]
     if not new or (k is None) != (v is None):
         raise ValueError("q, or k and v, must be given")
     if any(t.dim() != 3 or t.shape[2] != d or t.shape[0] != new[0].shape[0] for t in new) or any(t.shape[1] != Hkv for t in (k, v) if t is not None):
         raise ValueError("q must be [tokens, H, d]; k, v [tokens, Hkv, d]")
-    if any(t.dtype != k_pages.dtype for t in (v_pages, *new)):
-        raise TypeError("q, k, v and the pages must share a dtype")
+    if any(t.dtype != new[0].dtype for t in new):
+        raise TypeError("q, k, v must share a dtype")
     if page_table.dim() != 2 or kv_len.dim() != 1:
         raise ValueError("page_table must be [sequences, pages], kv_len [sequences]")
-    _check_device(k_pages.device, v_pages, page_table, kv_len, q_start, *new, lse_out, k_weight, cos, sin, positions, workspace)
+    _check_device(cache[0].device, *cache[1:], page_table, kv_len, q_start, *new, lse_out, k_weight, cos, sin, positions, workspace)
     n_seq, n_tokens = kv_len.shape[0], new[0].shape[0]
     _check_index(page_table, (n_seq, page_table.shape[1]), "page_table")
     _check_index(kv_len, (n_seq,), "kv_len")
     _check_index(q_start, (n_seq + 1,), "q_start")
     p = DaPaged()
-    p.H, p.Hkv, p.d, p.dtype = q.shape[1] if q is not None else Hkv, Hkv, d, _dtype_code(k_pages)
+    p.H, p.Hkv, p.d, p.dtype = q.shape[1] if q is not None else Hkv, Hkv, d, _dtype_code(new[0])
     p.n_seq, p.n_tokens = n_seq, n_tokens
     p.n_pages, p.page_size, p.max_pages = n_pages, page_size, page_table.shape[1]
-    p.page_stride, p.head_stride, p.row_stride = _strides(k_pages, "k_pages")
     p.page_table, p.kv_len, p.q_start = page_table.data_ptr(), kv_len.data_ptr(), q_start.data_ptr()
     for t, field in ((q, p.q_stride), (k, p.k_stride), (v, p.v_stride)):
         if t is not None:
@@ -547,8 +570,8 @@ def make_paged_params(k_pages, v_pages, page_table, kv_len, q_start, q=None, k=N
         if lse_out.dtype != torch.float32 or q is None or tuple(lse_out.shape) != tuple(q.shape[:2]) or not lse_out.is_contiguous():
             raise ValueError("lse_out must be contiguous float32 [tokens, H]")
         p.lse_out = lse_out.data_ptr()
-    _fill_workspace(p, workspace, k_pages.device)
-    p.layouts = {"pages": _layout(k_pages), "q": q if q is None else _layout(q), "k": k if k is None else _layout(k), "v": v if v is None else _layout(v)}
+    _fill_workspace(p, workspace, cache[0].device)
+    p.layouts = {"q": q if q is None else _layout(q), "k": k if k is None else _layout(k), "v": v if v is None else _layout(v)}
     p.held = (page_table, kv_len, q_start, lse_out, k_weight, cos, sin, positions, workspace)
     return p
 
@@ -584,3 +607,72 @@ def distr_attn_paged_fwd(q, k_pages, v_pages, o, params):
 
 def distr_attn_paged_workspace_bytes(params):
     return int(lib().distr_attn_paged_workspace_bytes(ctypes.byref(params)))
+
+
+def make_paged4_params(cache, page_table, kv_len, q_start, q=None, k=None, v=None, causal=True, softmax_scale=0.0, lse_out=None, norm=False,
+                       eps=1e-6, k_weight=None, rope="none", cos=None, sin=None, positions=None, workspace=None):
+    """Parameters of distr_attn_cache4_append and distr_attn_cache4_read (k, v given) and distr_attn_paged4_fwd (q given) for a batch of
+    sequences in one cache held in 4 bits: cache = (k_codes, k_scales, v_codes, v_scales), uint8, codes [pages, Hkv, page size, d / 2] with channel
+    2 j in the low bits of byte j, scales [pages, Hkv, page size, d / 32]: 2^(byte - 127) for 32 channels. Any strides with contiguous
+    rows, the same for keys and values. The rest as in make_paged_params; workspace of distr_attn_paged4_workspace_bytes."""
+    import torch
+    k_codes, k_scales, v_codes, v_scales = cache
+    for a, b, what in ((k_codes, v_codes, "codes"), (k_scales, v_scales, "scales")):
+        if a.dim() != 4 or a.shape != b.shape or _strides(a, what) != _strides(b, what):
+            raise ValueError(f"{what} of keys and values must be [pages, Hkv, page size, channels] of the same strides")
+        if a.dtype != torch.uint8 or b.dtype != torch.uint8:
+            raise TypeError(f"{what} must be uint8")
+    d = 2 * k_codes.shape[3]
+    if d % 32 != 0 or k_scales.shape != (*k_codes.shape[:3], d // 32):
+        raise ValueError("scales must be [pages, Hkv, page size, d / 32]")
+    p = _paged_params((*k_codes.shape[:3], d), cache, page_table, kv_len, q_start, q, k, v, causal, softmax_scale, lse_out, norm, eps, k_weight,
+                      rope, cos, sin, positions, workspace)
+    p.layouts["cache"] = (_layout(k_codes), _layout(k_scales))
+    p.strides = (_strides(k_codes, "codes"), _strides(k_scales, "scales"))
+    return p
+
+
+def _cache4(cache, params):
+    """The cache as the library takes it: its tensors are those of the call, the layout is that of params."""
+    k_codes, k_scales, v_codes, v_scales = cache
+    codes, scales = params.layouts["cache"]
+    if _layout(k_codes) != codes or _layout(v_codes) != codes or _layout(k_scales) != scales or _layout(v_scales) != scales:
+        raise ValueError("params were made for a cache of another shape, stride or device")
+    c = DaCache4(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
+    c.code_stride[:], c.scale_stride[:] = params.strides
+    return c
+
+
+def _run_cache4(name, params, k, v, cache):
+    if params.layouts["k"] is None:
+        raise ValueError("params were made without k and v")
+    _check_layout(k, params.layouts["k"], "k")
+    _check_layout(v, params.layouts["v"], "v")
+    _run(name, params, _at(k), _at(v), ctypes.byref(_cache4(cache, params)))
+
+
+def distr_attn_cache4_append(k, v, cache, params):
+    """The new tokens' keys (normed and rotated on the way if params say so) and values into the cache, in 4 bits. -> cache"""
+    _run_cache4("distr_attn_cache4_append", params, k, v, cache)
+    return cache
+
+
+def distr_attn_cache4_read(k, v, cache, params):
+    """What the cache holds of the sequences' last tokens, q_start[s + 1] - q_start[s] of sequence s, into k and v [tokens, Hkv, d]. -> (k, v)"""
+    _run_cache4("distr_attn_cache4_read", params, k, v, cache)
+    return k, v
+
+
+def distr_attn_paged4_fwd(q, cache, o, params):
+    """Exact attention of the new tokens over the cache, their own keys in it: o [tokens, H, d], contiguous."""
+    if params.layouts["q"] is None:
+        raise ValueError("params were made without q")
+    _check_layout(q, params.layouts["q"], "q")
+    if o.shape != q.shape or o.dtype != q.dtype or o.device != q.device or not o.is_contiguous():
+        raise ValueError("o must be contiguous, of q's shape and dtype, on its device")
+    _run("distr_attn_paged4_fwd", params, _at(q), _at(o), ctypes.byref(_cache4(cache, params)))
+    return o
+
+
+def distr_attn_paged4_workspace_bytes(params):
+    return int(lib().distr_attn_paged4_workspace_bytes(ctypes.byref(params)))

@@ -562,7 +562,8 @@ int check_in_place(const void* in, const void* out, const int64_t* in_stride, co
   return DA_OK;
 }
 
-int check_paged(const da_paged* p) {
+// What a call over pages says of its sequences. rows: of the smallest unit of the kernels.
+int check_batch(const da_paged* p, int rows) {
   if (!p) return fail(DA_ERR_INVALID_ARG, "params is null");
   int rc = check_shape(p->d, p->dtype);
   if (rc) return rc;
@@ -571,22 +572,80 @@ int check_paged(const da_paged* p) {
   if (p->n_pages <= 0 || p->page_size <= 0 || p->max_pages <= 0) return fail(DA_ERR_INVALID_ARG, "n_pages, page_size, max_pages must be positive");
   if (p->page_size % 16 != 0) return fail(DA_ERR_UNSUPPORTED, "page_size = %d: pages of a multiple of 16 tokens", p->page_size);
   if ((long long)p->max_pages * p->page_size > 1LL << 30) return fail(DA_ERR_UNSUPPORTED, "more than 2^30 tokens in a row of page_table");
-  const int sizes[] = {p->n_pages, p->Hkv, p->page_size};
-  const int64_t strides[] = {p->page_stride, p->head_stride, p->row_stride};
-  rc = check_strides(strides, sizes, 3, p->d, p->dtype, true, "k_pages and v_pages");
-  if (rc) return rc;
-  if (p->row_stride > 1 << 25) return fail(DA_ERR_UNSUPPORTED, "row_stride of more than 2^25 elements");
   if (!p->page_table || !p->kv_len || !p->q_start) return fail(DA_ERR_INVALID_ARG, "page_table, kv_len, q_start must be non-null");
   if ((((uintptr_t)p->page_table | (uintptr_t)p->kv_len | (uintptr_t)p->q_start) & 3u) != 0)
     return fail(DA_ERR_INVALID_ARG, "page_table, kv_len, q_start must be 4-byte aligned");
-  const int keys = 32, rows = 32;   // the smallest tile and unit of the kernels
+  const int keys = 32;   // the smallest tile of the kernels
   const double units = (double)p->n_tokens * (p->H / p->Hkv) / rows + p->n_seq;
   if (units * ((double)p->max_pages * p->page_size / keys + 1) * p->Hkv > 2e9 || units * p->Hkv * 16 > 4e9 || (double)p->n_tokens * p->H > 2e9)
     return fail(DA_ERR_UNSUPPORTED, "too many rows and keys for one call");
   return DA_OK;
 }
 
+int check_paged(const da_paged* p) {
+  int rc = check_batch(p, 32);
+  if (rc) return rc;
+  const int sizes[] = {p->n_pages, p->Hkv, p->page_size};
+  const int64_t strides[] = {p->page_stride, p->head_stride, p->row_stride};
+  rc = check_strides(strides, sizes, 3, p->d, p->dtype, true, "k_pages and v_pages");
+  if (rc) return rc;
+  if (p->row_stride > 1 << 25) return fail(DA_ERR_UNSUPPORTED, "row_stride of more than 2^25 elements");
+  return DA_OK;
+}
+
+int check_batch4(const da_paged* p) { return check_batch(p, 16); }
+
+int check_cache4(const da_cache4* c, const da_paged* p) {
+  if (!c) return fail(DA_ERR_INVALID_ARG, "cache is null");
+  void* const at[] = {c->k_codes, c->v_codes, c->k_scales, c->v_scales};
+  for (int i = 0; i < 4; ++i) {
+    if (!at[i] || ((uintptr_t)at[i] & (i < 2 ? 15u : 3u)) != 0)
+      return fail(DA_ERR_INVALID_ARG, "codes must be non-null and 16-byte, scales 4-byte aligned");
+    for (int j = 0; j < i; ++j)
+      if (at[i] == at[j]) return fail(DA_ERR_INVALID_ARG, "codes and scales of keys and values must not alias each other");
+  }
+  const int sizes[] = {p->n_pages, p->Hkv, p->page_size};
+  const int64_t row = p->d / 2, groups = p->d / 32;
+  for (int i = 0; i < 3; ++i) {
+    if (sizes[i] <= 1) continue;   // (never taken)
+    if (c->code_stride[i] < row || c->code_stride[i] % 16 != 0 || c->code_stride[i] > (int64_t)1 << 40)
+      return fail(DA_ERR_INVALID_ARG, "strides of codes must be multiples of 16 bytes, at least d / 2");
+    if (c->scale_stride[i] < groups || c->scale_stride[i] % groups != 0 || c->scale_stride[i] > (int64_t)1 << 40)
+      return fail(DA_ERR_INVALID_ARG, "strides of scales must be multiples of d / 32 bytes");
+  }
+  if (c->code_stride[2] > 1 << 25 || c->scale_stride[2] > 1 << 25) return fail(DA_ERR_UNSUPPORTED, "rows of codes or scales more than 2^25 bytes apart");
+  return DA_OK;
+}
+
+bool in_cache4(const void* x, const da_cache4* c) { return x == c->k_codes || x == c->k_scales || x == c->v_codes || x == c->v_scales; }
+
 float paged_scale(const da_paged* p) { return p->softmax_scale == 0.0f ? 1.0f / std::sqrt((float)p->d) : p->softmax_scale; }
+
+// Attention over pages: what is left to check, scratch, and launch(scale, scratch, its bytes, stream).
+template <typename LAUNCH>
+int attend_pages(const void* q, void* o, bool aliased, size_t want, const da_paged* p, const char* what, LAUNCH launch) {
+  if (p->causal != 0 && p->causal != 1) return fail(DA_ERR_INVALID_ARG, "causal must be 0 or 1");
+  const float scale = paged_scale(p);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(DA_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
+  if (p->n_tokens == 0) return DA_OK;
+  if (!q || !o || !aligned16(q) || !aligned16(o)) return fail(DA_ERR_INVALID_ARG, "q, o must be non-null and 16-byte aligned");
+  if (o == q || aliased) return fail(DA_ERR_INVALID_ARG, "o must not alias an input");
+  const int sizes[] = {p->n_tokens, p->H};
+  int rc = check_strides(p->q_stride, sizes, 2, p->d, p->dtype, false, "q");
+  if (rc) return rc;
+  if (((uintptr_t)p->lse_out & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
+  if (p->workspace && ((uintptr_t)p->workspace & 255u) != 0) return fail(DA_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  const hipStream_t stream = stream_of(p->stream);
+  void* scratch = p->workspace;
+  size_t bytes = scratch ? p->workspace_bytes : 0;
+  ShareLease lease;
+  if (!scratch && want) {
+    lease.take(stream);
+    scratch = lease.ptr;
+    bytes = scratch ? kShareBytes : 0;
+  }
+  return check_launch(launch(scale, scratch, std::min(bytes, want), stream), what, stream);
+}
 
 da_params short_form(int B, int H, int Hkv, int N, int d, int Br, int Bc, int n_groups, uint64_t seed, int causal) {
   da_params p = {};
@@ -782,28 +841,55 @@ size_t distr_attn_paged_workspace_bytes(const da_paged* p) {
 int distr_attn_paged_fwd(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged* p) {
   int rc = check_paged(p);
   if (rc) return rc;
-  if (p->causal != 0 && p->causal != 1) return fail(DA_ERR_INVALID_ARG, "causal must be 0 or 1");
-  const float scale = paged_scale(p);
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(DA_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
+  if (p->n_tokens != 0 && (!k_pages || !v_pages || !aligned16(k_pages) || !aligned16(v_pages)))
+    return fail(DA_ERR_INVALID_ARG, "k_pages, v_pages must be non-null and 16-byte aligned");
+  return attend_pages(q, o, o == k_pages || o == v_pages, da::paged_scratch_bytes(*p), p, "paged attention launch",
+                      [&](float scale, void* scratch, size_t bytes, hipStream_t stream) { return da::launch_paged(q, k_pages, v_pages, o, *p, scale, scratch, bytes, stream); });
+}
+
+int distr_attn_cache4_append(const void* k, const void* v, const da_cache4* cache, const da_paged* p) {
+  int rc = check_batch4(p);
+  if (!rc) rc = check_rotary(p->rotary, p->d);
+  if (!rc) rc = check_cache4(cache, p);
+  if (rc) return rc;
   if (p->n_tokens == 0) return DA_OK;
-  rc = check_tensors(q, k_pages, v_pages, o);
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(DA_ERR_INVALID_ARG, "k, v must be non-null and 16-byte aligned");
+  if (in_cache4(k, cache) || in_cache4(v, cache)) return fail(DA_ERR_INVALID_ARG, "the cache must not alias an input");
+  if (((uintptr_t)p->positions & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+  const int sizes[] = {p->n_tokens, p->Hkv};
+  rc = check_strides(p->k_stride, sizes, 2, p->d, p->dtype, false, "k");
+  if (!rc) rc = check_strides(p->v_stride, sizes, 2, p->d, p->dtype, false, "v");
   if (rc) return rc;
-  const int sizes[] = {p->n_tokens, p->H};
-  rc = check_strides(p->q_stride, sizes, 2, p->d, p->dtype, false, "q");
-  if (rc) return rc;
-  if (((uintptr_t)p->lse_out & 3u) != 0) return fail(DA_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
-  if (p->workspace && ((uintptr_t)p->workspace & 255u) != 0) return fail(DA_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   const hipStream_t stream = stream_of(p->stream);
-  void* scratch = p->workspace;
-  size_t bytes = scratch ? p->workspace_bytes : 0;
-  const size_t want = da::paged_scratch_bytes(*p);
-  ShareLease lease;
-  if (!scratch && want) {
-    lease.take(stream);
-    scratch = lease.ptr;
-    bytes = scratch ? kShareBytes : 0;
-  }
-  return check_launch(da::launch_paged(q, k_pages, v_pages, o, *p, scale, scratch, std::min(bytes, want), stream), "paged attention launch", stream);
+  return check_launch(da::launch_cache4_append(k, v, *cache, *p, stream), "4-bit cache append launch", stream);
+}
+
+int distr_attn_cache4_read(void* k, void* v, const da_cache4* cache, const da_paged* p) {
+  int rc = check_batch4(p);
+  if (!rc) rc = check_cache4(cache, p);
+  if (rc) return rc;
+  if (p->n_tokens == 0) return DA_OK;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(DA_ERR_INVALID_ARG, "k, v must be non-null and 16-byte aligned");
+  if (k == v || in_cache4(k, cache) || in_cache4(v, cache)) return fail(DA_ERR_INVALID_ARG, "k and v must not alias the cache or each other");
+  const int sizes[] = {p->n_tokens, p->Hkv};
+  rc = check_strides(p->k_stride, sizes, 2, p->d, p->dtype, true, "k");
+  if (!rc) rc = check_strides(p->v_stride, sizes, 2, p->d, p->dtype, true, "v");
+  if (rc) return rc;
+  const hipStream_t stream = stream_of(p->stream);
+  return check_launch(da::launch_cache4_read(k, v, *cache, *p, stream), "4-bit cache read launch", stream);
+}
+
+size_t distr_attn_paged4_workspace_bytes(const da_paged* p) {
+  if (check_batch4(p)) return 0;
+  return da::paged4_scratch_bytes(*p);
+}
+
+int distr_attn_paged4_fwd(const void* q, void* o, const da_cache4* cache, const da_paged* p) {
+  int rc = check_batch4(p);
+  if (!rc) rc = check_cache4(cache, p);
+  if (rc) return rc;
+  return attend_pages(q, o, in_cache4(o, cache), da::paged4_scratch_bytes(*p), p, "4-bit paged attention launch",
+                      [&](float scale, void* scratch, size_t bytes, hipStream_t stream) { return da::launch_paged4(q, o, *cache, *p, scale, scratch, bytes, stream); });
 }
 
 int distr_attn_set_stream(void* hip_stream) {

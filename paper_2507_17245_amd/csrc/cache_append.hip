@@ -32,26 +32,8 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(
   vl.template load<ONCE>(vp + at.lo);
   vh.template load<ONCE>(vp + at.hi);
 
-  // sequences that begin at or before the wave's first token
-  const int first = __builtin_amdgcn_readfirstlane(token), lane = threadIdx.x & 63;
-  int seq = -1;
-  for (int s = 0; s <= n_seq; s += 64) {
-    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(s + lane <= n_seq && q_start[min(s + lane, n_seq)] <= first));
-    seq += n;
-    if (n < 64) break;
-  }
-  // the lane's own token: one sequence on for every token in between where each has one, else step by step
-  const int guess = seq + token - first;
-  if (guess > seq && guess < n_seq && seq >= 0 && q_start[guess] == token && q_start[guess + 1] > token) {
-    seq = guess;
-  } else {
-    while (seq < n_seq && q_start[seq + 1] <= token) ++seq;
-  }
-  int place = -1, page = -1;
-  if (real && seq >= 0 && seq < n_seq) {
-    place = kv_len[seq] - (q_start[seq + 1] - token);
-    if (place >= 0 && place / page_size < max_pages) page = page_table[(size_t)seq * max_pages + place / page_size];
-  }
+  const TokenPlace place(token, real, q_start, kv_len, page_table, n_seq, page_size, max_pages);
+  const int page = place.page;
   float x[16];
   kl.values(x);
   kh.values(x + 8);
@@ -65,10 +47,10 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(
   if (page < 0 || page >= n_pages) return;
   if (at.turn) {
     Angles angles;
-    angles.load(r, positions ? positions[token] : place, at.pair, true);
+    angles.load(r, positions ? positions[token] : place.at, at.pair, true);
     rotate<ROPE, 1>(x, angles);
   }
-  const int64_t to = page * page_stride + head * head_stride + place % page_size * row_stride;
+  const int64_t to = page * page_stride + head * head_stride + place.at % page_size * row_stride;
   Eight<E>::template store<ONCE>(k_pages + to + at.lo, x);
   Eight<E>::template store<ONCE>(k_pages + to + at.hi, x + 8);
   vl.template put<ONCE>(v_pages + to + at.lo);

@@ -189,6 +189,12 @@ __device__ inline void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// LDS written by some lanes of a wave is read by others: nothing moves across (no instruction).
+__device__ inline void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 struct Problem {
   int B, H, Hkv, N, d, Br, n_groups, causal, n_planes, gray_mode;
   uint64_t seed;

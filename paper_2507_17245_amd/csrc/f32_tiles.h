@@ -278,12 +278,6 @@ struct Pair<bf16> {
   static __device__ float value(raw x, int i) { return __builtin_bit_cast(float, i ? x & 0xffff0000u : x << 16); }
 };
 
-// LDS written by some lanes of a wave is read by others: nothing moves across (no instruction).
-__device__ inline void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 }  // namespace
 
 }  // namespace da

@@ -34,4 +34,14 @@ size_t paged_f32_scratch_bytes(const da_paged& p);
 hipError_t launch_paged_f32(const void* q, const void* k_pages, const void* v_pages, void* o, const da_paged& p, float scale, void* scratch,
                             size_t scratch_bytes, hipStream_t stream);
 
+// The same over a cache of 4-bit codes.
+hipError_t launch_cache4_append(const void* k, const void* v, const da_cache4& cache, const da_paged& p, hipStream_t stream);
+hipError_t launch_cache4_read(void* k, void* v, const da_cache4& cache, const da_paged& p, hipStream_t stream);
+size_t paged4_scratch_bytes(const da_paged& p);
+hipError_t launch_paged4(const void* q, void* o, const da_cache4& cache, const da_paged& p, float scale, void* scratch, size_t scratch_bytes,
+                         hipStream_t stream);
+size_t paged4_f32_scratch_bytes(const da_paged& p);
+hipError_t launch_paged4_f32(const void* q, void* o, const da_cache4& cache, const da_paged& p, float scale, void* scratch, size_t scratch_bytes,
+                             hipStream_t stream);
+
 }  // namespace da

@@ -177,6 +177,33 @@ __device__ inline void load_weight(float (&w)[16], const void* weight, const Rot
   }
 }
 
+// Where a lane's token (of the batch's rows, ascending over the wave) lies in its sequence, and the page of the table there (-1: none).
+struct TokenPlace {
+  int at = -1, page = -1;
+  __device__ TokenPlace(int token, bool real, const int* __restrict__ q_start, const int* __restrict__ kv_len, const int* __restrict__ page_table, int n_seq,
+                        int page_size, int max_pages) {
+    // sequences that begin at or before the wave's first token
+    const int first = __builtin_amdgcn_readfirstlane(token), lane = threadIdx.x & 63;
+    int seq = -1;
+    for (int s = 0; s <= n_seq; s += 64) {
+      const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(s + lane <= n_seq && q_start[min(s + lane, n_seq)] <= first));
+      seq += n;
+      if (n < 64) break;
+    }
+    // the lane's own token: one sequence on for every token in between where each has one, else step by step
+    const int guess = seq + token - first;
+    if (guess > seq && guess < n_seq && seq >= 0 && q_start[guess] == token && q_start[guess + 1] > token) {
+      seq = guess;
+    } else {
+      while (seq < n_seq && q_start[seq + 1] <= token) ++seq;
+    }
+    if (real && seq >= 0 && seq < n_seq) {
+      at = kv_len[seq] - (q_start[seq + 1] - token);
+      if (at >= 0 && at / page_size < max_pages) page = page_table[(size_t)seq * max_pages + at / page_size];
+    }
+  }
+};
+
 }  // namespace
 
 }  // namespace da
