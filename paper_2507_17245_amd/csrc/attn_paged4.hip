@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kRows4 = 16, kKeys4 = 64;   // rows of a unit, keys of the line's tiles
 constexpr int paged4_pad(int waves) { return waves == 8 ? 6 : 3; }
+constexpr int kSimdWaves = 2;   // (2 | 3, us: 64 sequences of up to 8192 d64 47.4 | 48.3, 200 of up to 2500 d128 79.6 | 86: registers, and more parts to join)
 constexpr float kLift = 8.0f;   // the reference follows when a score is 2^8 times it (weights and sums have room, and rounding is relative)
 
 struct Codes {   // strides in bytes
@@ -30,24 +31,30 @@ struct Codes {   // strides in bytes
   int code_row, scale_row;
 };
 
-// Where 16 successive keys lie: the page (-1: in none of the cache's) and the row in it. A lane for each such group of a wave's next 64.
+// Where 16 successive keys lie, a lane for each such group of a wave's next 64: offsets of the first one's codes and scales, or, in a cache of more than
+// 2 GB, its page and row (far). The 16 lie in one page, so all of their rows are the cache's, whatever the sequence's length is; in the place of
+// keys that are in none of its pages stands its first row.
 struct CodeWindow {
-  int page, row;
-};
-__device__ inline CodeWindow code_window(const int* __restrict__ table, int key, int n_keys, int page_size, int n_pages) {
-  CodeWindow w = {-1, 0};
-  if (key < n_keys) {
-    const unsigned at = (unsigned)key / (unsigned)page_size;
-    const int id = table[at];
-    if (id >= 0 && id < n_pages) w = CodeWindow{id, (int)((unsigned)key - at * (unsigned)page_size)};
+  uint32_t code, scale;
+  uint64_t there;   // groups that lie in the cache
+  template <bool FAR>
+  __device__ void place(int page, int row, int n_pages, const Codes& c) {
+    const bool is = page >= 0 && page < n_pages;
+    page = is ? page : 0;
+    row = is ? row : 0;
+    code = FAR ? (uint32_t)page : (uint32_t)page * (uint32_t)c.code_page + (uint32_t)row * (uint32_t)c.code_row;
+    scale = FAR ? (uint32_t)row : (uint32_t)page * (uint32_t)c.scale_page + (uint32_t)row * (uint32_t)c.scale_row;
+    there = __builtin_amdgcn_ballot_w64(is);
   }
-  return w;
-}
+};
+__device__ inline __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* base) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x00020000); }
 
-__device__ inline f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ inline __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* base, unsigned bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000);
+// Nothing is known of x from here on: what is computed of it stays where it is used.
+__device__ inline int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
+__device__ inline f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // Largest and sum over the four lanes of a row (16 apart).
 __device__ inline float quarter_max(float x) {
   x = half_swap_max(x);
@@ -58,8 +65,8 @@ __device__ inline float quarter_sum(float x) {
   return x + __shfl_xor(x, 16);
 }
 
-template <int D, bool STATS, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void paged4_kernel(
+template <int D, bool STATS, int WAVES, bool FAR>
+__global__ __launch_bounds__(WAVES * 64, kSimdWaves) void paged4_kernel(
     const bf16* __restrict__ q, const Codes cache, bf16* __restrict__ o, const int* __restrict__ page_table, const int* __restrict__ q_start,
     const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv, int n_seq, int n_tokens, int n_pages, int page_size, int max_pages,
     int64_t q_token, int64_t q_head, int causal, float scale_log2e, int ranges, int least, unsigned most, float* __restrict__ part_o,
@@ -79,24 +86,28 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_kernel(
   const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size, most};
   const PagedLine<ROWS, BC, paged4_pad(WAVES)> line(batch, &line_lds, wave, WAVES);
   unsigned pos = 0, end = 1;
-  int wg = blockIdx.x;
+  int wg = blockIdx.x, head = 0;
   if (ranges) {
-    // Ranges that follow each other on one XCD: their units read the same keys.
+    // Every kv head's line is cut into the same `ranges` ones; those of one place in the line follow each other on one XCD, whose L2 then has the lines of
+    // 128 bytes that several heads' scales (or, tokens outside, codes) lie in.
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
-    const unsigned total = line.total * (unsigned)Hkv, length = paged_range(total, gridDim.x, least);
-    pos = paged_cut(line, wg, length, total);
-    end = paged_cut(line, wg + 1, length, total);
-    const PagedCut cut = paged_mark<ROWS>(line, pos, end, length, total);
+    const int part = wg / Hkv;
+    head = wg % Hkv;
+    wg = head * ranges + part;
+    const unsigned length = paged_range(line.total, ranges, least);
+    pos = paged_cut(line, part, length, line.total);
+    end = paged_cut(line, part + 1, length, line.total);
+    PagedCut cut = paged_mark<ROWS>(line, pos, end, length, line.total);
+    cut.head = head;
+    cut.last += head * ranges;
     if (tid == 0) cuts[wg] = cut;
   }
   while (pos < end) {
     PagedUnit u;
-    int head, t0, t1;
+    int t0, t1;
     if (ranges) {
-      head = (int)(pos / line.total);
-      const unsigned at = pos - (unsigned)head * line.total;
-      if (!line.template find<false>(at, &u)) return;
-      t0 = (int)(at - u.first);
+      if (!line.template find<false>(pos, &u)) return;
+      t0 = (int)(pos - u.first);
       t1 = min(u.places, t0 + (int)(end - pos));
     } else {
       // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
@@ -131,51 +142,52 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_kernel(
     const int k_at = m * cache.code_row + g * (D / 8), ks_at = m * cache.scale_row + g * (D / 4) / 32;
     const int vr = lane >> 2, vp = lane & 3;   // row of 16 and quarter of it that the lane brings of V
     const int v_at = vr * cache.code_row + vp * (D / 8), vs_at = vr * cache.scale_row + vp * (D / 4) / 32;
-    // LDS: 16-byte pieces exchanged so that neither the writes (a piece of 4 rows' quarters at a time) nor the transposing reads (two pieces of 8 rows) meet in a bank
-    auto swizzle = [](int row) { return D == 64 ? (row >> 1 & 3) << 1 | (row >> 1 & 1) : (row & 7) | (row & 1) << 3; };
+    // LDS: the 16-byte pieces of a row are exchanged so that neither a write (of eight lanes at a time: a piece of every quarter of two rows) nor a transposing read
+    // (two pieces of eight rows) meets a bank twice
+    auto piece_at = [](int row, int piece) {
+      return D == 64 ? piece ^ ((row >> 1 & 3) << 1 | ((row ^ row >> 1) & 1)) : piece ^ (piece >> 3) ^ (row & 7) << 1;
+    };
     char* const vb = v_lds[wave];
-    const int w_at = vr * ROWB, w_swz = swizzle(vr);
     const int r_row = 4 * g + (m >> 2);
-    const int r_at = r_row * ROWB + ((((m & 3) >> 1) ^ swizzle(r_row)) << 4) + 8 * (m & 1);
+    const int r_at = r_row * ROWB + (piece_at(r_row, (m & 3) >> 1) << 4) + 8 * (m & 1);
 
     int tile = t0 * (BC / FT) + wave;
     const int t_end = min(t1 * (BC / FT), (n_seen + FT - 1) / FT);
     // the window's lane for this wave's tile tile + WAVES i is that of i * GROUPS, and of the groups of 16 keys behind it
-    auto window_of = [&](int first) {
-      const int t = first + (lane / GROUPS) * WAVES;
-      return code_window(table, t * FT + lane % GROUPS * 16, n_seen, page_size, n_pages);
-    };
-    CodeWindow now = window_of(tile), next = window_of(tile + WINDOW / 2 * WAVES);
+    auto key_of = [&](int first) { return (first + (lane / GROUPS) * WAVES) * FT + lane % GROUPS * 16; };
+    auto page_of = [&](int key) { return key < n_seen ? table[(unsigned)key / (unsigned)page_size] : -1; };
+    CodeWindow now;
+    now.template place<FAR>(page_of(key_of(tile)), key_of(tile) % (unsigned)page_size, n_pages, cache);
+    int page_next = page_of(key_of(tile + WINDOW * WAVES));
     int at = 0;   // place in the window of the tile that is asked for
     uint32_t kc[GROUPS][WORDS], vc[GROUPS][WORDS];
     int ks[GROUPS], vs[GROUPS];
-    auto ask = [&](int t, const uint8_t* codes, const uint8_t* scales, int code_at, int scale_at, uint32_t (&c)[GROUPS][WORDS], int (&e)[GROUPS]) -> int {
-      int there = 0;
+    // Loads in this order and nowhere else: the waits for a tile's keys leave its values, and the next one's keys, on their way.
+    auto ask = [&](const uint8_t* codes, const uint8_t* scales, int code_at, int scale_at, uint32_t (&c)[GROUPS][WORDS], int (&e)[GROUPS]) {
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) {
-        const int page = __builtin_amdgcn_readlane(now.page, at * GROUPS + i), row = __builtin_amdgcn_readlane(now.row, at * GROUPS + i);
-        const int rows = min(n_seen - (t * FT + 16 * i), 16), id = max(page, 0);
-        there |= (page >= 0 ? 1 : 0) << i;
-        const __amdgpu_buffer_rsrc_t code_rsrc = rows_rsrc(codes + (id * cache.code_page + (int64_t)row * cache.code_row), page >= 0 ? (unsigned)((rows - 1) * cache.code_row + D / 2) : 0u);
-        const __amdgpu_buffer_rsrc_t scale_rsrc = rows_rsrc(scales + (id * cache.scale_page + (int64_t)row * cache.scale_row), page >= 0 ? (unsigned)((rows - 1) * cache.scale_row + D / 32) : 0u);
+        const int a = __builtin_amdgcn_readlane((int)now.code, at * GROUPS + i), b = __builtin_amdgcn_readlane((int)now.scale, at * GROUPS + i);
+        const __amdgpu_buffer_rsrc_t code_rsrc = rows_rsrc(FAR ? codes + (a * cache.code_page + (int64_t)b * cache.code_row) : codes);
+        const __amdgpu_buffer_rsrc_t scale_rsrc = rows_rsrc(FAR ? scales + (a * cache.scale_page + (int64_t)b * cache.scale_row) : scales);
+        e[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(scale_rsrc, scale_at, FAR ? 0 : b, 0);
         if constexpr (WORDS == 2) {
-          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(code_rsrc, code_at, 0, 0));
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(code_rsrc, code_at, FAR ? 0 : a, 0));
           c[i][0] = x[0];
           c[i][1] = x[1];
         } else {
-          const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_rsrc, code_at, 0, 0));
+          const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_rsrc, code_at, FAR ? 0 : a, 0));
 #pragma unroll
           for (int j = 0; j < 4; ++j) c[i][j] = x[j];
         }
-        e[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(scale_rsrc, scale_at, 0, 0);
       }
-      return there;
+      __builtin_amdgcn_sched_barrier(0);
     };
-    int there = 0;
-    if (tile < t_end) {
-      there = ask(tile, k_codes, k_scales, k_at, ks_at, kc, ks);
-      ask(tile, v_codes, v_scales, v_at, vs_at, vc, vs);
-    }
+    auto there_of = [&]() { return (int)(now.there >> (at * GROUPS) & ((1 << GROUPS) - 1)); };
+    // (also behind the last tile: the waits then know how many loads are on their way)
+    int there = there_of();
+    ask(k_codes, k_scales, k_at, ks_at, kc, ks);
+    ask(v_codes, v_scales, v_at, vs_at, vc, vs);
     f32x4 oacc[NCT], lacc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) oacc[ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -193,19 +205,23 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_kernel(
 #pragma unroll
         for (int s = 0; s < KSTEPS; ++s) sc[i] = mfma_16x16x32(Values8<bf16>(kc[i][s], scale_value(ks[i])).x, qop[s], sc[i]);
       }
-      const bool more = tile + WAVES < t_end;
-      if (more) {
-        ++at;
-        there = ask(tile + WAVES, k_codes, k_scales, k_at, ks_at, kc, ks);
+      if (++at == WINDOW) {
+        const int first = key_of(tile + WAVES);
+        at = 0;
+        now.template place<FAR>(page_next, first % (unsigned)page_size, n_pages, cache);
+        page_next = page_of(first + WINDOW * WAVES * FT);
       }
+      there = there_of();
+      ask(k_codes, k_scales, k_at, ks_at, kc, ks);
       const int n0 = tile * FT;
       const bool some = n0 + FT > all_see || seen != (1 << GROUPS) - 1;
       if (some) {
+        const int past = here(lim - n0 - 4 * g);   // keys of the lane's that the row sees
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (n0 + 16 * i + 4 * g + j > lim || !(seen >> i & 1)) sc[i][j] = -INFINITY;
+            if (16 * i + j > past || !(seen >> i & 1)) sc[i][j] = -INFINITY;
       }
       float mx = sc[0][0];
 #pragma unroll
@@ -232,67 +248,62 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_kernel(
           if constexpr (STATS) e_run += x;
           pop[i / 2][i % 2 * 4 + j] = (bf16)x;
         }
-      // V: values, and where rows do not all see a tile's keys and 32 channels are NaN, first without those, then they alone
-      bool odd = false;
+      // V. Rows that none of the unit's sees are taken as zeros.
+      bool odd = false;   // a value may be an infinity or a NaN
       if (some) {
 #pragma unroll
-        for (int i = 0; i < GROUPS; ++i) odd |= vs[i] == kScaleNaN;
+        for (int i = 0; i < GROUPS; ++i) {
+          if (n0 + 16 * i + vr >= n_seen || !(seen >> i & 1)) vs[i] = 0;
+          odd |= vs[i] > kScaleMost;
+        }
         odd = __builtin_amdgcn_ballot_w64(odd) != 0;
       }
-      auto convert = [&](auto value) {   // value(i, s): eight channels
-        wave_order();   // the reads of the previous tile come first
+      wave_order();   // the reads of the previous tile come first
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+        for (int s = 0; s < WORDS; ++s)
+          *(bf16x8*)(vb + (i * 16 + vr) * ROWB + (piece_at(vr, vp * WORDS + s) << 4)) = Values8<bf16>(vc[i][s], scale_value(vs[i])).x;
+      wave_order();
+      if (odd) {
+        // Keys that not every row sees, and an infinity or a NaN among their values: the product would bring it to the rows with P = 0, too. Those
+        // that a row sees are added to its sums, key by key; the product goes without.
+        const int last = here(lim - n0);
+#pragma unroll 1
+        for (int key = 0; key < FT; ++key) {
+          const bool sees = key <= last && (seen >> (key >> 4) & 1);
+          const char* row = vb + key * ROWB + 8 * (g & 1);
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) {
+            const bf16x4 x = *(const bf16x4*)(row + (piece_at(key & 15, 2 * ct + (g >> 1)) << 4));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) oacc[ct][j] += sees && !(__builtin_fabsf((float)x[j]) < INFINITY) ? (float)x[j] : 0.0f;
+          }
+        }
+        wave_order();
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
-          for (int s = 0; s < WORDS; ++s) *(bf16x8*)(vb + i * 16 * ROWB + w_at + (((vp * WORDS + s) ^ w_swz) << 4)) = value(i, s);
+          for (int s = 0; s < WORDS; ++s) {
+            bf16x8* at = (bf16x8*)(vb + (i * 16 + vr) * ROWB + (piece_at(vr, vp * WORDS + s) << 4));
+            bf16x8 x = *at;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __builtin_fabsf((float)x[j]) < INFINITY ? x[j] : (bf16)0.0f;
+            *at = x;
+          }
         wave_order();
-      };
+      }
       auto operand = [&](int tt, int ct) {
-        const char* p0 = vb + (r_at ^ (ct * 32)) + 32 * tt * ROWB;
+        const char* p0 = vb + (r_at ^ (piece_at(0, 2 * ct) << 4)) + 32 * tt * ROWB;
         return lds_read_tr_pair<bf16x8>(p0, p0 + 16 * ROWB);
       };
-      if (odd) {
-        bf16 one = (bf16)1.0f;
-        bf16x8 zeros, all;
+      ask(v_codes, v_scales, v_at, vs_at, vc, vs);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          zeros[j] = (bf16)0.0f;
-          all[j] = one;
-        }
-        convert([&](int i, int) { return vs[i] == kScaleNaN ? all : zeros; });
+      for (int tt = 0; tt < FT / 32; ++tt) lacc = mfma_16x16x32(ones, pop[tt], lacc);
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) {
-          f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int tt = 0; tt < FT / 32; ++tt) {
-            bf16x8 sees;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int i = 2 * tt + j / 4;
-              sees[j] = (bf16)(n0 + 16 * i + 4 * g + j % 4 > lim || !(seen >> i & 1) ? 0.0f : 1.0f);
-            }
-            z = mfma_16x16x32(operand(tt, ct), sees, z);
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (z[j] > 0.0f) oacc[ct][j] = __builtin_nanf("");
-        }
-        convert([&](int i, int s) { return vs[i] == kScaleNaN ? zeros : Values8<bf16>(vc[i][s], scale_value(vs[i])).x; });
-      } else {
-        convert([&](int i, int s) { return Values8<bf16>(vc[i][s], scale_value(vs[i])).x; });
-      }
-      if (more) ask(tile + WAVES, v_codes, v_scales, v_at, vs_at, vc, vs);
-#pragma unroll
-      for (int tt = 0; tt < FT / 32; ++tt) {
-        lacc = mfma_16x16x32(ones, pop[tt], lacc);
+      for (int tt = 0; tt < FT / 32; ++tt)
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) oacc[ct] = mfma_16x16x32(operand(tt, ct), pop[tt], oacc[ct]);
-      }
-      if (at == WINDOW / 2) {   // (the next to be asked for is behind it)
-        at = 0;
-        now = next;
-        next = window_of(tile + (1 + WINDOW / 2) * WAVES);
-      }
       // (behind a branch the compiler does not wait long enough for the products on every path)
       __builtin_amdgcn_sched_barrier(0);
       asm volatile("s_nop 7");
@@ -338,11 +349,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_kernel(
   }
 }
 
-template <int D, int WAVES>
+template <int D, int WAVES, bool FAR>
 hipError_t launch_as(const void* q, void* o, const Codes& cache, const da_paged& p, float scale, void* scratch, const PagedLaunch& l, hipStream_t stream) {
   const float scale_log2e = scale * 1.4426950408889634f;
   const PagedScratch at(scratch, l.workgroups, kRows4, D);
-  hipLaunchKernelGGL((p.lse_out ? paged4_kernel<D, true, WAVES> : paged4_kernel<D, false, WAVES>), dim3((unsigned)l.workgroups), dim3(WAVES * 64), 0, stream,
+  hipLaunchKernelGGL((p.lse_out ? paged4_kernel<D, true, WAVES, FAR> : paged4_kernel<D, false, WAVES, FAR>), dim3((unsigned)l.workgroups), dim3(WAVES * 64), 0, stream,
                      (const bf16*)q, cache, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size,
                      p.max_pages, p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, l.most, at.sums, at.stats, at.cuts);
   hipError_t e = hipGetLastError();
@@ -353,24 +364,34 @@ hipError_t launch_as(const void* q, void* o, const Codes& cache, const da_paged&
 }
 
 template <int D>
-hipError_t launch_d(const void* q, void* o, const Codes& cache, const da_paged& p, float scale, void* scratch, size_t scratch_bytes, hipStream_t stream) {
+hipError_t launch_d(const void* q, void* o, const Codes& cache, bool far, const da_paged& p, float scale, void* scratch, size_t scratch_bytes, hipStream_t stream) {
   const long long units = (long long)p.n_seq * p.Hkv;   // that there are about
-  auto launch = [&](int waves) { return paged_launch(p, kRows4, kKeys4, paged4_pad(waves), 8 * kComputeUnits / waves, 20, scratch_bytes); };
-  if (units <= kComputeUnits) return launch_as<D, 8>(q, o, cache, p, scale, scratch, launch(8), stream);
-  return launch_as<D, 4>(q, o, cache, p, scale, scratch, launch(4), stream);
+  const int waves = !far && units > kComputeUnits ? 4 : 8;
+  PagedLaunch l = paged_launch(p, kRows4, kKeys4, paged4_pad(waves), 4 * kSimdWaves * kComputeUnits / waves, 20, scratch_bytes);
+  if (l.ranges) {
+    l.ranges = l.workgroups / p.Hkv;
+    const int whole = 8 / std::gcd(8, p.Hkv);   // of a number of workgroups that the XCDs share evenly
+    if (l.ranges > 16 * whole) l.ranges -= l.ranges % whole;
+    if (l.ranges < 2) l.ranges = 0;
+    l.workgroups = l.ranges ? l.ranges * p.Hkv : (int)(paged_units(p, kRows4) * p.Hkv);
+  }
+  return (far ? launch_as<D, 8, true> : waves == 8 ? launch_as<D, 8, false> : launch_as<D, 4, false>)(q, o, cache, p, scale, scratch, l, stream);
 }
 
 }  // namespace
 
 size_t paged4_scratch_bytes(const da_paged& p) {
-  return p.dtype == DA_F32 ? paged4_f32_scratch_bytes(p) : paged_launch_bytes(2 * kComputeUnits, kRows4, p.d);
+  return p.dtype == DA_F32 ? paged4_f32_scratch_bytes(p) : paged_launch_bytes(kSimdWaves * kComputeUnits, kRows4, p.d);
 }
 
 hipError_t launch_paged4(const void* q, void* o, const da_cache4& c, const da_paged& p, float scale, void* scratch, size_t scratch_bytes, hipStream_t stream) {
   if (p.dtype == DA_F32) return launch_paged4_f32(q, o, c, p, scale, scratch, scratch_bytes, stream);
   const Codes cache = {(const uint8_t*)c.k_codes, (const uint8_t*)c.k_scales, (const uint8_t*)c.v_codes, (const uint8_t*)c.v_scales, c.code_stride[0],
                        c.code_stride[1], c.scale_stride[0], c.scale_stride[1], (int)c.code_stride[2], (int)c.scale_stride[2]};
-  return p.d == 64 ? launch_d<64>(q, o, cache, p, scale, scratch, scratch_bytes, stream) : launch_d<128>(q, o, cache, p, scale, scratch, scratch_bytes, stream);
+  // whether a kv head's pages reach farther than offsets of 31 bits
+  auto reaches = [&](const int64_t* stride) { return (p.n_pages - 1) * (double)stride[0] + (p.page_size - 1) * (double)stride[2] + p.d > 2e9; };
+  const bool far = reaches(c.code_stride) || reaches(c.scale_stride);
+  return p.d == 64 ? launch_d<64>(q, o, cache, far, p, scale, scratch, scratch_bytes, stream) : launch_d<128>(q, o, cache, far, p, scale, scratch, scratch_bytes, stream);
 }
 
 }  // namespace da
