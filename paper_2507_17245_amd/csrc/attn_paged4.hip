@@ -1,387 +1,573 @@
-// Attention of new tokens over a paged cache of 4-bit codes (fp4.h), bf16. Work split: paged_units.h.
+// Attention of new tokens over a paged cache of 4-bit codes (fp4.h), bf16: single tokens to chunks of a prompt. Work split: paged_units.h.
 //
 //   O = softmax(scale Q K^T) V over the keys that a row sees, one pass: running reference and sum of every row.
 //
-// A unit is up to 16 query rows of a sequence and a kv head (all query heads of the kv head, token after token). Every wave of a workgroup has all rows
-// and every WAVES-th tile of its own (4352 bytes of keys and values: 64 keys at d = 64, 32 at 128), with a softmax state of its own and no
-// barrier until the states meet. Bound: reading the codes, and beside it the conversions and exponentials.
-//   S^T = K Q^T   by v_mfma_f32_16x16x32_bf16. A lane loads of a key what it is the operand for (8 or 16 bytes: the contraction is dealt out so), converts it with
-//                 its scale (every value of a code is a bf16 number) and multiplies; no LDS.
-//   O^T = V^T P^T P is where it is needed. V is converted with its scales, written to LDS a wave's tile at a time and read transposed.
-// K of the next tile is asked for when this one's is converted, V likewise.
-#include <cfloat>
-
-#include "attn_bf16_impl.h"
-#include "fp4.h"
-#include "paged.h"
-#include "paged_units.h"
+// A unit is up to 128 query rows of a sequence and a kv head (all query heads of the kv head, token after token); of calls with single tokens up to
+// 16 rows, by a kernel with the walk of few rows alone (paged4_few.h).
+//   more than 32 rows: as in attn_paged.hip: waves own 32 rows each, and of eight waves each of a pair with the same rows walks half of the unit's
+//     tiles of 64 keys in buffers of its half's own. The four waves that share a tile load 16 keys of it each, convert them and write them to LDS
+//     as bf16, keys two tiles ahead of the products, values one; codes are asked for a tile before. Bound: the matrix products (at d = 64 the
+//     exponentials beside them); the conversions are 16 (d = 64) or 32 instructions a wave and tile.
+//   up to 32 rows: 16 at a time as few rows.
+#include "paged4_few.h"
 
 namespace da {
 
 namespace {
 
-constexpr int kRows4 = 16, kKeys4 = 64;   // rows of a unit, keys of the line's tiles
-constexpr int paged4_pad(int waves) { return waves == 8 ? 6 : 3; }
+constexpr int kUnitRows = 128, kFewRows = 16, kTileKeys = 64, kRW = 4;   // rows and keys of the line's units and tiles, waves over the rows
+constexpr int paged4_pad(int rows, int waves) { return rows != kFewRows ? 8 : waves == 8 ? 6 : 3; }
 constexpr int kSimdWaves = 2;   // (2 | 3, us: 64 sequences of up to 8192 d64 47.4 | 48.3, 200 of up to 2500 d128 79.6 | 86: registers, and more parts to join)
-constexpr float kLift = 8.0f;   // the reference follows when a score is 2^8 times it (weights and sums have room, and rounding is relative)
 
-struct Codes {   // strides in bytes
-  const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
-  int64_t code_page, code_head, scale_page, scale_head;
-  int code_row, scale_row;
-};
+// Where the 16-byte pieces of a row of 64 keys lie in LDS: neither the writes (eight lanes at a time: a piece of every quarter of two rows) nor the reads of K (the
+// same piece of eight rows) and the transposing ones of V (two pairs of pieces of four rows) meet in a bank.
+template <int D>
+__device__ inline int k_piece(int row, int piece) {
+  return D == 64 ? piece ^ (row & 7) : piece ^ (piece >> 3) ^ (row & 7) << 1 ^ (row >> 3 & 1);
+}
+template <int D>
+__device__ inline int v_piece(int row, int piece) {
+  return D == 64 ? piece ^ ((row >> 1 & 1) << 2 | (row & 1)) : piece ^ (piece >> 3) ^ ((row & 3) << 2 | (row & 1) << 1);
+}
 
-// Where 16 successive keys lie, a lane for each such group of a wave's next 64: offsets of the first one's codes and scales, or, in a cache of more than
-// 2 GB, its page and row (far). The 16 lie in one page, so all of their rows are the cache's, whatever the sequence's length is; in the place of
-// keys that are in none of its pages stands its first row.
-struct CodeWindow {
-  uint32_t code, scale;
-  uint64_t there;   // groups that lie in the cache
-  template <bool FAR>
-  __device__ void place(int page, int row, int n_pages, const Codes& c) {
-    const bool is = page >= 0 && page < n_pages;
-    page = is ? page : 0;
-    row = is ? row : 0;
-    code = FAR ? (uint32_t)page : (uint32_t)page * (uint32_t)c.code_page + (uint32_t)row * (uint32_t)c.code_row;
-    scale = FAR ? (uint32_t)row : (uint32_t)page * (uint32_t)c.scale_page + (uint32_t)row * (uint32_t)c.scale_row;
-    there = __builtin_amdgcn_ballot_w64(is);
+// Codes of 16 keys or values, on their way or here: a lane has a quarter of a row.
+template <int D>
+struct Quarter {
+  static constexpr int WORDS = D / 32;
+  uint32_t codes[WORDS];
+  int scale;
+  __device__ void load(const uint8_t* from, const uint8_t* scales, uint64_t code, uint64_t at_scale, int code_at, int scale_at) {
+    scale = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rows_rsrc(scales + at_scale), scale_at, 0, 0);
+    if constexpr (WORDS == 2) {
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows_rsrc(from + code), code_at, 0, 0));
+      codes[0] = x[0];
+      codes[1] = x[1];
+    } else {
+      const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows_rsrc(from + code), code_at, 0, 0));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) codes[j] = x[j];
+    }
+  }
+  template <typename AT>
+  __device__ void store(AT at, bool zero) const {   // at(piece of the quarter): where it lies
+    const float s = scale_value(zero ? 0 : scale);
+#pragma unroll
+    for (int j = 0; j < WORDS; ++j) *(bf16x8*)at(j) = Values8<bf16>(codes[j], s).x;
   }
 };
-__device__ inline __amdgpu_buffer_rsrc_t rows_rsrc(const uint8_t* base) { return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x00020000); }
 
-// Nothing is known of x from here on: what is computed of it stays where it is used.
-__device__ inline int here(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-__device__ inline f32x4 mfma_16x16x32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-// Largest and sum over the four lanes of a row (16 apart).
-__device__ inline float quarter_max(float x) {
-  x = half_swap_max(x);
-  return fmaxf(x, __shfl_xor(x, 16));
-}
-__device__ inline float quarter_sum(float x) {
-  x = half_swap_sum(x);
-  return x + __shfl_xor(x, 16);
-}
-
-template <int D, bool STATS, int WAVES, bool FAR>
-__global__ __launch_bounds__(WAVES * 64, kSimdWaves) void paged4_kernel(
-    const bf16* __restrict__ q, const Codes cache, bf16* __restrict__ o, const int* __restrict__ page_table, const int* __restrict__ q_start,
-    const int* __restrict__ kv_len, float* __restrict__ lse, int H, int Hkv, int n_seq, int n_tokens, int n_pages, int page_size, int max_pages,
-    int64_t q_token, int64_t q_head, int causal, float scale_log2e, int ranges, int least, unsigned most, float* __restrict__ part_o,
-    f32x4* __restrict__ part_stat, PagedCut* __restrict__ cuts) {
-  constexpr int ROWS = kRows4, BC = kKeys4, FT = D == 64 ? 64 : 32, GROUPS = FT / 16, KSTEPS = D / 32, NCT = D / 16, WORDS = D / 32;
-  constexpr int WINDOW = 64 / GROUPS;
-  constexpr int TILEB = FT * D * 2, ROWB = D * 2;
-  static_assert(TILEB >= ROWS * D * 4, "a wave's sums take the place of its tile");
-  __shared__ __attribute__((aligned(1024))) char v_lds[WAVES][TILEB];
-  __shared__ f32x4 stat_lds[WAVES][ROWS];
-  __shared__ PagedLds line_lds;
-
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int m = lane & 15, g = lane >> 4;
-  const int group = H / Hkv;
-  const PagedBatch batch = {q_start, kv_len, n_seq, n_tokens, group, max_pages * page_size, most};
-  const PagedLine<ROWS, BC, paged4_pad(WAVES)> line(batch, &line_lds, wave, WAVES);
+// The workgroup's work: pos .. end of a line (ranges), or one unit.
+template <typename LINE, int ROWS>
+struct Share {
   unsigned pos = 0, end = 1;
   int wg = blockIdx.x, head = 0;
-  if (ranges) {
+  __device__ Share(const Paged4Call& p, const LINE& line) {
+    if (!p.ranges) return;
     // Every kv head's line is cut into the same `ranges` ones; those of one place in the line follow each other on one XCD, whose L2 then has the lines of
     // 128 bytes that several heads' scales (or, tokens outside, codes) lie in.
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
-    const int part = wg / Hkv;
-    head = wg % Hkv;
-    wg = head * ranges + part;
-    const unsigned length = paged_range(line.total, ranges, least);
+    const int part = wg / p.Hkv;
+    head = wg % p.Hkv;
+    wg = head * p.ranges + part;
+    const unsigned length = paged_range(line.total, p.ranges, p.least);
     pos = paged_cut(line, part, length, line.total);
     end = paged_cut(line, part + 1, length, line.total);
     PagedCut cut = paged_mark<ROWS>(line, pos, end, length, line.total);
     cut.head = head;
-    cut.last += head * ranges;
-    if (tid == 0) cuts[wg] = cut;
+    cut.last += head * p.ranges;
+    if (threadIdx.x == 0) p.cuts[wg] = cut;
   }
-  while (pos < end) {
-    PagedUnit u;
-    int t0, t1;
-    if (ranges) {
-      if (!line.template find<false>(pos, &u)) return;
+  // The next unit and its tiles; false: none.
+  __device__ bool next(const Paged4Call& p, const LINE& line, PagedUnit& u, int& t0, int& t1) {
+    if (pos >= end) return false;
+    if (p.ranges) {
+      if (!line.template find<false>(pos, &u)) return false;
       t0 = (int)(pos - u.first);
       t1 = min(u.places, t0 + (int)(end - pos));
     } else {
       // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
-      head = wg % Hkv;
-      if (!line.template find<true>(wg / Hkv, &u)) return;
+      head = wg % p.Hkv;
+      if (!line.template find<true>(wg / p.Hkv, &u)) return false;
       u.m0 = (u.rows - 1) / ROWS * ROWS - u.m0;
       t0 = 0;
       t1 = u.places;
     }
-    const bool whole = t0 == 0 && t1 == u.places;
     pos += (unsigned)(t1 - t0);
+    return true;
+  }
+};
 
-    const int n_keys = min(u.len, batch.max_keys);
-    const int* table = page_table + (int64_t)u.seq * max_pages;
-    const int m1 = min(u.m0 + ROWS, u.rows), mr = min(u.m0 + m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
-    const int token = u.q0 + mr / group, q_of = head * group + mr % group;
-    const int lim = min(causal ? u.len - u.nq + mr / group : n_keys - 1, n_keys - 1);   // last key this row sees
-    const int n_seen = causal ? min(n_keys, max(u.len - u.nq + (m1 - 1) / group + 1, 0)) : n_keys;   // no row sees more
-    const int all_see = causal ? min(max(u.len - u.nq + u.m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
-
-    // Operands of Q: the channels of a lane's pieces of K.
-    bf16x8 qop[KSTEPS];
-    {
-      const bf16* q_row = q + token * q_token + q_of * q_head + g * (D / 4);
-#pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 8 * s);
-    }
-    const uint8_t* k_codes = cache.k_codes + head * cache.code_head;
-    const uint8_t* v_codes = cache.v_codes + head * cache.code_head;
-    const uint8_t* k_scales = cache.k_scales + head * cache.scale_head;
-    const uint8_t* v_scales = cache.v_scales + head * cache.scale_head;
-    const int k_at = m * cache.code_row + g * (D / 8), ks_at = m * cache.scale_row + g * (D / 4) / 32;
-    const int vr = lane >> 2, vp = lane & 3;   // row of 16 and quarter of it that the lane brings of V
-    const int v_at = vr * cache.code_row + vp * (D / 8), vs_at = vr * cache.scale_row + vp * (D / 4) / 32;
-    // LDS: the 16-byte pieces of a row are exchanged so that neither a write (of eight lanes at a time: a piece of every quarter of two rows) nor a transposing read
-    // (two pieces of eight rows) meets a bank twice
-    auto piece_at = [](int row, int piece) {
-      return D == 64 ? piece ^ ((row >> 1 & 3) << 1 | ((row ^ row >> 1) & 1)) : piece ^ (piece >> 3) ^ (row & 7) << 1;
-    };
-    char* const vb = v_lds[wave];
-    const int r_row = 4 * g + (m >> 2);
-    const int r_at = r_row * ROWB + (piece_at(r_row, (m & 3) >> 1) << 4) + 8 * (m & 1);
-
-    int tile = t0 * (BC / FT) + wave;
-    const int t_end = min(t1 * (BC / FT), (n_seen + FT - 1) / FT);
-    // the window's lane for this wave's tile tile + WAVES i is that of i * GROUPS, and of the groups of 16 keys behind it
-    auto key_of = [&](int first) { return (first + (lane / GROUPS) * WAVES) * FT + lane % GROUPS * 16; };
-    auto page_of = [&](int key) { return key < n_seen ? table[(unsigned)key / (unsigned)page_size] : -1; };
-    CodeWindow now;
-    now.template place<FAR>(page_of(key_of(tile)), key_of(tile) % (unsigned)page_size, n_pages, cache);
-    int page_next = page_of(key_of(tile + WINDOW * WAVES));
-    int at = 0;   // place in the window of the tile that is asked for
-    uint32_t kc[GROUPS][WORDS], vc[GROUPS][WORDS];
-    int ks[GROUPS], vs[GROUPS];
-    // Loads in this order and nowhere else: the waits for a tile's keys leave its values, and the next one's keys, on their way.
-    auto ask = [&](const uint8_t* codes, const uint8_t* scales, int code_at, int scale_at, uint32_t (&c)[GROUPS][WORDS], int (&e)[GROUPS]) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < GROUPS; ++i) {
-        const int a = __builtin_amdgcn_readlane((int)now.code, at * GROUPS + i), b = __builtin_amdgcn_readlane((int)now.scale, at * GROUPS + i);
-        const __amdgpu_buffer_rsrc_t code_rsrc = rows_rsrc(FAR ? codes + (a * cache.code_page + (int64_t)b * cache.code_row) : codes);
-        const __amdgpu_buffer_rsrc_t scale_rsrc = rows_rsrc(FAR ? scales + (a * cache.scale_page + (int64_t)b * cache.scale_row) : scales);
-        e[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(scale_rsrc, scale_at, FAR ? 0 : b, 0);
-        if constexpr (WORDS == 2) {
-          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(code_rsrc, code_at, FAR ? 0 : a, 0));
-          c[i][0] = x[0];
-          c[i][1] = x[1];
-        } else {
-          const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_rsrc, code_at, FAR ? 0 : a, 0));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) c[i][j] = x[j];
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    auto there_of = [&]() { return (int)(now.there >> (at * GROUPS) & ((1 << GROUPS) - 1)); };
-    // (also behind the last tile: the waits then know how many loads are on their way)
-    int there = there_of();
-    ask(k_codes, k_scales, k_at, ks_at, kc, ks);
-    ask(v_codes, v_scales, v_at, vs_at, vc, vs);
-    f32x4 oacc[NCT], lacc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int ct = 0; ct < NCT; ++ct) oacc[ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    bf16x8 ones;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ones[j] = (bf16)1.0f;
-    // The reference is a score, unscaled (a scaled one is rounded, which shows on large scores); sum before rounding, over this lane's keys.
-    float ref = -FLT_MAX, e_run = 0.0f;
-    for (; tile < t_end; tile += WAVES) {
-      const int seen = there;
-      f32x4 sc[GROUPS];
-#pragma unroll
-      for (int i = 0; i < GROUPS; ++i) {
-        sc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int s = 0; s < KSTEPS; ++s) sc[i] = mfma_16x16x32(Values8<bf16>(kc[i][s], scale_value(ks[i])).x, qop[s], sc[i]);
-      }
-      if (++at == WINDOW) {
-        const int first = key_of(tile + WAVES);
-        at = 0;
-        now.template place<FAR>(page_next, first % (unsigned)page_size, n_pages, cache);
-        page_next = page_of(first + WINDOW * WAVES * FT);
-      }
-      there = there_of();
-      ask(k_codes, k_scales, k_at, ks_at, kc, ks);
-      const int n0 = tile * FT;
-      const bool some = n0 + FT > all_see || seen != (1 << GROUPS) - 1;
-      if (some) {
-        const int past = here(lim - n0 - 4 * g);   // keys of the lane's that the row sees
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (16 * i + j > past || !(seen >> i & 1)) sc[i][j] = -INFINITY;
-      }
-      float mx = sc[0][0];
-#pragma unroll
-      for (int i = 0; i < GROUPS; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[i][j]);
-      if (__builtin_amdgcn_ballot_w64((mx - ref) * scale_log2e > kLift) != 0) {
-        const float ref_new = fmaxf(ref, quarter_max(mx));
-        const float alpha = __builtin_amdgcn_exp2f((ref - ref_new) * scale_log2e);
-        lacc *= alpha;
-        if constexpr (STATS) e_run *= alpha;
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) oacc[ct] *= alpha;
-        ref = ref_new;
-      }
-      // P rounded to bf16 as the operands of P.V; the row sum is taken over the rounded values (on the matrix pipe), so that the rounding of a
-      // row's largest weights cancels
-      bf16x8 pop[FT / 32];
-#pragma unroll
-      for (int i = 0; i < GROUPS; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float x = __builtin_amdgcn_exp2f((sc[i][j] - ref) * scale_log2e);
-          if constexpr (STATS) e_run += x;
-          pop[i / 2][i % 2 * 4 + j] = (bf16)x;
-        }
-      // V. Rows that none of the unit's sees are taken as zeros.
-      bool odd = false;   // a value may be an infinity or a NaN
-      if (some) {
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i) {
-          if (n0 + 16 * i + vr >= n_seen || !(seen >> i & 1)) vs[i] = 0;
-          odd |= vs[i] > kScaleMost;
-        }
-        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
-      }
-      wave_order();   // the reads of the previous tile come first
-#pragma unroll
-      for (int i = 0; i < GROUPS; ++i)
-#pragma unroll
-        for (int s = 0; s < WORDS; ++s)
-          *(bf16x8*)(vb + (i * 16 + vr) * ROWB + (piece_at(vr, vp * WORDS + s) << 4)) = Values8<bf16>(vc[i][s], scale_value(vs[i])).x;
-      wave_order();
-      if (odd) {
-        // Keys that not every row sees, and an infinity or a NaN among their values: the product would bring it to the rows with P = 0, too. Those
-        // that a row sees are added to its sums, key by key; the product goes without.
-        const int last = here(lim - n0);
-#pragma unroll 1
-        for (int key = 0; key < FT; ++key) {
-          const bool sees = key <= last && (seen >> (key >> 4) & 1);
-          const char* row = vb + key * ROWB + 8 * (g & 1);
-#pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) {
-            const bf16x4 x = *(const bf16x4*)(row + (piece_at(key & 15, 2 * ct + (g >> 1)) << 4));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) oacc[ct][j] += sees && !(__builtin_fabsf((float)x[j]) < INFINITY) ? (float)x[j] : 0.0f;
-          }
-        }
-        wave_order();
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i)
-#pragma unroll
-          for (int s = 0; s < WORDS; ++s) {
-            bf16x8* at = (bf16x8*)(vb + (i * 16 + vr) * ROWB + (piece_at(vr, vp * WORDS + s) << 4));
-            bf16x8 x = *at;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = __builtin_fabsf((float)x[j]) < INFINITY ? x[j] : (bf16)0.0f;
-            *at = x;
-          }
-        wave_order();
-      }
-      auto operand = [&](int tt, int ct) {
-        const char* p0 = vb + (r_at ^ (piece_at(0, 2 * ct) << 4)) + 32 * tt * ROWB;
-        return lds_read_tr_pair<bf16x8>(p0, p0 + 16 * ROWB);
-      };
-      ask(v_codes, v_scales, v_at, vs_at, vc, vs);
-#pragma unroll
-      for (int tt = 0; tt < FT / 32; ++tt) lacc = mfma_16x16x32(ones, pop[tt], lacc);
-#pragma unroll
-      for (int tt = 0; tt < FT / 32; ++tt)
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) oacc[ct] = mfma_16x16x32(operand(tt, ct), pop[tt], oacc[ct]);
-      // (behind a branch the compiler does not wait long enough for the products on every path)
-      __builtin_amdgcn_sched_barrier(0);
-      asm volatile("s_nop 7");
-    }
-    // the waves' states meet
-    const float l_tot = lacc[0], e_tot = STATS ? quarter_sum(e_run) : 0.0f;
-    if (g == 0) stat_lds[wave][m] = f32x4{ref, l_tot, e_tot, 0.0f};
-    __syncthreads();
-    float ref_all = stat_lds[0][m][0], l_all = 0.0f, e_all = 0.0f;
-#pragma unroll
-    for (int j = 1; j < WAVES; ++j) ref_all = fmaxf(ref_all, stat_lds[j][m][0]);
-#pragma unroll
-    for (int j = 0; j < WAVES; ++j) {
-      const f32x4 st = stat_lds[j][m];
-      const float x = __builtin_amdgcn_exp2f((st[0] - ref_all) * scale_log2e);
-      l_all += st[1] * x;
-      e_all += st[2] * x;
-    }
-    // (a row that sees nothing has sum 0 and is 0)
-    const float weight = __builtin_amdgcn_exp2f((ref - ref_all) * scale_log2e) * (!whole ? 1.0f : l_all == 0.0f ? 0.0f : 1.0f / l_all);
-    // a wave's sums: 16 rows of D floats in its buffer, the 16-byte pieces exchanged by the row
-#pragma unroll
-    for (int ct = 0; ct < NCT; ++ct) *(f32x4*)(vb + m * (D * 4) + (((4 * ct + g) ^ m) << 4)) = oacc[ct] * weight;
-    __syncthreads();
-    const size_t slot = (2 * (size_t)wg + (t0 == 0 ? 2 : 1)) * ROWS;
-    for (int i = tid; i < (m1 - u.m0) * (D / 4); i += WAVES * 64) {
-      const int row = i / (D / 4), piece = i % (D / 4), r = u.m0 + row;
-      f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int j = 0; j < WAVES; ++j) x += *(const f32x4*)(v_lds[j] + row * (D * 4) + ((piece ^ row) << 4));
-      if (whole) {
-        const bf16x4 y = {(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
-        *(bf16x4*)(o + ((int64_t)(u.q0 + r / group) * H + head * group + r % group) * D + piece * 4) = y;
-      } else {
-        *(f32x4*)(part_o + (slot + row) * D + piece * 4) = x;
-      }
-    }
-    if (wave == 0 && g == 0 && u.m0 + m < m1) {
-      if (!whole) part_stat[slot + m] = f32x4{ref_all * scale_log2e, l_all, e_all, 0.0f};
-      else if (STATS) lse[(int64_t)token * H + q_of] = row_statistic(ref_all * scale_log2e, e_all);
-    }
+// Single tokens: units of 16 rows.
+template <int D, bool STATS, int WAVES, bool FAR>
+__global__ __launch_bounds__(WAVES * 64, kSimdWaves) void paged4_few_kernel(const Paged4Call p) {
+  __shared__ __attribute__((aligned(1024))) char v_lds[WAVES][8192];
+  __shared__ f32x4 stat_lds[WAVES][16];
+  __shared__ PagedLds line_lds;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const PagedBatch batch = {p.q_start, p.kv_len, p.n_seq, p.n_tokens, p.H / p.Hkv, p.max_pages * p.page_size, p.most};
+  typedef PagedLine<kFewRows, kTileKeys, paged4_pad(kFewRows, WAVES)> Line;
+  const Line line(batch, &line_lds, wave, WAVES);
+  Share<Line, kFewRows> share(p, line);
+  PagedUnit u;
+  int t0, t1;
+  while (share.next(p, line, u, t0, t1)) {
+    const size_t slot = (2 * (size_t)share.wg + (t0 == 0 ? 2 : 1)) * kFewRows;
+    few_rows<D, STATS, WAVES, FAR>(p, u, share.head, u.m0, t0, t1, t0 == 0 && t1 == u.places, slot, wave, [&](int w) { return v_lds[w]; }, stat_lds);
     __syncthreads();   // (the next tiles take the place of the sums)
   }
 }
 
-template <int D, int WAVES, bool FAR>
-hipError_t launch_as(const void* q, void* o, const Codes& cache, const da_paged& p, float scale, void* scratch, const PagedLaunch& l, hipStream_t stream) {
-  const float scale_log2e = scale * 1.4426950408889634f;
-  const PagedScratch at(scratch, l.workgroups, kRows4, D);
-  hipLaunchKernelGGL((p.lse_out ? paged4_kernel<D, true, WAVES, FAR> : paged4_kernel<D, false, WAVES, FAR>), dim3((unsigned)l.workgroups), dim3(WAVES * 64), 0, stream,
-                     (const bf16*)q, cache, (bf16*)o, p.page_table, p.q_start, p.kv_len, p.lse_out, p.H, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size,
-                     p.max_pages, p.q_stride[0], p.q_stride[1], p.causal, scale_log2e, l.ranges, l.least, l.most, at.sums, at.stats, at.cuts);
+// Chunks and mixed batches: units of 128 rows. WAVES: 8, one workgroup a compute unit; 4: two, one beginning or ending its units beside the others' walks.
+template <int D, bool STATS, int WAVES, bool FAR>
+__global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4Call p) {
+  constexpr int ROWS = kUnitRows, BC = kTileKeys, ROWB = D * 2, TILEB = BC * ROWB;
+  constexpr int MB = BC / 32, TT = BC / 16, KSTEPS = D / 16, NMB = D / 32, WORDS = D / 32;
+  constexpr float kSumTrigger = (BC / 2) * 256.0f;   // (as in attn_bf16_impl.h)
+  constexpr int HALVES = WAVES == 2 * kRW ? 2 : 1, BUFB = HALVES * TILEB;
+  static_assert(BUFB >= WAVES / 4 * 8192, "room for the waves' tiles with few rows");
+  __shared__ __attribute__((aligned(1024))) char k_lds0[BUFB];
+  __shared__ __attribute__((aligned(1024))) char k_lds1[BUFB];
+  __shared__ __attribute__((aligned(1024))) char v_lds0[BUFB];
+  __shared__ __attribute__((aligned(1024))) char v_lds1[BUFB];
+  __shared__ f32x4 stat_lds[WAVES][16];
+  __shared__ PagedLds line_lds;
+
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % kRW, half = HALVES == 1 ? 0 : wave / kRW;
+  const int group = p.H / p.Hkv;
+  const PagedBatch batch = {p.q_start, p.kv_len, p.n_seq, p.n_tokens, group, p.max_pages * p.page_size, p.most};
+  auto k_buf = [&](int par) -> char* { return (par ? k_lds1 : k_lds0) + half * TILEB; };
+  auto v_buf = [&](int par) -> char* { return (par ? v_lds1 : v_lds0) + half * TILEB; };
+  auto few_buf = [&](int w) -> char* {   // 8 KB of a wave's own
+    constexpr int EACH = WAVES / 4;
+    char* const from = w / EACH == 0 ? k_lds0 : w / EACH == 1 ? k_lds1 : w / EACH == 2 ? v_lds0 : v_lds1;
+    return from + w % EACH * 8192;
+  };
+  typedef PagedLine<ROWS, BC, paged4_pad(ROWS, WAVES)> Line;
+  const Line line(batch, &line_lds, wave, WAVES);
+  Share<Line, ROWS> share(p, line);
+  PagedUnit u;
+  int t0, t1;
+  while (share.next(p, line, u, t0, t1)) {
+    const int head = share.head;
+    const bool whole = t0 == 0 && t1 == u.places;
+    const size_t slot0 = (2 * (size_t)share.wg + (t0 == 0 ? 2 : 1)) * ROWS;
+    const int unit_end = min(u.m0 + ROWS, u.rows);
+    bool few = u.rows - u.m0 <= 32;
+    if (!few) {
+      const int lane = here(tid) & 63, lq = lane & 31, hh = lane >> 5;
+      const int n_keys = min(u.len, batch.max_keys);
+      const int* table = p.page_table + (int64_t)u.seq * p.max_pages;
+      const int n_seen = p.causal ? min(n_keys, max(u.len - u.nq + (unit_end - 1) / group + 1, 0)) : n_keys;   // no row sees more
+      const int all_see = p.causal ? min(max(u.len - u.nq + u.m0 / group + 1, 0), n_keys) : n_keys;   // keys below this every row sees
+      const int m = u.m0 + rw * 32 + lq, m_ld = min(m, u.rows - 1);   // this lane's row (surplus rows: a valid one, never stored)
+      const int token = u.q0 + m_ld / group, q_of = head * group + m_ld % group;
+      const int lim = min(p.causal ? u.len - u.nq + m_ld / group : n_keys - 1, n_keys - 1);   // last key this row sees
+      const int seen_tiles = (n_seen + BC - 1) / BC;
+      // the halves' tiles; a half without any walks one behind the last key: zeros, masked out
+      const int n_all = max(min(t1, seen_tiles) - t0, 0), n_most = max((n_all + HALVES - 1) / HALVES, 1);
+      const int n_tiles = half ? max(n_all - n_most, 1) : n_most;
+      const int tile0 = half ? (n_all > 1 ? t0 + n_most : seen_tiles) : (n_all > 0 ? t0 : seen_tiles);
+      const bool idle = u.m0 + rw * 32 >= u.rows;   // a wave without rows brings its part of the tiles in
+
+      bf16x8 qop[KSTEPS];
+      {
+        const bf16* q_row = p.q + token * p.q_token + q_of * p.q_head;
+#pragma unroll
+        for (int s = 0; s < KSTEPS; ++s) qop[s] = *(const bf16x8*)(q_row + 16 * s + 8 * hh);
+      }
+
+      // Lane i: where the wave's 16 keys of tile (first + i) of the half lie, and which of the tile's groups lie in the cache.
+      struct Window {
+        uint32_t code, scale;
+        int there;
+      };
+      auto window_of = [&](int first) {
+        Window w = {0, 0, 0};
+        const int key = (tile0 + first + lane) * BC;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = key + 16 * i, page = at < n_seen ? table[(unsigned)at / (unsigned)p.page_size] : -1;
+          CodeWindow c;
+          c.template place<FAR>(page, at % (unsigned)p.page_size, p.n_pages, p.cache);
+          w.there |= (page >= 0 && page < p.n_pages ? 1 : 0) << i;
+          if (i == rw) {
+            w.code = c.code;
+            w.scale = c.scale;
+          }
+        }
+        return w;
+      };
+      // Two windows, the second from the middle of the first on; it takes the first's place when that half is done with.
+      int base;
+      Window now, next;
+      auto advance = [&](int it) {   // tiles before `it` are done with: those up to it + 31 lie in the window from here on
+        if (it < base + 32) return;
+        base += 32;
+        now = next;
+        next = window_of(base + 32);
+      };
+      auto there_of = [&](int it) { return __builtin_amdgcn_readlane(now.there, it - base); };
+      const std::true_type yes;
+      const std::false_type no;
+
+      const int vr = lane >> 2, vp = lane & 3;   // row of the wave's 16 and quarter of it that the lane brings
+      const int code_at = vr * p.cache.code_row + vp * (D / 8), scale_at = vr * p.cache.scale_row + vp * (D / 4) / 32;
+      const uint8_t* k_codes = p.cache.k_codes + head * p.cache.code_head;
+      const uint8_t* v_codes = p.cache.v_codes + head * p.cache.code_head;
+      const uint8_t* k_scales = p.cache.k_scales + head * p.cache.scale_head;
+      const uint8_t* v_scales = p.cache.v_scales + head * p.cache.scale_head;
+      Quarter<D> k_ahead, v_ahead;   // of the tiles whose turn is next
+      auto ask = [&](Quarter<D>& to, const uint8_t* codes, const uint8_t* scales, int it) {
+        const int a = __builtin_amdgcn_readlane((int)now.code, it - base), b = __builtin_amdgcn_readlane((int)now.scale, it - base);
+        to.load(codes, scales, FAR ? (uint64_t)(a * p.cache.code_page + (int64_t)b * p.cache.code_row) : (uint64_t)(uint32_t)a,
+                FAR ? (uint64_t)(a * p.cache.scale_page + (int64_t)b * p.cache.scale_row) : (uint64_t)(uint32_t)b, code_at, scale_at);
+      };
+      auto ask_k = [&](int it) { ask(k_ahead, k_codes, k_scales, it); };
+      auto ask_v = [&](int it) { ask(v_ahead, v_codes, v_scales, it); };
+      auto put_k = [&](int par) {
+        char* const to = k_buf(par) + (16 * rw + vr) * ROWB;
+        k_ahead.store([&](int j) { return to + (k_piece<D>(vr, vp * WORDS + j) << 4); }, false);
+      };
+      auto put_v = [&](int it, int par) {   // rows that none of the unit's sees: zeros
+        char* const to = v_buf(par) + (16 * rw + vr) * ROWB;
+        const bool hidden = (tile0 + it) * BC + 16 * rw + vr >= n_seen || !(there_of(it) >> rw & 1);
+        v_ahead.store([&](int j) { return to + (v_piece<D>(vr, vp * WORDS + j) << 4); }, hidden);
+      };
+      // What tile `it` brings in: K(it + 2) where K(it) was, V(it + 1) where V(it - 1) was; and the codes of the next ones.
+      auto feed = [&](int it, int par) {
+        put_k(par);
+        put_v(it + 1, par ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+        ask_k(it + 3);
+        ask_v(it + 2);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto masked = [&](int it) { return (tile0 + it) * BC + BC > all_see || there_of(it) != 15; };
+
+      f32x16 oacc[NMB];
+      float nref, l_run, e_run;   // negated reference (exp2 domain), sums over this lane's half of the keys
+      float trigger;              // below zero until the row has met a score above -infinity: its first one becomes the reference
+      const int ka = lq * ROWB + (k_piece<D>(lq, hh) << 4);
+      const int row_l = 4 * hh + ((lane & 15) >> 2);
+      const int va = row_l * ROWB + (v_piece<D>(row_l, (lane >> 4 & 1) << 1 | (lane & 3) >> 1) << 4) + 8 * (lane & 1);
+      auto v_operand = [&](const char* tile, int tt, int mb) {
+        const char* p0 = tile + (va ^ (v_piece<D>(0, 4 * mb) << 4)) + 16 * tt * ROWB;
+        return lds_read_tr_pair<bf16x8>(p0, p0 + 8 * ROWB);
+      };
+
+      auto qk = [&](int par, f32x16 (&sacc)[MB]) {
+        const char* at = k_buf(par);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sacc[mb][i] = 0.0f;
+#pragma unroll
+          for (int s = 0; s < KSTEPS; ++s)
+            sacc[mb] = mfma_32x32x16(*(const bf16x8*)(at + (ka ^ (k_piece<D>(0, 2 * s) << 4)) + mb * 32 * ROWB), qop[s], sacc[mb]);
+        }
+      };
+      auto apply_mask = [&](int it, f32x16 (&sc)[MB]) {
+        const int there = there_of(it), past = here(lim - (tile0 + it) * BC - 4 * hh);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (32 * mb + 8 * (i >> 2) + (i & 3) > past || !(there >> (2 * mb + (i >> 3)) & 1)) sc[mb][i] = -INFINITY;
+      };
+      auto tile_max = [&](const f32x16 (&sc)[MB]) -> float {
+        float mt = sc[0][0];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[mb][i]);
+        return __builtin_fmaf(half_swap_max(mt), p.scale_log2e, nref);
+      };
+      auto exp_tile = [&](const f32x16 (&sc)[MB], bf16x8 (&pop)[TT]) -> float {   // -> sum before rounding, with STATS
+        float sum = 0.0f;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            const float x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i], p.scale_log2e, nref));
+            const float x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mb][i + 1], p.scale_log2e, nref));
+            const bf16x2 pr = {(bf16)x0, (bf16)x1};
+            pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
+            pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
+            if constexpr (STATS) sum += x0 + x1;
+          }
+        return sum;
+      };
+      const RowSum row_sum(lane);
+      auto shift_reference = [&](float delta) {
+        nref -= delta;
+        const float alpha = __builtin_amdgcn_exp2f(fminf(-delta, 0.0f));   // (a first reference has no sums)
+        l_run *= alpha;
+        if constexpr (STATS) e_run *= alpha;
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mb][i] *= alpha;
+      };
+      // One tile, as in attn_bf16_impl.h. clean_c: neither it nor the next needs the mask.
+      auto body = [&](auto clean_c, auto next_c, int it, int par, f32x16 (&sc)[MB], f32x16 (&sn)[MB]) {
+        constexpr bool CLEAN = decltype(clean_c)::value, HAS_NEXT = decltype(next_c)::value;
+        if constexpr (HAS_NEXT) {
+          feed(it, par);
+          qk(par ^ 1, sn);
+        }
+        bf16x8 pop[TT];
+        float es = exp_tile(sc, pop);
+        float rs = row_sum(pop);
+        if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
+          const float mt = tile_max(sc);
+          const bool first = trigger < 0.0f && mt > -INFINITY;
+          if (first) trigger = kSumTrigger;
+          shift_reference(mt > kLift || first ? mt : 0.0f);
+          es = exp_tile(sc, pop);
+          rs = RowSum::by_lanes(pop);
+        }
+        l_run += rs;
+        if constexpr (STATS) e_run += es;
+        const char* vb = v_buf(par);
+        {
+          constexpr int PF = (4 / NMB < TT) ? 4 / NMB : TT - 1;
+          bf16x8 va[PF + 1][NMB];
+#pragma unroll
+          for (int s = 0; s < PF; ++s)
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) va[s][mb] = v_operand(vb, s, mb);
+#pragma unroll
+          for (int tt = 0; tt < TT; ++tt) {
+            if (tt + PF < TT) {
+#pragma unroll
+              for (int mb = 0; mb < NMB; ++mb) va[(tt + PF) % (PF + 1)][mb] = v_operand(vb, tt + PF, mb);
+            }
+#pragma unroll
+            for (int mb = 0; mb < NMB; ++mb) oacc[mb] = mfma_32x32x16(va[tt % (PF + 1)][mb], pop[tt], oacc[mb]);
+          }
+        }
+        if constexpr (!CLEAN) {   // (the wait behind these products as in attn_bf16_few.hip)
+          __builtin_amdgcn_sched_barrier(0);
+          asm volatile("s_nop 3");
+        }
+        if constexpr (HAS_NEXT && !CLEAN) {
+          if (masked(it + 1)) apply_mask(it + 1, sn);
+        }
+        lds_barrier();
+      };
+
+#pragma unroll
+      for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[mb][i] = 0.0f;
+      nref = l_run = e_run = 0.0f;
+      trigger = kSumTrigger;
+      base = 0;
+      now = window_of(0);
+      next = window_of(32);
+      ask_k(0);
+      ask_v(0);
+      put_k(0);
+      put_v(0, 0);
+      ask_k(1);
+      put_k(1);
+      ask_k(2);
+      ask_v(1);
+      __syncthreads();
+      if (idle) {
+        lds_barrier();
+        for (int it = 0; it < n_tiles - 1; ++it) {
+          advance(it);
+          feed(it, it & 1);
+          lds_barrier();
+        }
+        lds_barrier();
+      } else {
+        f32x16 s0[MB], s1[MB];
+        qk(0, s0);
+        if (masked(0)) apply_mask(0, s0);
+        const float first_max = tile_max(s0);
+        if (first_max > -INFINITY) nref -= first_max;
+        else trigger = -1.0f;
+        lds_barrier();
+        const int n_full = min(max(all_see / BC - tile0, 0), n_tiles);   // tiles that need no mask for their place
+        int it = 0;
+        while (it < n_tiles - 1) {
+          advance(it);
+          if ((it & 1) == 0) {
+            // clean tiles of the window from `it` on
+            const uint64_t bad = __builtin_amdgcn_ballot_w64(now.there != 15) >> (it - base);
+            const int clean = min(min(n_full, it + (bad ? __builtin_ctzll(bad) : 64)), base + 60);   // (four tiles ahead are looked up)
+            if (it + 2 < clean) {
+              do {
+                body(yes, yes, it, 0, s0, s1);
+                body(yes, yes, it + 1, 1, s1, s0);
+                __builtin_amdgcn_sched_barrier(0);   // (as above, for the way out of this loop)
+                asm volatile("s_nop 3");
+                it += 2;
+              } while (it + 2 < clean);
+              continue;
+            }
+          }
+          body(no, yes, it, it & 1, s0, s1);
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) s0[mb] = s1[mb];
+          ++it;
+        }
+        advance(it);
+        body(no, no, it, it & 1, s0, s1);
+      }
+      if (HALVES == 2 && n_tiles < n_most) lds_barrier();   // (the other half's last tile)
+      // Where some rows do not see all keys of a tile, an infinity or a NaN among its values reaches their sums (0 times it). Sums that are no
+      // numbers have the unit's rows taken again as few rows, which looks at the values of such tiles.
+      if (n_seen > all_see) {
+        float odd = 0.0f;
+#pragma unroll
+        for (int mb = 0; mb < NMB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(oacc[mb][i], 0.0f, odd);
+        few = __syncthreads_or(odd != 0.0f);   // (NaN is)
+      }
+      if (!few) {
+        // ---- the halves meet: each hands the other one half of the channels and finishes the rest ----------------
+        constexpr int OB = NMB / HALVES;
+        const int c0 = HALVES == 2 ? half * (D / 2) : 0;
+        float l_tot = half_swap_sum(l_run), e_tot = STATS ? half_swap_sum(e_run) : 0.0f;
+        float ref = -nref;
+        f32x16 out[OB];
+        if constexpr (HALVES == 2) {
+          static_assert(kRW * OB * 4096 <= BUFB && WAVES * 512 <= BUFB, "the exchange fits the tile buffers");
+          f32x4* stat = (f32x4*)k_lds0;
+          f32x4* give = (f32x4*)(half ? v_lds1 : v_lds0) + rw * (OB * 256) + lane;
+          const f32x4* take = (const f32x4*)(half ? v_lds0 : v_lds1) + rw * (OB * 256) + lane;
+          if (hh == 0) stat[wave * 32 + lq] = f32x4{-nref, l_tot, e_tot, 0.0f};
+#pragma unroll
+          for (int mb = 0; mb < OB; ++mb) {
+            f32x16 theirs;
+            if (half) {
+              theirs = oacc[mb];
+              out[mb] = oacc[mb + OB];
+            } else {
+              theirs = oacc[mb + OB];
+              out[mb] = oacc[mb];
+            }
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) give[(mb * 4 + i4) * 64] = f32x4{theirs[4 * i4], theirs[4 * i4 + 1], theirs[4 * i4 + 2], theirs[4 * i4 + 3]};
+          }
+          __syncthreads();
+          // (a half that saw nothing of a row has sum 0 and no reference; a NaN sum makes the row NaN)
+          const f32x4 st = stat[(wave ^ kRW) * 32 + lq];
+          const float mine_ref = l_tot == 0.0f ? -FLT_MAX : -nref, other_ref = st[1] == 0.0f ? -FLT_MAX : st[0];
+          ref = fmaxf(mine_ref, other_ref);
+          const float wm = __builtin_amdgcn_exp2f(mine_ref - ref), wo = __builtin_amdgcn_exp2f(other_ref - ref);
+          l_tot = __builtin_fmaf(wm, l_tot, wo * st[1]);
+          e_tot = __builtin_fmaf(wm, e_tot, wo * st[2]);
+#pragma unroll
+          for (int mb = 0; mb < OB; ++mb)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+              const f32x4 x = take[(mb * 4 + i4) * 64];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) out[mb][4 * i4 + j] = __builtin_fmaf(wm, out[mb][4 * i4 + j], wo * x[j]);
+            }
+        } else {
+          if (l_tot == 0.0f) ref = -FLT_MAX;   // (as above, for the unit's other parts: a row that saw nothing has no reference)
+#pragma unroll
+          for (int mb = 0; mb < OB; ++mb) out[mb] = oacc[mb];
+        }
+        const float inv = !whole ? 1.0f : l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
+        if (m < u.rows) {
+          const int64_t row = (int64_t)token * p.H + q_of;
+          const size_t slot = slot0 + rw * 32 + lq;
+          if (hh == 0 && half == 0) {
+            if (!whole) p.part_stat[slot] = f32x4{ref, l_tot, e_tot, 0.0f};
+            else if (STATS) p.lse[row] = row_statistic(ref, e_tot);
+          }
+#pragma unroll
+          for (int mb = 0; mb < OB; ++mb)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) {
+              const int c = c0 + 32 * mb + 8 * i4 + 4 * hh;
+              const f32x4 x = f32x4{out[mb][4 * i4], out[mb][4 * i4 + 1], out[mb][4 * i4 + 2], out[mb][4 * i4 + 3]} * inv;
+              if (whole) *(bf16x4*)(p.o + row * D + c) = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+              else *(f32x4*)(p.part_o + slot * D + c) = x;
+            }
+        }
+      }
+      __syncthreads();   // (the next unit's tiles take the place of the sums)
+    }
+    if (few) {
+      for (int m0 = u.m0; m0 < unit_end; m0 += kFewRows) {
+        few_rows<D, STATS, WAVES, FAR>(p, u, head, m0, t0, t1, whole, slot0 + (m0 - u.m0), wave, few_buf, stat_lds);
+        __syncthreads();
+      }
+    }
+  }
+}
+
+template <int D, int ROWS, int WAVES, bool FAR>
+hipError_t launch_as(Paged4Call call, void* scratch, const PagedLaunch& l, hipStream_t stream) {
+  const PagedScratch at(scratch, l.workgroups, ROWS, D);
+  call.ranges = l.ranges;
+  call.least = l.least;
+  call.most = l.most;
+  call.part_o = at.sums;
+  call.part_stat = at.stats;
+  call.cuts = at.cuts;
+  const dim3 grid((unsigned)l.workgroups), block(WAVES * 64);
+  if constexpr (ROWS == kFewRows) {
+    if (call.lse) hipLaunchKernelGGL((paged4_few_kernel<D, true, WAVES, FAR>), grid, block, 0, stream, call);
+    else hipLaunchKernelGGL((paged4_few_kernel<D, false, WAVES, FAR>), grid, block, 0, stream, call);
+  } else {
+    if (call.lse) hipLaunchKernelGGL((paged4_rows_kernel<D, true, WAVES, FAR>), grid, block, 0, stream, call);
+    else hipLaunchKernelGGL((paged4_rows_kernel<D, false, WAVES, FAR>), grid, block, 0, stream, call);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !l.ranges) return e;
-  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, kRows4>), dim3((unsigned)(l.workgroups * (kRows4 * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
-                     at.cuts, (bf16*)o, p.lse_out, p.H, p.Hkv);
+  hipLaunchKernelGGL((paged_combine_kernel<bf16, D, ROWS>), dim3((unsigned)(l.workgroups * (ROWS * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
+                     at.cuts, call.o, call.lse, call.H, call.Hkv);
   return hipGetLastError();
 }
 
+struct Paged4Form {
+  int rows, waves;   // of a unit, of a workgroup
+  PagedLaunch launch;
+};
+Paged4Form paged4_form(const da_paged& p, size_t scratch_bytes) {
+  const int group = p.H / p.Hkv;
+  const long long heads = (long long)p.n_seq * p.Hkv, full = (long long)p.n_tokens * group / kUnitRows * p.Hkv;
+  auto form = [&](int rows, int waves, int from) {
+    PagedLaunch l = paged_launch(p, rows, kTileKeys, paged4_pad(rows, waves), 4 * kSimdWaves * kComputeUnits / waves, from, scratch_bytes);
+    if (l.ranges) {
+      l.ranges = l.workgroups / p.Hkv;
+      const int whole = 8 / std::gcd(8, p.Hkv);   // of a number of workgroups that the XCDs share evenly
+      if (l.ranges > 16 * whole) l.ranges -= l.ranges % whole;
+      if (l.ranges < 2) l.ranges = 0;
+      l.workgroups = l.ranges ? l.ranges * p.Hkv : (int)(paged_units(p, rows) * p.Hkv);
+    }
+    return Paged4Form{rows, waves, l};
+  };
+  if (p.n_tokens <= p.n_seq && group <= 2 * kFewRows) return form(kFewRows, heads <= kComputeUnits ? 8 : 4, 20);
+  if (full > kComputeUnits) return Paged4Form{kUnitRows, 4, PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, 0, 0}};
+  return form(kUnitRows, heads > kComputeUnits ? 4 : 8, 16 + (int)std::min(std::max(heads, full), (long long)kComputeUnits) / 6);
+}
+
 template <int D>
-hipError_t launch_d(const void* q, void* o, const Codes& cache, bool far, const da_paged& p, float scale, void* scratch, size_t scratch_bytes, hipStream_t stream) {
-  const long long units = (long long)p.n_seq * p.Hkv;   // that there are about
-  const int waves = !far && units > kComputeUnits ? 4 : 8;
-  PagedLaunch l = paged_launch(p, kRows4, kKeys4, paged4_pad(waves), 4 * kSimdWaves * kComputeUnits / waves, 20, scratch_bytes);
-  if (l.ranges) {
-    l.ranges = l.workgroups / p.Hkv;
-    const int whole = 8 / std::gcd(8, p.Hkv);   // of a number of workgroups that the XCDs share evenly
-    if (l.ranges > 16 * whole) l.ranges -= l.ranges % whole;
-    if (l.ranges < 2) l.ranges = 0;
-    l.workgroups = l.ranges ? l.ranges * p.Hkv : (int)(paged_units(p, kRows4) * p.Hkv);
-  }
-  return (far ? launch_as<D, 8, true> : waves == 8 ? launch_as<D, 8, false> : launch_as<D, 4, false>)(q, o, cache, p, scale, scratch, l, stream);
+hipError_t launch_d(const Paged4Call& call, bool far, const da_paged& p, void* scratch, size_t scratch_bytes, hipStream_t stream) {
+  const Paged4Form f = paged4_form(p, scratch_bytes);
+  const auto launch = f.rows == kFewRows ? (f.waves == 8 ? (far ? launch_as<D, kFewRows, 8, true> : launch_as<D, kFewRows, 8, false>)
+                                                         : (far ? launch_as<D, kFewRows, 4, true> : launch_as<D, kFewRows, 4, false>))
+                                         : (f.waves == 8 ? (far ? launch_as<D, kUnitRows, 8, true> : launch_as<D, kUnitRows, 8, false>)
+                                                         : (far ? launch_as<D, kUnitRows, 4, true> : launch_as<D, kUnitRows, 4, false>));
+  return launch(call, scratch, f.launch, stream);
 }
 
 }  // namespace
 
 size_t paged4_scratch_bytes(const da_paged& p) {
-  return p.dtype == DA_F32 ? paged4_f32_scratch_bytes(p) : paged_launch_bytes(kSimdWaves * kComputeUnits, kRows4, p.d);
+  return p.dtype == DA_F32 ? paged4_f32_scratch_bytes(p) : paged_launch_bytes(kSimdWaves * kComputeUnits, kUnitRows, p.d);
 }
 
 hipError_t launch_paged4(const void* q, void* o, const da_cache4& c, const da_paged& p, float scale, void* scratch, size_t scratch_bytes, hipStream_t stream) {
@@ -391,7 +577,26 @@ hipError_t launch_paged4(const void* q, void* o, const da_cache4& c, const da_pa
   // whether a kv head's pages reach farther than offsets of 31 bits
   auto reaches = [&](const int64_t* stride) { return (p.n_pages - 1) * (double)stride[0] + (p.page_size - 1) * (double)stride[2] + p.d > 2e9; };
   const bool far = reaches(c.code_stride) || reaches(c.scale_stride);
-  return p.d == 64 ? launch_d<64>(q, o, cache, far, p, scale, scratch, scratch_bytes, stream) : launch_d<128>(q, o, cache, far, p, scale, scratch, scratch_bytes, stream);
+  Paged4Call call = {};
+  call.q = (const bf16*)q;
+  call.cache = cache;
+  call.o = (bf16*)o;
+  call.page_table = p.page_table;
+  call.q_start = p.q_start;
+  call.kv_len = p.kv_len;
+  call.lse = p.lse_out;
+  call.H = p.H;
+  call.Hkv = p.Hkv;
+  call.n_seq = p.n_seq;
+  call.n_tokens = p.n_tokens;
+  call.n_pages = p.n_pages;
+  call.page_size = p.page_size;
+  call.max_pages = p.max_pages;
+  call.q_token = p.q_stride[0];
+  call.q_head = p.q_stride[1];
+  call.causal = p.causal;
+  call.scale_log2e = scale * 1.4426950408889634f;
+  return p.d == 64 ? launch_d<64>(call, far, p, scratch, scratch_bytes, stream) : launch_d<128>(call, far, p, scratch, scratch_bytes, stream);
 }
 
 }  // namespace da

@@ -345,8 +345,10 @@ def test_nan_in_keys_and_values(d, dtype, new):
             assert torch.equal(o[row].isnan(), want), (s, i)
             assert torch.equal(lse[row].isnan(), torch.tensor([False, False] + [s == 0 and place >= n - 3] * 2))
     clean = Batch4([n, n], [new, new], 4, 2, d, dtype, page=32)
-    want, _ = _attention(clean)
-    assert torch.equal(torch.where(o.isnan(), 0, o), torch.where(o.isnan(), 0, want))   # what is no NaN is as without it
+    want, want_lse = _attention(clean)
+    # What is no NaN is what it is without it. Rows beside a NaN may be walked otherwise, their sums taken in another order: not the same bits, but
+    # within the bounds of the definition, as any order is.
+    _check(clean, torch.where(o.isnan(), want, o), torch.where(lse.isnan(), want_lse, lse), rows_of=[0, 1, 20, 36, 37, 38, 39])
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
