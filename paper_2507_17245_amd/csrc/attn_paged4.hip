@@ -15,6 +15,7 @@ namespace da {
 
 namespace {
 
+// Places of the line: a tile of a unit of 128 rows takes 2600 cycles where its keys come from memory, one of few rows 410: four of them are one place.
 constexpr int kUnitRows = 128, kFewRows = 16, kTileKeys = 64, kRW = 4;   // rows and keys of the line's units and tiles, waves over the rows
 constexpr int paged4_pad(int rows, int waves) { return rows != kFewRows ? 8 : waves == 8 ? 6 : 3; }
 constexpr int kSimdWaves = 2;   // (2 | 3, us: 64 sequences of up to 8192 d64 47.4 | 48.3, 200 of up to 2500 d128 79.6 | 86: registers, and more parts to join)
@@ -63,11 +64,11 @@ struct Share {
   int wg = blockIdx.x, head = 0;
   __device__ Share(const Paged4Call& p, const LINE& line) {
     if (!p.ranges) return;
-    // Every kv head's line is cut into the same `ranges` ones; those of one place in the line follow each other on one XCD, whose L2 then has the lines of
-    // 128 bytes that several heads' scales (or, tokens outside, codes) lie in.
+    // Every kv head's line is cut into the same `ranges` ones. What follows each other here lies on one XCD: with few rows those of one place in the lines, as
+    // several heads' scales (and, tokens outside, codes) lie in one line of 128 bytes; with units of 128 rows those of one head, which read the same keys.
     if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
-    const int part = wg / p.Hkv;
-    head = wg % p.Hkv;
+    const int part = ROWS == kFewRows ? wg / p.Hkv : wg % p.ranges;
+    head = ROWS == kFewRows ? wg % p.Hkv : wg / p.ranges;
     wg = head * p.ranges + part;
     const unsigned length = paged_range(line.total, p.ranges, p.least);
     pos = paged_cut(line, part, length, line.total);
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
     char* const from = w / EACH == 0 ? k_lds0 : w / EACH == 1 ? k_lds1 : w / EACH == 2 ? v_lds0 : v_lds1;
     return from + w % EACH * 8192;
   };
-  typedef PagedLine<ROWS, BC, paged4_pad(ROWS, WAVES)> Line;
+  typedef PagedLine<ROWS, BC, paged4_pad(ROWS, WAVES), 2 * kFewRows> Line;
   const Line line(batch, &line_lds, wave, WAVES);
   Share<Line, ROWS> share(p, line);
   PagedUnit u;
@@ -154,7 +155,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
     const bool whole = t0 == 0 && t1 == u.places;
     const size_t slot0 = (2 * (size_t)share.wg + (t0 == 0 ? 2 : 1)) * ROWS;
     const int unit_end = min(u.m0 + ROWS, u.rows);
-    bool few = u.rows - u.m0 <= 32;
+    const int few_tiles = u.rows <= 2 * kFewRows ? kFewTiles : 1;   // of a place
+    bool few = u.rows - u.m0 <= 2 * kFewRows;
     if (!few) {
       const int lane = here(tid) & 63, lq = lane & 31, hh = lane >> 5;
       const int n_keys = min(u.len, batch.max_keys);
@@ -186,9 +188,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
       auto window_of = [&](int first) {
         Window w = {0, 0, 0};
         const int key = (tile0 + first + lane) * BC;
+        int pages[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pages[i] = table[(unsigned)max(min(key + 16 * i, n_seen - 1), 0) / (unsigned)p.page_size];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int at = key + 16 * i, page = at < n_seen ? table[(unsigned)at / (unsigned)p.page_size] : -1;
+          const int at = key + 16 * i, page = at < n_seen ? pages[i] : -1;
           CodeWindow c;
           c.template place<FAR>(page, at % (unsigned)p.page_size, p.n_pages, p.cache);
           w.there |= (page >= 0 && page < p.n_pages ? 1 : 0) << i;
@@ -226,9 +231,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
       };
       auto ask_k = [&](int it) { ask(k_ahead, k_codes, k_scales, it); };
       auto ask_v = [&](int it) { ask(v_ahead, v_codes, v_scales, it); };
-      auto put_k = [&](int par) {
+      auto put_k = [&](const Quarter<D>& from, int par) {
         char* const to = k_buf(par) + (16 * rw + vr) * ROWB;
-        k_ahead.store([&](int j) { return to + (k_piece<D>(vr, vp * WORDS + j) << 4); }, false);
+        from.store([&](int j) { return to + (k_piece<D>(vr, vp * WORDS + j) << 4); }, false);
       };
       auto put_v = [&](int it, int par) {   // rows that none of the unit's sees: zeros
         char* const to = v_buf(par) + (16 * rw + vr) * ROWB;
@@ -237,7 +242,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
       };
       // What tile `it` brings in: K(it + 2) where K(it) was, V(it + 1) where V(it - 1) was; and the codes of the next ones.
       auto feed = [&](int it, int par) {
-        put_k(par);
+        put_k(k_ahead, par);
         put_v(it + 1, par ^ 1);
         __builtin_amdgcn_sched_barrier(0);
         ask_k(it + 3);
@@ -295,7 +300,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
             const bf16x2 pr = {(bf16)x0, (bf16)x1};
             pop[mb * 2 + (i >> 3)][i & 7] = pr[0];
             pop[mb * 2 + (i >> 3)][(i & 7) + 1] = pr[1];
-            if constexpr (STATS) sum += x0 + x1;
+            if constexpr (STATS) {
+              sum += x0 + x1;
+              asm volatile("" : "+v"(sum));   // (at once: pairs that wait for their turn do not fit the registers, d = 128 with row statistics 570 -> 505 us)
+            }
           }
         return sum;
       };
@@ -367,12 +375,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
       base = 0;
       now = window_of(0);
       next = window_of(32);
-      ask_k(0);
-      ask_v(0);
-      put_k(0);
-      put_v(0, 0);
-      ask_k(1);
-      put_k(1);
+      {
+        Quarter<D> first;
+        ask(first, k_codes, k_scales, 0);
+        ask_v(0);
+        ask_k(1);
+        put_k(first, 0);
+        put_v(0, 0);
+        put_k(k_ahead, 1);
+      }
       ask_k(2);
       ask_v(1);
       __syncthreads();
@@ -500,7 +511,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
     }
     if (few) {
       for (int m0 = u.m0; m0 < unit_end; m0 += kFewRows) {
-        few_rows<D, STATS, WAVES, FAR>(p, u, head, m0, t0, t1, whole, slot0 + (m0 - u.m0), wave, few_buf, stat_lds);
+        few_rows<D, STATS, WAVES, FAR>(p, u, head, m0, t0 * few_tiles, t1 * few_tiles, whole, slot0 + (m0 - u.m0), wave, few_buf, stat_lds);
         __syncthreads();
       }
     }

@@ -63,7 +63,9 @@ struct PagedLds {   // of a workgroup
   unsigned places[64], units[64];     // of each 64 sequences, up to 4096 of them
 };
 
-template <int ROWS, int KEYS, int PAD>
+// FEW: sequences of up to so many query rows have places of kFewTiles tiles.
+constexpr int kFewTiles = 4;
+template <int ROWS, int KEYS, int PAD, int FEW = 0>
 struct PagedSequence {   // what a lane knows of its sequence
   int q0, nq, len, units, places;   // (places of a unit)
   unsigned sum, unit_sum;   // places and units of the sequences up to it, in its 64
@@ -75,7 +77,8 @@ struct PagedSequence {   // what a lane knows of its sequence
       nq = max(min(max(to, 0), b.n_tokens) - q0, 0);
       len = max(keys, 0);
       units = (int)(((unsigned)nq * (unsigned)b.group + (ROWS - 1)) / ROWS);
-      places = max((min(len, b.max_keys) + KEYS - 1) / KEYS, 1) + PAD;
+      const int keys_of = FEW > 0 && nq * b.group <= FEW ? KEYS * kFewTiles : KEYS;
+      places = max((min(len, b.max_keys) + keys_of - 1) / keys_of, 1) + PAD;
     }
     sum = wave_scan((unsigned)units * (unsigned)places);
     unit_sum = wave_scan((unsigned)units);
@@ -96,13 +99,13 @@ struct PagedSequence {   // what a lane knows of its sequence
 // take a share of, and the 64 that are asked for are loaded again; beyond, the sums are taken again, too.
 // Starts out of order may count the same tokens many times, more than 32 bits hold and than the parts of units have scratch for: sums stay at the
 // largest number then, and a line of more places than ascending starts can make is taken as empty (no range has work).
-template <int ROWS, int KEYS, int PAD>
+template <int ROWS, int KEYS, int PAD, int FEW = 0>
 struct PagedLine {
-  typedef PagedSequence<ROWS, KEYS, PAD> Sequence;
+  typedef PagedSequence<ROWS, KEYS, PAD, FEW> Sequence;
   static constexpr unsigned kPad = PAD;
   const PagedBatch b;
   PagedLds* const lds;
-  unsigned total, tiles;   // its places, those of them that are tiles
+  unsigned total, tiles;   // its places, those of them that are tiles (or kFewTiles of them)
   // (called by all threads of the workgroup)
   __device__ PagedLine(const PagedBatch& batch, PagedLds* to, int wave, int waves) : b(batch), lds(to) {
     const int lane = threadIdx.x & 63, n = (b.n_seq + 63) / 64;
