@@ -628,7 +628,7 @@ def make_paged4_params(cache, page_table, kv_len, q_start, q=None, k=None, v=Non
     p = _paged_params((*k_codes.shape[:3], d), cache, page_table, kv_len, q_start, q, k, v, causal, softmax_scale, lse_out, norm, eps, k_weight,
                       rope, cos, sin, positions, workspace)
     p.layouts["cache"] = (_layout(k_codes), _layout(k_scales))
-    p.strides = (_strides(k_codes, "codes"), _strides(k_scales, "scales"))
+    p.strides = tuple((ctypes.c_int64 * 3)(*_strides(t, what)) for t, what in ((k_codes, "codes"), (k_scales, "scales")))
     return p
 
 
@@ -638,9 +638,7 @@ def _cache4(cache, params):
     codes, scales = params.layouts["cache"]
     if _layout(k_codes) != codes or _layout(v_codes) != codes or _layout(k_scales) != scales or _layout(v_scales) != scales:
         raise ValueError("params were made for a cache of another shape, stride or device")
-    c = DaCache4(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr())
-    c.code_stride[:], c.scale_stride[:] = params.strides
-    return c
+    return DaCache4(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), *params.strides)
 
 
 def _run_cache4(name, params, k, v, cache):

@@ -53,7 +53,7 @@ struct Quarter {
   __device__ void store(AT at, bool zero) const {   // at(piece of the quarter): where it lies
     const float s = scale_value(zero ? 0 : scale);
 #pragma unroll
-    for (int j = 0; j < WORDS; ++j) *(bf16x8*)at(j) = Values8<bf16>(codes[j], s).x;
+    for (int j = 0; j < WORDS; ++j) *(bf16x8*)at(j) = values_of(codes[j], s);
   }
 };
 

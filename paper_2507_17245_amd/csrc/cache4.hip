@@ -1,7 +1,8 @@
 // New keys and values into a paged cache of 4-bit codes, and out of it again (fp4.h has the form).
 //
-// Bound: k and v and their codes, each moved once. Append: lanes as in cache_append.hip, two pieces of eight channels each; the scale of 32 channels is the
-// largest of its four pieces' (which lanes of one row hold, wherever the rotation puts them), exchanged through LDS.
+// Bound: k and v and their codes, each moved once. A workgroup takes successive rows, heads fastest; one wave finds where their tokens lie.
+// Append: lanes as in cache_append.hip, two pieces of eight channels each; the scale of 32 channels is the largest of its four pieces' (which lanes
+// of one row hold, wherever the rotation puts them), exchanged through LDS.
 // The codes are those of the exact row: with norm or rotation the row is taken in 32 bits with a bound on its error, and where a code or a scale
 // differs between the two ends of that bound (one wave of a hundred), the wave takes its rows again in 64 bits.
 // Read: a lane converts eight channels, 4 bytes to 16 or 32.
@@ -12,7 +13,7 @@ namespace da {
 
 namespace {
 
-constexpr int kThreads4 = 256;
+constexpr int kThreads4 = 256, kMostTokens4 = 64;
 
 struct Cache4 {   // strides in bytes
   uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
@@ -23,7 +24,33 @@ struct Batch4 {
   const int* __restrict__ kv_len;
   const int* __restrict__ q_start;
   int Hkv, n_seq, n_tokens, n_pages, page_size, max_pages;
+  int tokens;        // of a workgroup
+  uint32_t by_heads; // 2^32 / Hkv, rounded up: x * by_heads >> 32 is x / Hkv for x < 2^16 (several tokens to a workgroup)
 };
+
+// Where the workgroup's tokens lie.
+struct Places4 {
+  int at[kMostTokens4];   // place in the sequence; -1: none in the cache
+  int64_t code[kMostTokens4], scale[kMostTokens4];
+  __device__ void find(const Cache4& cache, const Batch4& b, int first) {   // of the tokens from `first` on
+    if (threadIdx.x < 64) {
+      const int token = min(first + (int)threadIdx.x, b.n_tokens - 1);
+      const bool real = first + (int)threadIdx.x < b.n_tokens;
+      const TokenPlace place(token, real, b.q_start, b.kv_len, b.page_table, b.n_seq, b.page_size, b.max_pages);
+      const bool is = real && place.page >= 0 && place.page < b.n_pages;
+      const int row = is ? place.at % (unsigned)b.page_size : 0, page = is ? place.page : 0;
+      at[threadIdx.x] = is ? place.at : -1;
+      code[threadIdx.x] = page * cache.code_page + row * cache.code_row;
+      scale[threadIdx.x] = page * cache.scale_page + row * cache.scale_row;
+    }
+    __syncthreads();
+  }
+};
+// Row `pair` of the workgroup's: its token there and its head.
+__device__ inline void row_of(const Batch4& b, unsigned pair, int& token, int& head) {
+  token = b.tokens == 1 ? 0 : (int)__umulhi(pair, b.by_heads);
+  head = (int)pair - token * b.Hkv;
+}
 
 template <int LPR>
 __device__ inline double row_sum(double x) {
@@ -32,19 +59,27 @@ __device__ inline double row_sum(double x) {
   return x;
 }
 
-// The row in 64 bits: x as loaded, w its weights (norm), t its angles (turn).
-template <int LPR, int ROPE>
-__device__ inline void exact_row(double (&y)[16], const float (&x)[16], const float (&w)[16], const Angles& t, bool norm, float eps, bool turn) {
-  double rms = 1.0;
-  if (norm) {
+// A lane's sixteen channels of a row in 64 bits; weights and angles are loaded again.
+template <typename E, int D, int ROPE>
+__device__ inline void exact_row(double (&y)[16], const Eight<E> (&row)[2], const void* weight, const Rotary& r, int head, const LanePlace<ROPE>& at, int pos) {
+  constexpr int LPR = D / 16;
+  float x[16];
+  row[0].values(x);
+  row[1].values(x + 8);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) y[j] = (double)x[j];
+  if (r.norm) {
     double s = 0.0;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) s += (double)x[j] * (double)x[j];
-    rms = 1.0 / __builtin_sqrt(row_sum<LPR>(s) * (1.0 / (16 * LPR)) + (double)eps);
-  }
+    for (int j = 0; j < 16; ++j) s += y[j] * y[j];
+    const double rms = 1.0 / __builtin_sqrt(row_sum<LPR>(s) * (1.0 / (16 * LPR)) + (double)r.eps);
+    load_weight<D>(x, weight, r, head, at);
 #pragma unroll
-  for (int j = 0; j < 16; ++j) y[j] = norm ? (double)x[j] * rms * (double)w[j] : (double)x[j];
-  if (turn) {
+    for (int j = 0; j < 16; ++j) y[j] = y[j] * rms * (double)x[j];
+  }
+  if (at.turn) {
+    Angles t;
+    t.load(r, pos, at.pair, true);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int ia = ROPE == 1 ? j : 2 * j, ib = ROPE == 1 ? 8 + j : 2 * j + 1;
@@ -54,119 +89,174 @@ __device__ inline void exact_row(double (&y)[16], const float (&x)[16], const fl
     }
   }
 }
+
+// Largest of eight magnitudes; NaN stays.
 template <typename T>
-__device__ inline T most_of(const T* x) {   // of eight magnitudes; NaN stays
+__device__ inline T most_of(const T* x) {
   T m = __builtin_elementwise_abs(x[0]);
 #pragma unroll
   for (int j = 1; j < 8; ++j) m = __builtin_elementwise_maximum(m, __builtin_elementwise_abs(x[j]));
   return m;
 }
 
-template <typename E, int D, int ROPE>
+// Eight channels as they come, to codes.
+template <typename E>
+struct Plain8;
+template <>
+struct Plain8<float> {
+  static __device__ float most(const Eight<float>& x) {
+    float y[8];
+    x.values(y);
+    return most_of(y);
+  }
+  static __device__ uint32_t codes(const Eight<float>& x, int e) {
+    float y[8];
+    x.values(y);
+    return codes_of(y, e);
+  }
+};
+template <>
+struct Plain8<bf16> {
+  static __device__ float most(const Eight<bf16>& x) {   // (by the bits: a NaN is above the infinity)
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x.raw[j] & 0x7fff7fffu));
+    return __builtin_bit_cast(float, (uint32_t)(m[0] > m[1] ? m[0] : m[1]) << 16);
+  }
+  static __device__ uint32_t codes(const Eight<bf16>& x, int e) {
+    const float s = scale_value(e);
+    const uint32_t w[4] = {x.raw[0], x.raw[1], x.raw[2], x.raw[3]};
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[0]), s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[1]), s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[2]), s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[3]), s, 3);
+  }
+};
+
+template <typename E, int D, int ROPE, bool ONCE>
 __global__ __launch_bounds__(kThreads4) void cache4_append_kernel(const E* __restrict__ k, const E* __restrict__ v, const Cache4 cache, const Batch4 b,
                                                                  const int* __restrict__ positions, const void* __restrict__ weight, const Rotary r,
                                                                  int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head) {
-  constexpr int LPR = D / 16, PIECES = D / 8;
-  // Scale bytes of the pieces of 8 channels: K at the upper and at the lower end of its error, V.
-  __shared__ __attribute__((aligned(16))) uint32_t scales[kThreads4 / LPR][PIECES];
-  const long long pair = ((long long)blockIdx.x * kThreads4 + threadIdx.x) / LPR;
+  constexpr int LPR = D / 16, PIECES = D / 8, STEP = kThreads4 / LPR;
+  __shared__ Places4 places;
+  __shared__ __attribute__((aligned(16))) int k_most[STEP][PIECES], v_most[STEP][PIECES];   // scale bytes of the pieces of 8 channels
   const LanePlace<ROPE> at(threadIdx.x % LPR, r.rot_dim);
-  const int token = (int)min(pair / b.Hkv, (long long)b.n_tokens - 1), head = (int)(pair % b.Hkv);
-  Eight<E> kl, kh, vl, vh;
-  const E* kp = k + token * k_token + head * k_head;
-  const E* vp = v + token * v_token + head * v_head;
-  kl.load(kp + at.lo);
-  kh.load(kp + at.hi);
-  vl.load(vp + at.lo);
-  vh.load(vp + at.hi);
-  const TokenPlace place(token, pair / b.Hkv < b.n_tokens, b.q_start, b.kv_len, b.page_table, b.n_seq, b.page_size, b.max_pages);
-  const bool stored = place.page >= 0 && place.page < b.n_pages;
-
-  float x[16], y[16], w[16], u[16];
-  kl.values(x);
-  kh.values(x + 8);
-  vl.values(u);
-  vh.values(u + 8);
+  // (rows of the whole call stay below 2^31; a workgroup's are those of 64 tokens at most)
+  const unsigned rows = (unsigned)b.n_tokens * (unsigned)b.Hkv, row = threadIdx.x / LPR, from = blockIdx.x * STEP, pair = min(from + row, rows - 1);
+  const int first = (int)(from / (unsigned)b.Hkv), token = (int)(pair / (unsigned)b.Hkv), head = (int)(pair - (unsigned)token * (unsigned)b.Hkv);
+  Eight<E> kp[2], vp[2];
+  const E* k_row = k + token * k_token + head * k_head;
+  const E* v_row = v + token * v_token + head * v_head;
+  kp[0].template load<ONCE>(k_row + at.lo);
+  kp[1].template load<ONCE>(k_row + at.hi);
+  vp[0].template load<ONCE>(v_row + at.lo);
+  vp[1].template load<ONCE>(v_row + at.hi);
+  places.find(cache, b, first);
+  const int place = places.at[token - first];
+  const bool stored = from + row < rows && place >= 0;
+  const bool exact = r.norm == 0 && r.rope == 0;   // keys go as they come
   Angles angles;
-  if (at.turn) angles.load(r, positions ? positions[token] : place.at, at.pair, true);
-  bool doubt = false;
-#pragma unroll
-  for (int j = 0; j < 16; ++j) y[j] = x[j];
-  if (r.norm) {
-    load_weight<D>(w, weight, r, head, at);
-    float s = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) s = __builtin_fmaf(x[j], x[j], s);
-    s = __builtin_fmaf(row_sum<LPR>(s), 1.0f / (16 * LPR), r.eps);
-    doubt = !(s > 0x1p-90f && s < 0x1p120f);   // (squares that leave a float's range)
-    const float rms = 1.0f / __builtin_sqrtf(s);
-#pragma unroll
-    for (int j = 0; j < 16; ++j) y[j] = x[j] * rms * w[j];
-  }
-  // What y may be off by: 19 roundings of 2^-24 at most in what a channel is the sum of (the squares' sum counts half), with room.
-  float off[16];
-#pragma unroll
-  for (int j = 0; j < 16; ++j) off[j] = __builtin_fabsf(y[j]);
+  bool there = true;
   if (at.turn) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int ia = ROPE == 1 ? j : 2 * j, ib = ROPE == 1 ? 8 + j : 2 * j + 1;
-      const float a = off[ia], c = off[ib], tc = __builtin_fabsf(angles.c[j]), ts = __builtin_fabsf(angles.s[j]);
-      off[ia] = __builtin_fmaf(a, tc, c * ts);
-      off[ib] = __builtin_fmaf(a, ts, c * tc);
-    }
-    rotate<ROPE, 1>(y, angles);
+    const int pos = positions ? positions[token] : place;
+    there = pos >= 0 && pos < r.n_pos;
+    angles.load(r, there ? pos : 0, at.pair, true);
   }
-  const float part = r.norm || r.rope ? 0x1p-19f : 0.0f;
-  float up[16], down[16];
-#pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    up[j] = part != 0.0f ? __builtin_fmaf(off[j], part, y[j]) : y[j];   // (-0 stays)
-    down[j] = part != 0.0f ? __builtin_fmaf(off[j], -part, y[j]) : y[j];
-  }
-  // (the ends' magnitudes may be either's: both bounds of the largest one)
-  uint32_t* mine = scales[threadIdx.x / LPR];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float pu = most_of(up + 8 * h), pd = most_of(down + 8 * h);
-    float hi = __builtin_elementwise_maximum(pu, pd), lo = 0.0f;
-#pragma unroll
-    for (int j = 8 * h; j < 8 * h + 8; ++j) lo = fmaxf(lo, fminf(__builtin_fabsf(up[j]), __builtin_fabsf(down[j])));
-    // (what is no number in 32 bits, or near the least of them, is for 64 to say)
-    if (part != 0.0f) doubt |= !(hi < INFINITY) || (hi < 0x1p-100f && hi > 0.0f);
-    mine[(h ? at.hi : at.lo) / 8] = (uint32_t)scale_of(hi) | (uint32_t)scale_of(lo) << 8 | (uint32_t)scale_of(most_of(u + 8 * h)) << 16;
-  }
-  wave_order();
+  int* const k_mine = k_most[row];
+  int* const v_mine = v_most[row];
+  constexpr float part = 0x1p-19f;
+  bool doubt = false;
   int k_scale[2], v_scale[2];
   uint32_t code[2], v_code[2];
+  float y[16], off[16];
+  if (exact) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) k_mine[(h ? at.hi : at.lo) / 8] = scale_of(Plain8<E>::most(kp[h]));
+  } else {
+    kp[0].values(y);
+    kp[1].values(y + 8);
+    if (r.norm) {
+      float w[16];
+      load_weight<D>(w, weight, r, head, at);
+      float s = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s = __builtin_fmaf(y[j], y[j], s);
+      s = __builtin_fmaf(row_sum<LPR>(s), 1.0f / (16 * LPR), r.eps);
+      doubt = !(s > 0x1p-90f && s < 0x1p120f);   // (squares that leave a float's range)
+      const float rms = 1.0f / __builtin_sqrtf(s);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) y[j] = y[j] * rms * w[j];
+    }
+    // What y may be off by. A channel without rotation: 15 roundings of 2^-24 (the squares' sum, of 20, counts half). A rotated one, a c - b s: those and two
+    // more, of |a c| + |b s| <= sqrt((a^2 + b^2) (c^2 + s^2)), the length of the pair that comes out, and no more than |y_a| + |y_b|. Twice that, for what
+    // is itself rounded here.
+    if (at.turn) {
+      rotate<ROPE, 1>(y, angles);
+      if (!there) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] = __builtin_nanf("");
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int ia = ROPE == 1 ? j : 2 * j, ib = ROPE == 1 ? 8 + j : 2 * j + 1;
+        off[ia] = off[ib] = __builtin_fabsf(y[ia]) + __builtin_fabsf(y[ib]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) off[j] = __builtin_fabsf(y[j]);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float most = most_of(y + 8 * h), by = most_of(off + 8 * h) * part, hi = most + by;
+      const int e = scale_of(hi);
+      // (what is no number in 32 bits, or near the least of them, is for 64 to say)
+      doubt |= e != scale_of(most - by) || !(hi < INFINITY) || (hi < 0x1p-100f && hi > 0.0f);
+      k_mine[(h ? at.hi : at.lo) / 8] = e;
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) v_mine[(h ? at.hi : at.lo) / 8] = scale_of(Plain8<E>::most(vp[h]));
+  wave_order();
+  typedef __attribute__((ext_vector_type(4))) int i32x4;
+  auto of_group = [&](const int* mine, int h) {
+    const i32x4 s = *(const i32x4*)&mine[(h ? at.hi : at.lo) / 32 * 4];
+    return max(max(s[0], s[1]), max(s[2], s[3]));
+  };
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const u32x4 s = *(const u32x4*)&mine[(h ? at.hi : at.lo) / 32 * 4];
-    auto most = [&](int shift) { return (int)max(max(s[0] >> shift & 255, s[1] >> shift & 255), max(s[2] >> shift & 255, s[3] >> shift & 255)); };
-    k_scale[h] = most(0);
-    if (part != 0.0f) doubt |= k_scale[h] != most(8);
-    code[h] = codes_of(up + 8 * h, k_scale[h]);
-    if (part != 0.0f) doubt |= code[h] != codes_of(down + 8 * h, k_scale[h]);
-    v_scale[h] = most(16);
-    v_code[h] = v_scale[h] == kScaleNaN ? 0u : codes_of(u + 8 * h, v_scale[h]);
+    k_scale[h] = of_group(k_mine, h);
+    v_scale[h] = of_group(v_mine, h);
+    v_code[h] = v_scale[h] == kScaleNaN ? 0u : Plain8<E>::codes(vp[h], v_scale[h]);
+    if (exact) {
+      code[h] = Plain8<E>::codes(kp[h], k_scale[h]);
+    } else {
+      auto end = [&](float part) {   // codes at an end of the error
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __builtin_fmaf(off[8 * h + j], part, y[8 * h + j]);
+        return codes_of(x, k_scale[h]);
+      };
+      code[h] = end(part);
+      doubt |= code[h] != end(-part);
+    }
   }
-  if (__builtin_amdgcn_ballot_w64(doubt && stored) != 0) {
+  if (!exact && __builtin_amdgcn_ballot_w64(doubt && stored) != 0) {
     double z[16];
-    exact_row<LPR, ROPE>(z, x, w, angles, r.norm, r.eps, at.turn);
+    exact_row<E, D, ROPE>(z, kp, weight, r, head, at, at.turn ? positions ? positions[token] : place : 0);
     wave_order();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) mine[(h ? at.hi : at.lo) / 8] = (uint32_t)scale_of(most_of(z + 8 * h));
+    for (int h = 0; h < 2; ++h) k_mine[(h ? at.hi : at.lo) / 8] = scale_of(most_of(z + 8 * h));
     wave_order();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const u32x4 s = *(const u32x4*)&mine[(h ? at.hi : at.lo) / 32 * 4];
-      k_scale[h] = (int)max(max(s[0], s[1]), max(s[2], s[3]));
+      k_scale[h] = of_group(k_mine, h);
       code[h] = codes_of(z + 8 * h, k_scale[h]);
     }
   }
   if (!stored) return;
-  const int64_t codes = place.page * cache.code_page + head * cache.code_head + place.at % b.page_size * cache.code_row;
-  const int64_t scale = place.page * cache.scale_page + head * cache.scale_head + place.at % b.page_size * cache.scale_row;
+  const int64_t codes = places.code[token - first] + head * cache.code_head, scale = places.scale[token - first] + head * cache.scale_head;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int c = h ? at.hi : at.lo;
@@ -179,46 +269,69 @@ __global__ __launch_bounds__(kThreads4) void cache4_append_kernel(const E* __res
   }
 }
 
-template <typename E, int D>
+template <typename E, int D, bool ONCE>
 __global__ __launch_bounds__(kThreads4) void cache4_read_kernel(E* __restrict__ k, E* __restrict__ v, const Cache4 cache, const Batch4 b, int64_t k_token,
                                                                int64_t k_head, int64_t v_token, int64_t v_head) {
-  constexpr int LPR = D / 8;
-  const long long pair = ((long long)blockIdx.x * kThreads4 + threadIdx.x) / LPR;
-  const int c = threadIdx.x % LPR * 8;
-  const int token = (int)min(pair / b.Hkv, (long long)b.n_tokens - 1), head = (int)(pair % b.Hkv);
-  const TokenPlace place(token, pair / b.Hkv < b.n_tokens, b.q_start, b.kv_len, b.page_table, b.n_seq, b.page_size, b.max_pages);
-  if (place.page < 0 || place.page >= b.n_pages) return;
-  const int64_t codes = place.page * cache.code_page + head * cache.code_head + place.at % b.page_size * cache.code_row + c / 2;
-  const int64_t scale = place.page * cache.scale_page + head * cache.scale_head + place.at % b.page_size * cache.scale_row + c / 32;
-  const uint32_t kc = *(const uint32_t*)(cache.k_codes + codes), vc = *(const uint32_t*)(cache.v_codes + codes);
-  const float ks = scale_value(cache.k_scales[scale]), vs = scale_value(cache.v_scales[scale]);
-  typedef Values8<E> Values;
-  *(Values*)(k + token * k_token + head * k_head + c) = Values(kc, ks);
-  *(Values*)(v + token * v_token + head * v_head + c) = Values(vc, vs);
+  typedef Values16<E> Values;   // 16 bytes
+  constexpr int CH = Values::CHANNELS, LPR = D / CH, STEP = kThreads4 / LPR, FLIGHT = 4;   // rows of a lane on their way at once
+  __shared__ Places4 places;
+  const int c = threadIdx.x % LPR * CH, row = threadIdx.x / LPR, first = blockIdx.x * b.tokens;
+  const unsigned rows = (unsigned)min(b.tokens, b.n_tokens - first) * (unsigned)b.Hkv;
+  places.find(cache, b, first);
+  for (unsigned base = row; base < rows; base += FLIGHT * STEP) {
+    typename Values::Codes kc[FLIGHT], vc[FLIGHT];
+    int ks[FLIGHT], vs[FLIGHT], t[FLIGHT], head[FLIGHT];
+#pragma unroll
+    for (int i = 0; i < FLIGHT; ++i) {
+      row_of(b, min(base + i * STEP, rows - 1), t[i], head[i]);
+      const int64_t codes = places.code[t[i]] + head[i] * cache.code_head + c / 2, scale = places.scale[t[i]] + head[i] * cache.scale_head + c / 32;
+      kc[i] = *(const typename Values::Codes*)(cache.k_codes + codes);
+      vc[i] = *(const typename Values::Codes*)(cache.v_codes + codes);
+      ks[i] = cache.k_scales[scale];
+      vs[i] = cache.v_scales[scale];
+    }
+#pragma unroll
+    for (int i = 0; i < FLIGHT; ++i) {
+      if (base + i * STEP >= rows || places.at[t[i]] < 0) continue;
+      Values(kc[i], scale_value(ks[i])).template store<ONCE>(k + (first + t[i]) * k_token + head[i] * k_head + c);
+      Values(vc[i], scale_value(vs[i])).template store<ONCE>(v + (first + t[i]) * v_token + head[i] * v_head + c);
+    }
+  }
 }
 
 Cache4 cache_of(const da_cache4& c) {
   return Cache4{(uint8_t*)c.k_codes, (uint8_t*)c.k_scales, (uint8_t*)c.v_codes, (uint8_t*)c.v_scales,
                 c.code_stride[0], c.code_stride[1], c.code_stride[2], c.scale_stride[0], c.scale_stride[1], c.scale_stride[2]};
 }
-Batch4 batch_of(const da_paged& p) {
-  return Batch4{p.page_table, p.kv_len, p.q_start, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages};
+// lanes: of a row. Workgroups of `rounds` rounds over their rows where there are tokens for more than fill the chip, and at least a token each.
+Batch4 batch_of(const da_paged& p, int lanes, int rounds) {
+  const long long rows = (long long)p.n_tokens * p.Hkv, round = kThreads4 / lanes;
+  const long long want = std::max(1LL, std::min(rounds * round, rows / (4 * kComputeUnits)));   // rows of a workgroup
+  const int tokens = (int)std::max(1LL, std::min({want / p.Hkv, (long long)kMostTokens4, 65535LL / p.Hkv}));
+  return Batch4{p.page_table, p.kv_len, p.q_start, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, tokens,
+                (uint32_t)((((uint64_t)1 << 32) + p.Hkv - 1) / p.Hkv)};
 }
-unsigned grid_of(const da_paged& p, int lanes) {
-  return (unsigned)(((long long)p.n_tokens * p.Hkv * lanes + kThreads4 - 1) / kThreads4);
-}
+unsigned grid_of(const da_paged& p, const Batch4& b) { return (unsigned)((p.n_tokens + b.tokens - 1) / b.tokens); }
 
 template <typename E, int D, int ROPE>
 void append(const void* k, const void* v, const da_cache4& cache, const da_paged& p, hipStream_t stream) {
   const Rotary r = {p.rotary.norm, p.rotary.eps, p.rotary.weight_dtype, p.rotary.weight_heads, p.rotary.rope,
                     p.rotary.rope ? p.rotary.rot_dim : 0, p.rotary.n_pos, p.rotary.cos_table, p.rotary.sin_table};
-  hipLaunchKernelGGL((cache4_append_kernel<E, D, ROPE>), dim3(grid_of(p, D / 16)), dim3(kThreads4), 0, stream, (const E*)k, (const E*)v, cache_of(cache),
-                     batch_of(p), p.positions, p.rotary.k_weight, r, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
+  const unsigned step = kThreads4 / (D / 16), grid = (unsigned)(((long long)p.n_tokens * p.Hkv + step - 1) / step);
+  // What is read is not needed again. us, kept in the caches | past them: 28 MB of k and v 23.3 | 24.4, 74 MB 52 | 46 (with their reads); floats: no difference.
+  constexpr bool kCan = sizeof(E) == 2;
+  const bool once = kCan && (long long)p.n_tokens * p.Hkv * D * 2 * (long long)sizeof(E) > kPastCaches / 2;
+  hipLaunchKernelGGL((once ? cache4_append_kernel<E, D, ROPE, kCan> : cache4_append_kernel<E, D, ROPE, false>), dim3(grid), dim3(kThreads4), 0, stream, (const E*)k, (const E*)v, cache_of(cache), batch_of(p, D / 16, 1),
+                     p.positions, p.rotary.k_weight, r, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
 }
 template <typename E, int D>
 void read(void* k, void* v, const da_cache4& cache, const da_paged& p, hipStream_t stream) {
-  hipLaunchKernelGGL((cache4_read_kernel<E, D>), dim3(grid_of(p, D / 8)), dim3(kThreads4), 0, stream, (E*)k, (E*)v, cache_of(cache), batch_of(p),
-                     p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
+  const Batch4 b = batch_of(p, D / Values16<E>::CHANNELS, 8);
+  // us, kept in the caches | past them: 40 MB of k and v 17.5 | 16.0, 268 MB 69 | 43.5; floats, 157 MB, in two stores of a lane 44.7 | 56.9
+  constexpr bool kCan = sizeof(E) == 2;
+  const bool once = kCan && (long long)p.n_tokens * p.Hkv * D * 2 * (long long)sizeof(E) > kPastCaches;
+  hipLaunchKernelGGL((once ? cache4_read_kernel<E, D, kCan> : cache4_read_kernel<E, D, false>), dim3(grid_of(p, b)), dim3(kThreads4), 0, stream, (E*)k, (E*)v,
+                     cache_of(cache), b, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
 }
 
 }  // namespace

@@ -18,8 +18,8 @@ __device__ inline float scale_value(int e) { return __builtin_bit_cast(float, (u
 // The scale byte for the largest magnitude of 32 channels (not negative; NaN where one is).
 __device__ inline int scale_of(float most) {
   if (!(most < INFINITY)) return kScaleNaN;
-  const uint32_t b = __builtin_bit_cast(uint32_t, most);
-  return min(max((int)(b >> 23) - 2 + ((b & 0x7fffffu) > 0x600000u), kScaleLeast), kScaleMost);
+  // (beyond 1.75 times a power the next one)
+  return min(max((int)((__builtin_bit_cast(uint32_t, most) + 0x1fffffu) >> 23) - 2, kScaleLeast), kScaleMost);
 }
 __device__ inline int scale_of(double most) {
   if (!(most < (double)INFINITY)) return kScaleNaN;
@@ -44,6 +44,7 @@ __device__ inline float to_odd(double x) {
   b -= __builtin_fabs((double)f) > __builtin_fabs(x) ? 1 : 0;
   return __builtin_bit_cast(float, b | 1);
 }
+
 __device__ inline uint32_t codes_of(const double* x, int e) {
   float y[8];
 #pragma unroll
@@ -51,27 +52,44 @@ __device__ inline uint32_t codes_of(const double* x, int e) {
   return codes_of(y, 127);
 }
 
-// Eight channels of a row, as values.
-template <typename E>
-struct Values8;
-template <>
-struct Values8<bf16> {
+// Eight channels of a row, as operands of a product.
+__device__ inline bf16x8 values_of(uint32_t c, float s) {
+  const bf16x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3)};
   bf16x8 x;
-  __device__ Values8(uint32_t c, float s) {
-    const bf16x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3)};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = y[j >> 1][j & 1];
+  for (int j = 0; j < 8; ++j) x[j] = y[j >> 1][j & 1];
+  return x;
+}
+
+// 16 bytes of values.
+template <typename E>
+struct Values16;
+template <>
+struct Values16<bf16> {
+  static constexpr int CHANNELS = 8;
+  typedef uint32_t Codes;
+  bf16x8 x;
+  __device__ Values16(uint32_t c, float s) : x(values_of(c, s)) {}
+  template <bool ONCE>
+  __device__ void store(bf16* p) const {
+    if constexpr (ONCE) __builtin_nontemporal_store(x, (bf16x8*)p);
+    else *(bf16x8*)p = x;
   }
 };
 template <>
-struct Values8<float> {
-  f32x4 x[2];
-  __device__ Values8(uint32_t c, float s) {
-    const f32x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1),
-                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3)};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j >> 2][j & 3] = y[j >> 1][j & 1];
+struct Values16<float> {
+  static constexpr int CHANNELS = 4;
+  typedef uint16_t Codes;
+  f32x4 x;
+  __device__ Values16(uint32_t c, float s) {
+    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+    x = f32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+  template <bool ONCE>
+  __device__ void store(float* p) const {
+    if constexpr (ONCE) __builtin_nontemporal_store(x, (f32x4*)p);
+    else *(f32x4*)p = x;
   }
 };
 

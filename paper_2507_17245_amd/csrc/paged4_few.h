@@ -170,7 +170,7 @@ __device__ inline void few_rows(const Paged4Call& p, const PagedUnit& u, int hea
     for (int i = 0; i < GROUPS; ++i) {
       sc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) sc[i] = mfma_16x16x32(Values8<bf16>(kc[i][s], scale_value(ks[i])).x, qop[s], sc[i]);
+      for (int s = 0; s < KSTEPS; ++s) sc[i] = mfma_16x16x32(values_of(kc[i][s], scale_value(ks[i])), qop[s], sc[i]);
     }
     if (++at == WINDOW) {
       const int first = key_of(tile + WAVES);
@@ -230,7 +230,7 @@ __device__ inline void few_rows(const Paged4Call& p, const PagedUnit& u, int hea
     for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
       for (int s = 0; s < WORDS; ++s)
-        *(bf16x8*)(vb + (i * 16 + vr) * ROWB + (piece_at(vr, vp * WORDS + s) << 4)) = Values8<bf16>(vc[i][s], scale_value(vs[i])).x;
+        *(bf16x8*)(vb + (i * 16 + vr) * ROWB + (piece_at(vr, vp * WORDS + s) << 4)) = values_of(vc[i][s], scale_value(vs[i]));
     wave_order();
     if (odd) {
       // Keys that not every row sees, and an infinity or a NaN among their values: the product would bring it to the rows with P = 0, too. Those
