@@ -327,10 +327,9 @@ void append(const void* k, const void* v, const da_cache4& cache, const da_paged
 template <typename E, int D>
 void read(void* k, void* v, const da_cache4& cache, const da_paged& p, hipStream_t stream) {
   const Batch4 b = batch_of(p, D / Values16<E>::CHANNELS, 8);
-  // us, kept in the caches | past them: 40 MB of k and v 17.5 | 16.0, 268 MB 69 | 43.5; floats, 157 MB, in two stores of a lane 44.7 | 56.9
-  constexpr bool kCan = sizeof(E) == 2;
-  const bool once = kCan && (long long)p.n_tokens * p.Hkv * D * 2 * (long long)sizeof(E) > kPastCaches;
-  hipLaunchKernelGGL((once ? cache4_read_kernel<E, D, kCan> : cache4_read_kernel<E, D, false>), dim3(grid_of(p, b)), dim3(kThreads4), 0, stream, (E*)k, (E*)v,
+  // us, kept in the caches | past them: 40 MB of k and v 16.7 | 16.0, 268 MB 69 | 43.5, floats, 127 MB 39 | 25.6 (the smaller ones may be found there by who reads them next)
+  const bool once = (long long)p.n_tokens * p.Hkv * D * 2 * (long long)sizeof(E) > kPastCaches / 2;
+  hipLaunchKernelGGL((once ? cache4_read_kernel<E, D, true> : cache4_read_kernel<E, D, false>), dim3(grid_of(p, b)), dim3(kThreads4), 0, stream, (E*)k, (E*)v,
                      cache_of(cache), b, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
 }
 
