@@ -17,7 +17,7 @@ namespace {
 
 // Places of the line: a tile of a unit of 128 rows takes 2600 cycles where its keys come from memory, one of few rows 410: four of them are one place.
 constexpr int kUnitRows = 128, kFewRows = 16, kTileKeys = 64, kRW = 4;   // rows and keys of the line's units and tiles, waves over the rows
-constexpr int paged4_pad(int rows, int waves) { return rows != kFewRows ? 8 : waves == 8 ? 6 : 3; }
+constexpr int paged4_pad(int rows, int waves) { return rows != kFewRows ? 8 : waves == 8 ? 10 : 6; }
 constexpr int kSimdWaves = 2;   // (2 | 3, us: 64 sequences of up to 8192 d64 47.4 | 48.3, 200 of up to 2500 d128 79.6 | 86: registers, and more parts to join)
 
 // Where the 16-byte pieces of a row of 64 keys lie in LDS: neither the writes (eight lanes at a time: a piece of every quarter of two rows) nor the reads of K (the
@@ -109,11 +109,17 @@ __global__ __launch_bounds__(WAVES * 64, kSimdWaves) void paged4_few_kernel(cons
   typedef PagedLine<kFewRows, kTileKeys, paged4_pad(kFewRows, WAVES)> Line;
   const Line line(batch, &line_lds, wave, WAVES);
   Share<Line, kFewRows> share(p, line);
+  // Every key is read once. Calls of more than 64 MB leave the caches alone where a head's rows lie together (else heads share lines): 64 sequences of up to 8192 d64
+  // 47.1 -> 44.4 us, one of 100003 Hkv8 d128 34.4 -> 30.5, 200 of up to 2500 79 -> 74.5; but 16 of up to 2000 d64 14.8 -> 15.6, and tokens outside, H16 d128 73.7 -> 76.8.
+  const bool once = (long long)line.tiles * p.Hkv * (kTileKeys * 2 * (D / 2 + D / 32)) > 64LL << 20 && p.cache.code_row == D / 2;
   PagedUnit u;
   int t0, t1;
   while (share.next(p, line, u, t0, t1)) {
     const size_t slot = (2 * (size_t)share.wg + (t0 == 0 ? 2 : 1)) * kFewRows;
-    few_rows<D, STATS, WAVES, FAR>(p, u, share.head, u.m0, t0, t1, t0 == 0 && t1 == u.places, slot, wave, [&](int w) { return v_lds[w]; }, stat_lds);
+    const bool whole = t0 == 0 && t1 == u.places;
+    auto buffer = [&](int w) { return v_lds[w]; };
+    if (!FAR && once) few_rows<D, STATS, WAVES, FAR, !FAR>(p, u, share.head, u.m0, t0, t1, whole, slot, wave, buffer, stat_lds);
+    else few_rows<D, STATS, WAVES, FAR, false>(p, u, share.head, u.m0, t0, t1, whole, slot, wave, buffer, stat_lds);
     __syncthreads();   // (the next tiles take the place of the sums)
   }
 }
@@ -511,7 +517,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
     }
     if (few) {
       for (int m0 = u.m0; m0 < unit_end; m0 += kFewRows) {
-        few_rows<D, STATS, WAVES, FAR>(p, u, head, m0, t0 * few_tiles, t1 * few_tiles, whole, slot0 + (m0 - u.m0), wave, few_buf, stat_lds);
+        few_rows<D, STATS, WAVES, FAR, false>(p, u, head, m0, t0 * few_tiles, t1 * few_tiles, whole, slot0 + (m0 - u.m0), wave, few_buf, stat_lds);
         __syncthreads();
       }
     }
@@ -542,13 +548,22 @@ hipError_t launch_as(Paged4Call call, void* scratch, const PagedLaunch& l, hipSt
   return hipGetLastError();
 }
 
+// How a call is launched. us, H32 Hkv8, sequences of random lengths from a quarter of the given one on:
+//   units of 16 rows for no more new tokens than sequences. Workgroups of eight waves up to 256 units, else of four, of two for more than 512 where the table has
+//     room for 1280 keys (four | two waves: 256 sequences of up to 100 d64 17.1 | 11.1, 600 24.2 | 19.8, 1000 32.3 | 28.6; 1000 of up to 300 79.5 | 58.8, d128 104 | 79; but
+//     200 of up to 2500 d64 48.2 | 51.4, d128 72.4 | 77).
+//   their units stay whole (ranges | whole: 64 sequences of up to 1000 d64 18.7 | 12.2, d128 20 | 14.9; 256 of up to 1500 51 | 41.6; 200 of up to 2500 d128 77.6 | 73) unless the table
+//     has room for so many keys that the longest one holds up the others: d64 one sequence of 2500 11.2 | 12.4, 16 of up to 6000 19.5 | 21.3, 64 of up to 8192
+//     45.6 | 48, 32 of up to 16000, which fill the chip once, 46 | 49; d128 one of 1500 11.4 | 12.0, 16 of up to 4000 19.1 | 21.5, 64 of up to 6000 54.5 | 57.4.
+//   units of 128 rows otherwise: as in attn_paged.hip.
 struct Paged4Form {
   int rows, waves;   // of a unit, of a workgroup
   PagedLaunch launch;
 };
 Paged4Form paged4_form(const da_paged& p, size_t scratch_bytes) {
   const int group = p.H / p.Hkv;
-  const long long heads = (long long)p.n_seq * p.Hkv, full = (long long)p.n_tokens * group / kUnitRows * p.Hkv;
+  const long long heads = (long long)p.n_seq * p.Hkv, full = (long long)p.n_tokens * group / kUnitRows * p.Hkv, room = (long long)p.max_pages * p.page_size;
+  const int units = (int)std::min(std::max(heads, full), (long long)kComputeUnits);   // that there are at least
   auto form = [&](int rows, int waves, int from) {
     PagedLaunch l = paged_launch(p, rows, kTileKeys, paged4_pad(rows, waves), 4 * kSimdWaves * kComputeUnits / waves, from, scratch_bytes);
     if (l.ranges) {
@@ -560,18 +575,30 @@ Paged4Form paged4_form(const da_paged& p, size_t scratch_bytes) {
     }
     return Paged4Form{rows, waves, l};
   };
-  if (p.n_tokens <= p.n_seq && group <= 2 * kFewRows) return form(kFewRows, heads <= kComputeUnits ? 8 : 4, 20);
+  if (p.n_tokens <= p.n_seq && group <= 2 * kFewRows) {
+    const int few = (int)std::min(heads, (long long)kComputeUnits);
+    const int from = heads > kComputeUnits ? (p.d == 64 ? 96 : 64) : p.d == 64 ? 24 + few / 2 : 18 + few / 4;
+    return form(kFewRows, heads <= kComputeUnits ? 8 : heads > 2 * kComputeUnits && room <= 20 * kTileKeys ? 2 : 4, from);
+  }
   if (full > kComputeUnits) return Paged4Form{kUnitRows, 4, PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, 0, 0}};
-  return form(kUnitRows, heads > kComputeUnits ? 4 : 8, 16 + (int)std::min(std::max(heads, full), (long long)kComputeUnits) / 6);
+  return form(kUnitRows, heads > kComputeUnits ? 4 : 8, 16 + units / 6);
 }
 
+template <int D, int WAVES>
+auto few_launch(bool far) {
+  return far ? launch_as<D, kFewRows, WAVES, true> : launch_as<D, kFewRows, WAVES, false>;
+}
+template <int D, int WAVES>
+auto rows_launch(bool far) {
+  return far ? launch_as<D, kUnitRows, WAVES, true> : launch_as<D, kUnitRows, WAVES, false>;
+}
 template <int D>
 hipError_t launch_d(const Paged4Call& call, bool far, const da_paged& p, void* scratch, size_t scratch_bytes, hipStream_t stream) {
   const Paged4Form f = paged4_form(p, scratch_bytes);
-  const auto launch = f.rows == kFewRows ? (f.waves == 8 ? (far ? launch_as<D, kFewRows, 8, true> : launch_as<D, kFewRows, 8, false>)
-                                                         : (far ? launch_as<D, kFewRows, 4, true> : launch_as<D, kFewRows, 4, false>))
-                                         : (f.waves == 8 ? (far ? launch_as<D, kUnitRows, 8, true> : launch_as<D, kUnitRows, 8, false>)
-                                                         : (far ? launch_as<D, kUnitRows, 4, true> : launch_as<D, kUnitRows, 4, false>));
+  const auto launch = f.rows == kUnitRows ? (f.waves == 8 ? rows_launch<D, 8>(far) : rows_launch<D, 4>(far))
+                      : f.waves == 8      ? few_launch<D, 8>(far)
+                      : f.waves == 4      ? few_launch<D, 4>(far)
+                                          : few_launch<D, 2>(far);
   return launch(call, scratch, f.launch, stream);
 }
 

@@ -79,10 +79,10 @@ struct Paged4Call {
 //                 its scale (every value of a code is a bf16 number) and multiplies; no LDS.
 //   O^T = V^T P^T P is where it is needed. V is converted with its scales, written to LDS a wave's tile at a time and read transposed.
 // K of the next tile is asked for when this one's is converted, V likewise. buffer(wave): 8 KB of a wave's own. slot: place of the rows' sums in
-// scratch, where not the whole of a unit's tiles is walked.
-template <int D, bool STATS, int WAVES, bool FAR, typename BUFFER>
-__device__ inline void few_rows(const Paged4Call& p, const PagedUnit& u, int head, int m0, int t0, int t1, bool whole, size_t slot, int wave, BUFFER buffer,
-                                f32x4 (*stat_lds)[16]) {
+// scratch, where not the whole of a unit's tiles is walked. ONCE: what is read is not kept in the caches.
+template <int D, bool STATS, int WAVES, bool FAR, bool ONCE, typename BUFFER>
+__device__ inline void few_rows(const Paged4Call& p, const PagedUnit& u, int head, int m0, int t0, int t1, bool whole, size_t slot, int wave,
+                                BUFFER buffer, f32x4 (*stat_lds)[16]) {
   constexpr int ROWS = 16, BC = 64, FT = D == 64 ? 64 : 32, GROUPS = FT / 16, KSTEPS = D / 32, NCT = D / 16, WORDS = D / 32;
   constexpr int WINDOW = 64 / GROUPS, ROWB = D * 2;
   static_assert(FT * ROWB >= ROWS * D * 4, "a wave's sums take the place of its tile");
@@ -131,6 +131,7 @@ __device__ inline void few_rows(const Paged4Call& p, const PagedUnit& u, int hea
   int ks[GROUPS], vs[GROUPS];
   // Loads in this order and nowhere else: the waits for a tile's keys leave its values, and the next one's keys, on their way.
   auto ask = [&](const uint8_t* codes, const uint8_t* scales, int code_at, int scale_at, uint32_t (&c)[GROUPS][WORDS], int (&e)[GROUPS]) {
+    constexpr int kKeep = ONCE ? 2 : 0;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
@@ -139,11 +140,11 @@ __device__ inline void few_rows(const Paged4Call& p, const PagedUnit& u, int hea
       const __amdgpu_buffer_rsrc_t scale_rsrc = rows_rsrc(FAR ? scales + (a * p.cache.scale_page + (int64_t)b * p.cache.scale_row) : scales);
       e[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(scale_rsrc, scale_at, FAR ? 0 : b, 0);
       if constexpr (WORDS == 2) {
-        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(code_rsrc, code_at, FAR ? 0 : a, 0));
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(code_rsrc, code_at, FAR ? 0 : a, kKeep));
         c[i][0] = x[0];
         c[i][1] = x[1];
       } else {
-        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_rsrc, code_at, FAR ? 0 : a, 0));
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(code_rsrc, code_at, FAR ? 0 : a, kKeep));
 #pragma unroll
         for (int j = 0; j < 4; ++j) c[i][j] = x[j];
       }
