@@ -25,7 +25,7 @@ struct Batch4 {
   const int* __restrict__ q_start;
   int Hkv, n_seq, n_tokens, n_pages, page_size, max_pages;
   int tokens;        // of a workgroup
-  uint32_t by_heads; // 2^32 / Hkv, rounded up: x * by_heads >> 32 is x / Hkv for x < 2^16 (several tokens to a workgroup)
+  uint32_t by_heads; // 2^31 / Hkv, rounded up: 2 x * by_heads >> 32 is x / Hkv for x < 2^16 (several tokens to a workgroup, so Hkv < 2^15)
 };
 
 // Where the workgroup's tokens lie.
@@ -48,7 +48,7 @@ struct Places4 {
 };
 // Row `pair` of the workgroup's: its token there and its head.
 __device__ inline void row_of(const Batch4& b, unsigned pair, int& token, int& head) {
-  token = b.tokens == 1 ? 0 : (int)__umulhi(pair, b.by_heads);
+  token = b.tokens == 1 ? 0 : (int)__umulhi(2 * pair, b.by_heads);
   head = (int)pair - token * b.Hkv;
 }
 
@@ -309,7 +309,7 @@ Batch4 batch_of(const da_paged& p, int lanes, int rounds) {
   const long long want = std::max(1LL, std::min(rounds * round, rows / (4 * kComputeUnits)));   // rows of a workgroup
   const int tokens = (int)std::max(1LL, std::min({want / p.Hkv, (long long)kMostTokens4, 65535LL / p.Hkv}));
   return Batch4{p.page_table, p.kv_len, p.q_start, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, tokens,
-                (uint32_t)((((uint64_t)1 << 32) + p.Hkv - 1) / p.Hkv)};
+                (uint32_t)(((1u << 31) + (unsigned)p.Hkv - 1) / (unsigned)p.Hkv)};
 }
 unsigned grid_of(const da_paged& p, const Batch4& b) { return (unsigned)((p.n_tokens + b.tokens - 1) / b.tokens); }
 

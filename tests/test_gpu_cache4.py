@@ -504,3 +504,31 @@ def test_steps_of_a_program(dtype):
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
         done = [a + 1 for a in done]
     assert kept
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("Hkv,d,page", [(1, 64, 16), (1, 128, 48), (2, 64, 64), (3, 128, 16), (7, 64, 32), (16, 64, 16), (100, 64, 16)])
+def test_reads_of_many_tokens(Hkv, d, page, dtype):
+    """Workgroups of several tokens: numbers of heads that divide their rows, that do not, and a single one."""
+    n = [70000 // (Hkv * d // 64) // 2, 1, 0, 70000 // (Hkv * d // 64) // 3 + 5]
+    g = torch.Generator().manual_seed(Hkv)
+    need = [-(-x // page) for x in n]
+    n_pages = sum(need) + 2
+    table = torch.full((4, max(need)), -1, dtype=torch.int32)
+    ids, at = torch.randperm(n_pages, generator=g).to(torch.int32), 0
+    for s, m in enumerate(need):
+        table[s, :m] = ids[at:at + m]
+        at += m
+    cache = [torch.randint(0, 256, (n_pages, Hkv, page, d // 2), generator=g, dtype=torch.uint8), torch.randint(100, 140, (n_pages, Hkv, page, d // 32), generator=g, dtype=torch.uint8),
+             torch.randint(0, 256, (n_pages, Hkv, page, d // 2), generator=g, dtype=torch.uint8), torch.randint(100, 140, (n_pages, Hkv, page, d // 32), generator=g, dtype=torch.uint8)]
+    dev = tuple(t.cuda() for t in cache)
+    start = torch.tensor([1 + sum(n[:i]) for i in range(5)], dtype=torch.int32)
+    k, v = (torch.full((sum(n) + 2, Hkv, d), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    p = da.make_paged4_params(dev, table.cuda(), torch.tensor(n, dtype=torch.int32).cuda(), start.cuda(), k=k, v=v)
+    da.distr_attn_cache4_read(k, v, dev, p)
+    for x, codes, scales in ((k, cache[0], cache[1]), (v, cache[2], cache[3])):
+        want = torch.full(x.shape, 7.0, dtype=torch.float64)
+        for s, m in enumerate(n):
+            ids = table[s, :need[s]].long()
+            want[start[s]:start[s] + m] = decode(codes[ids], scales[ids]).transpose(1, 2).reshape(-1, Hkv, d)[:m]
+        assert torch.equal(x.cpu().double(), want)
