@@ -437,14 +437,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
         body(no, no, it, it & 1, s0, s1);
       }
       if (HALVES == 2 && n_tiles < n_most) lds_barrier();   // (the other half's last tile)
-      // Where some rows do not see all keys of a tile, an infinity or a NaN among its values reaches their sums (0 times it). Sums that are no
-      // numbers have the unit's rows taken again as few rows, which looks at the values of such tiles.
-      if (n_seen > all_see) {
-        float odd = 0.0f;
+      // Taken again as few rows: a unit with sums that are no numbers where some rows do not see all keys of a tile (an infinity or a NaN among its values
+      // reaches their sums, 0 times it; few rows look at the values), and one with scores so large that the rounding of a reference moves its weights
+      // out of a float's range.
+      {
+        float odd = __builtin_fabsf(nref) <= 0x1p28f ? 0.0f : 1.0f;
+        if (n_seen > all_see) {
 #pragma unroll
-        for (int mb = 0; mb < NMB; ++mb)
+          for (int mb = 0; mb < NMB; ++mb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(oacc[mb][i], 0.0f, odd);
+            for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(oacc[mb][i], 0.0f, odd);
+        }
         few = __syncthreads_or(odd != 0.0f);   // (NaN is)
       }
       if (!few) {

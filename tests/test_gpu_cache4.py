@@ -532,3 +532,33 @@ def test_reads_of_many_tokens(Hkv, d, page, dtype):
             ids = table[s, :need[s]].long()
             want[start[s]:start[s] + m] = decode(codes[ids], scales[ids]).transpose(1, 2).reshape(-1, Hkv, d)[:m]
         assert torch.equal(x.cpu().double(), want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [1e3, 1e9, 1e30, -1e9, -1e30])
+def test_chunks_of_far_scores(d, dtype, size):
+    """Scores of thousands to 1e32 of either sign: the keys of the largest one alone have weight, all of them the same (products and sums of equal numbers are exact)."""
+    n, new = 200, 70
+    b = Batch4([n, n], [new, new], 4, 2, d, dtype, page=16)
+    q = torch.full_like(b.dev["q"], abs(size))
+    k = torch.ones(2, n, d).double()
+    k[:, 90:] = 0.5 if size > 0 else 1.5
+    k *= math.copysign(1.0, size)
+    codes, scales = encode(k)
+    for s in range(2):
+        for j in range(-(-n // 16)):
+            m = min(16, n - 16 * j)
+            b.cache4[0][b.table[s, j].item(), :, :m] = codes[:, 16 * j:16 * j + m].cuda()
+            b.cache4[1][b.table[s, j].item(), :, :m] = scales[:, 16 * j:16 * j + m].cuda()
+    o, lse = _attention(b, q=q)
+    value = float(q[0, 0, 0])
+    low = math.copysign(1.0, size) * d * value / math.sqrt(d)
+    for s in range(2):
+        v = b.values[s][:, :90]
+        want, most = v.mean(1).repeat_interleave(2, 0), v.abs().mean(1).repeat_interleave(2, 0)
+        err = (o[s * new:(s + 1) * new].double() - want).abs()
+        # (90 equal weights, whatever the parts: the same products in the same order. bf16: rounded once, above and below)
+        assert (err <= most * (2.0 ** -7 if dtype == BF else 2.0 ** -17) + want.abs() * 2.0 ** -8).all()
+    want = low + math.log(90)
+    assert ((lse.double() - want).abs() <= abs(want) * 2.0 ** -21 + 2.0 ** -15).all()
