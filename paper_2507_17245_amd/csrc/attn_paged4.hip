@@ -10,15 +10,13 @@
 //     exponentials beside them); the conversions are 16 (d = 64) or 32 instructions a wave and tile.
 //   up to 32 rows: 16 at a time as few rows.
 #include "paged4_few.h"
+#include "paged4_split.h"
 
 namespace da {
 
 namespace {
 
-// Places of the line: a tile of a unit of 128 rows takes 2600 cycles where its keys come from memory, one of few rows 410: four of them are one place.
-constexpr int kUnitRows = 128, kFewRows = 16, kTileKeys = 64, kRW = 4;   // rows and keys of the line's units and tiles, waves over the rows
-constexpr int paged4_pad(int rows, int waves) { return rows != kFewRows ? 8 : waves == 8 ? 10 : 6; }
-constexpr int kSimdWaves = 2;   // (2 | 3, us: 64 sequences of up to 8192 d64 47.4 | 48.3, 200 of up to 2500 d128 79.6 | 86: registers, and more parts to join)
+constexpr int kRW = 4;   // waves over the 128 rows of a unit
 
 // Where the 16-byte pieces of a row of 64 keys lie in LDS: neither the writes (eight lanes at a time: a piece of every quarter of two rows) nor the reads of K (the
 // same piece of eight rows) and the transposing ones of V (two pairs of pieces of four rows) meet in a bank.
@@ -57,47 +55,6 @@ struct Quarter {
   }
 };
 
-// The workgroup's work: pos .. end of a line (ranges), or one unit.
-template <typename LINE, int ROWS>
-struct Share {
-  unsigned pos = 0, end = 1;
-  int wg = blockIdx.x, head = 0;
-  __device__ Share(const Paged4Call& p, const LINE& line) {
-    if (!p.ranges) return;
-    // Every kv head's line is cut into the same `ranges` ones. What follows each other here lies on one XCD: with few rows those of one place in the lines, as
-    // several heads' scales (and, tokens outside, codes) lie in one line of 128 bytes; with units of 128 rows those of one head, which read the same keys.
-    if ((gridDim.x & 7) == 0) wg = (wg & 7) * (gridDim.x >> 3) + (wg >> 3);
-    const int part = ROWS == kFewRows ? wg / p.Hkv : wg % p.ranges;
-    head = ROWS == kFewRows ? wg % p.Hkv : wg / p.ranges;
-    wg = head * p.ranges + part;
-    const unsigned length = paged_range(line.total, p.ranges, p.least);
-    pos = paged_cut(line, part, length, line.total);
-    end = paged_cut(line, part + 1, length, line.total);
-    PagedCut cut = paged_mark<ROWS>(line, pos, end, length, line.total);
-    cut.head = head;
-    cut.last += head * p.ranges;
-    if (threadIdx.x == 0) p.cuts[wg] = cut;
-  }
-  // The next unit and its tiles; false: none.
-  __device__ bool next(const Paged4Call& p, const LINE& line, PagedUnit& u, int& t0, int& t1) {
-    if (pos >= end) return false;
-    if (p.ranges) {
-      if (!line.template find<false>(pos, &u)) return false;
-      t0 = (int)(pos - u.first);
-      t1 = min(u.places, t0 + (int)(end - pos));
-    } else {
-      // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
-      head = wg % p.Hkv;
-      if (!line.template find<true>(wg / p.Hkv, &u)) return false;
-      u.m0 = (u.rows - 1) / ROWS * ROWS - u.m0;
-      t0 = 0;
-      t1 = u.places;
-    }
-    pos += (unsigned)(t1 - t0);
-    return true;
-  }
-};
-
 // Single tokens: units of 16 rows.
 template <int D, bool STATS, int WAVES, bool FAR>
 __global__ __launch_bounds__(WAVES * 64, kSimdWaves) void paged4_few_kernel(const Paged4Call p) {
@@ -108,7 +65,7 @@ __global__ __launch_bounds__(WAVES * 64, kSimdWaves) void paged4_few_kernel(cons
   const PagedBatch batch = {p.q_start, p.kv_len, p.n_seq, p.n_tokens, p.H / p.Hkv, p.max_pages * p.page_size, p.most};
   typedef PagedLine<kFewRows, kTileKeys, paged4_pad(kFewRows, WAVES)> Line;
   const Line line(batch, &line_lds, wave, WAVES);
-  Share<Line, kFewRows> share(p, line);
+  Share<Paged4Call, Line, kFewRows> share(p, line);
   // Every key is read once. Calls of more than 64 MB leave the caches alone where a head's rows lie together (else heads share lines): 64 sequences of up to 8192 d64
   // 47.1 -> 44.4 us, one of 100003 Hkv8 d128 34.4 -> 30.5, 200 of up to 2500 79 -> 74.5; but 16 of up to 2000 d64 14.8 -> 15.6, and tokens outside, H16 d128 73.7 -> 76.8.
   const bool once = (long long)line.tiles * p.Hkv * (kTileKeys * 2 * (D / 2 + D / 32)) > 64LL << 20 && p.cache.code_row == D / 2;
@@ -153,7 +110,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
   };
   typedef PagedLine<ROWS, BC, paged4_pad(ROWS, WAVES), 2 * kFewRows> Line;
   const Line line(batch, &line_lds, wave, WAVES);
-  Share<Line, ROWS> share(p, line);
+  Share<Paged4Call, Line, ROWS> share(p, line);
   PagedUnit u;
   int t0, t1;
   while (share.next(p, line, u, t0, t1)) {
@@ -549,42 +506,6 @@ hipError_t launch_as(Paged4Call call, void* scratch, const PagedLaunch& l, hipSt
   hipLaunchKernelGGL((paged_combine_kernel<bf16, D, ROWS>), dim3((unsigned)(l.workgroups * (ROWS * D / 1024))), dim3(256), 0, stream, at.sums, at.stats,
                      at.cuts, call.o, call.lse, call.H, call.Hkv);
   return hipGetLastError();
-}
-
-// How a call is launched. us, H32 Hkv8, sequences of random lengths from a quarter of the given one on:
-//   units of 16 rows for no more new tokens than sequences. Workgroups of eight waves up to 256 units, else of four, of two for more than 512 where the table has
-//     room for 1280 keys (four | two waves: 256 sequences of up to 100 d64 17.1 | 11.1, 600 24.2 | 19.8, 1000 32.3 | 28.6; 1000 of up to 300 79.5 | 58.8, d128 104 | 79; but
-//     200 of up to 2500 d64 48.2 | 51.4, d128 72.4 | 77).
-//   their units stay whole (ranges | whole: 64 sequences of up to 1000 d64 18.7 | 12.2, d128 20 | 14.9; 256 of up to 1500 51 | 41.6; 200 of up to 2500 d128 77.6 | 73) unless the table
-//     has room for so many keys that the longest one holds up the others: d64 one sequence of 2500 11.2 | 12.4, 16 of up to 6000 19.5 | 21.3, 64 of up to 8192
-//     45.6 | 48, 32 of up to 16000, which fill the chip once, 46 | 49; d128 one of 1500 11.4 | 12.0, 16 of up to 4000 19.1 | 21.5, 64 of up to 6000 54.5 | 57.4.
-//   units of 128 rows otherwise: as in attn_paged.hip.
-struct Paged4Form {
-  int rows, waves;   // of a unit, of a workgroup
-  PagedLaunch launch;
-};
-Paged4Form paged4_form(const da_paged& p, size_t scratch_bytes) {
-  const int group = p.H / p.Hkv;
-  const long long heads = (long long)p.n_seq * p.Hkv, full = (long long)p.n_tokens * group / kUnitRows * p.Hkv, room = (long long)p.max_pages * p.page_size;
-  const int units = (int)std::min(std::max(heads, full), (long long)kComputeUnits);   // that there are at least
-  auto form = [&](int rows, int waves, int from) {
-    PagedLaunch l = paged_launch(p, rows, kTileKeys, paged4_pad(rows, waves), 4 * kSimdWaves * kComputeUnits / waves, from, scratch_bytes);
-    if (l.ranges) {
-      l.ranges = l.workgroups / p.Hkv;
-      const int whole = 8 / std::gcd(8, p.Hkv);   // of a number of workgroups that the XCDs share evenly
-      if (l.ranges > 16 * whole) l.ranges -= l.ranges % whole;
-      if (l.ranges < 2) l.ranges = 0;
-      l.workgroups = l.ranges ? l.ranges * p.Hkv : (int)(paged_units(p, rows) * p.Hkv);
-    }
-    return Paged4Form{rows, waves, l};
-  };
-  if (p.n_tokens <= p.n_seq && group <= 2 * kFewRows) {
-    const int few = (int)std::min(heads, (long long)kComputeUnits);
-    const int from = heads > kComputeUnits ? (p.d == 64 ? 96 : 64) : p.d == 64 ? 24 + few / 2 : 18 + few / 4;
-    return form(kFewRows, heads <= kComputeUnits ? 8 : heads > 2 * kComputeUnits && room <= 20 * kTileKeys ? 2 : 4, from);
-  }
-  if (full > kComputeUnits) return Paged4Form{kUnitRows, 4, PagedLaunch{(int)(paged_units(p, kUnitRows) * p.Hkv), 0, 0, 0}};
-  return form(kUnitRows, heads > kComputeUnits ? 4 : 8, 16 + units / 6);
 }
 
 template <int D, int WAVES>

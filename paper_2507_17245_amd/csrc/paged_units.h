@@ -185,7 +185,7 @@ struct PagedLine {
   }
 };
 
-// (All kv heads' places stay below 2^32, by the call's checks: 2e9 tiles and 2.5e8 units of up to 8 places more.)
+// (All kv heads' places stay below 2^32, by the call's checks: 2e9 tiles of 32 keys and 2.5e8 units of up to 8 places more, or 1e9 of 64 and 11 more.)
 // Length of a range: equal ones for `workgroups` of them, none shorter than `least` tiles.
 __device__ inline unsigned paged_range(unsigned total, int workgroups, int least) {
   return max((total + (unsigned)workgroups - 1) / (unsigned)workgroups, (unsigned)least);
