@@ -185,6 +185,8 @@ __global__ __launch_bounds__(kThreads4) void cache4_append_kernel(const E* __res
       for (int j = 0; j < 16; ++j) s = __builtin_fmaf(y[j], y[j], s);
       s = __builtin_fmaf(row_sum<LPR>(s), 1.0f / (16 * LPR), r.eps);
       doubt = !(s > 0x1p-90f && s < 0x1p120f);   // (squares that leave a float's range)
+      // (a channel that is no full float before its weight, 2^-150 off, counts for less than `part` of the scale by a weight of up to 2^24 only)
+      doubt |= !(most_of(w) <= 0x1p24f && most_of(w + 8) <= 0x1p24f);
       const float rms = 1.0f / __builtin_sqrtf(s);
 #pragma unroll
       for (int j = 0; j < 16; ++j) y[j] = y[j] * rms * w[j];

@@ -124,6 +124,22 @@ def test_norms_of_rows_whose_squares_leave_the_range(dtype, scale):
         b.to_device()
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("large", [2.0 ** 25, 2.0 ** 60, 2.0 ** 100])
+def test_weights_that_lift_channels_out_of_nowhere(dtype, large):
+    """Channels so small that their norm is no full float, and weights that make them count: the codes are still those of the exact row."""
+    d, eps = 64, 1e-6
+    b = Batch4([50], [50], 2, 2, d, dtype, stored="old")
+    k = b.raw[0].double()
+    k[..., :32] *= 2.0 ** -95
+    k[..., 32:] *= 2.0 ** 50
+    k = k.to(dtype)
+    w = 1 + 0.3 * torch.randn(d, generator=torch.Generator().manual_seed(6))
+    w[:32] *= large
+    got = _append(b, k.cuda(), b.raw[1].cuda(), norm=True, eps=eps, k_weight=w.cuda())
+    _same(got, _expected(b, normed(k.double(), w.double(), float(torch.tensor(eps, dtype=F))), b.raw[1].double()))
+
+
 def test_rows_next_to_a_border():
     """Rotations that put thousands of channels within 2^-24 of a border between two codes: 32 bits alone get some of them wrong."""
     d, n = 64, 400
