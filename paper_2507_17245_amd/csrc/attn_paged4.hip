@@ -557,6 +557,7 @@ hipError_t launch_paged4(const void* q, void* o, const da_cache4& c, const da_pa
   call.q_token = p.q_stride[0];
   call.q_head = p.q_stride[1];
   call.causal = p.causal;
+  call.near = c.code_stride[1] == p.d / 2 && c.code_stride[2] > p.d / 2;
   call.scale_log2e = scale * 1.4426950408889634f;
   return p.d == 64 ? launch_d<64>(call, far, p, scratch, scratch_bytes, stream) : launch_d<128>(call, far, p, scratch, scratch_bytes, stream);
 }

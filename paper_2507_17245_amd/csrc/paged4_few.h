@@ -66,6 +66,7 @@ struct Paged4Call {
   int causal;
   float scale_log2e;
   int ranges, least;
+  int near;   // successive heads' rows of codes lie next to each other
   unsigned most;
   float* __restrict__ part_o;
   f32x4* __restrict__ part_stat;

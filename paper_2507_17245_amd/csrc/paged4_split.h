@@ -43,9 +43,16 @@ struct Share {
       t0 = (int)(pos - u.first);
       t1 = min(u.places, t0 + (int)(end - pos));
     } else {
-      // (a kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first)
+      // A kv head's units on one XCD where there are eight of them; those of a sequence that see the most keys first. Few rows of heads whose rows of codes lie next
+      // to each other and share lines of 128 bytes: every eighth unit's heads on one XCD (else | so, us, H32 Hkv8: 200 sequences of up to 2500 d64 109 | 72, d128 129 |
+      // 100, 64 of up to 1000 20.3 | 14.6; heads outside tokens d128, which share none, 67 | 69).
+      int unit = wg / p.Hkv;
       head = wg % p.Hkv;
-      if (!line.template find<true>(wg / p.Hkv, &u)) return false;
+      if (ROWS == kFewRows && p.near && wg < (int)(gridDim.x / (8u * (unsigned)p.Hkv)) * 8 * p.Hkv) {
+        unit = (wg >> 3) / p.Hkv * 8 + (wg & 7);
+        head = (wg >> 3) % p.Hkv;
+      }
+      if (!line.template find<true>(unit, &u)) return false;
       u.m0 = (u.rows - 1) / ROWS * ROWS - u.m0;
       t0 = 0;
       t1 = u.places;
