@@ -79,7 +79,8 @@ struct Paged4Call {
 //   S^T = K Q^T   by v_mfma_f32_16x16x32_bf16. A lane loads of a key what it is the operand for (8 or 16 bytes: the contraction is dealt out so), converts it with
 //                 its scale (every value of a code is a bf16 number) and multiplies; no LDS.
 //   O^T = V^T P^T P is where it is needed. V is converted with its scales, written to LDS a wave's tile at a time and read transposed.
-// K of the next tile is asked for when this one's is converted, V likewise. buffer(wave): 8 KB of a wave's own. slot: place of the rows' sums in
+// K of the next tile is asked for when this one's is converted, V likewise (one | two tiles ahead, us: 1000 sequences of up to 300 H16 d64 107 | 171, 64 of up to
+// 8192 45.5 | 48.7, one of 100003 H16 d128 74 | 77: registers that other waves need). buffer(wave): 8 KB of a wave's own. slot: place of the rows' sums in
 // scratch, where not the whole of a unit's tiles is walked. ONCE: what is read is not kept in the caches.
 template <int D, bool STATS, int WAVES, bool FAR, bool ONCE, typename BUFFER>
 __device__ inline void few_rows(const Paged4Call& p, const PagedUnit& u, int head, int m0, int t0, int t1, bool whole, size_t slot, int wave,
