@@ -334,6 +334,53 @@ def test_many_sequences(n_seq, dtype, roomy):
     _check(b, o, lse, only=set(range(0, n_seq, 1 if n_seq < 100 else n_seq // 60)))
 
 
+@pytest.mark.parametrize("n_seq,Hkv,d,most", [(7, 5, 64, 300), (70, 8, 64, 300), (203, 3, 128, 90), (403, 1, 64, 60), (90, 16, 128, 200), (40, 8, 128, 3000)])
+def test_either_order_of_a_page(n_seq, Hkv, d, most):
+    """Where heads' rows lie next to each other their workgroups are dealt out otherwise: the same cache in both orders of a page gives the same results, bit for bit."""
+    g = torch.Generator().manual_seed(n_seq)
+    lens = torch.randint(0, most, (n_seq,), generator=g).tolist()
+    new = [min(n, 1) for n in lens]
+    done = []
+    for order in ("heads", "tokens"):
+        b = Batch4(lens, new, 2 * Hkv, Hkv, d, BF, page=16, order=order, pad_back=1)
+        o, lse = _attention(b)
+        _check(b, o, lse, only=set(range(0, n_seq, max(1, n_seq // 20))))
+        done.append((b, o, lse))
+    assert all(torch.equal(x, y) for x, y in zip(done[0][0].values, done[1][0].values))
+    assert torch.equal(done[0][1].nan_to_num(9.0), done[1][1].nan_to_num(9.0)) and torch.equal(done[0][2].nan_to_num(9.0), done[1][2].nan_to_num(9.0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_two_streams_at_once(dtype):
+    """Appends, reads and attention of two caches on streams of their own without workspaces, call after call: the same as one after the other."""
+    batches = [Batch4([3000 + 500 * i, 70], [1, 1 + 40 * i], 8, 2, 64, dtype, seed=i, stored="old", room=300) for i in range(2)]
+    torch.cuda.synchronize()
+
+    def run(b):
+        k, v = (x.cuda() for x in b.raw)
+        back = [torch.zeros_like(k) for _ in range(2)]
+        o = torch.zeros(b.T, b.H, b.d, dtype=b.dtype, device="cuda")
+        for _ in range(5):
+            da.distr_attn_cache4_append(k, v, b.cache4, da.make_paged4_params(b.cache4, *b.index(), k=k, v=v))
+            da.distr_attn_cache4_read(*back, b.cache4, da.make_paged4_params(b.cache4, *b.index(), k=back[0], v=back[1]))
+            da.distr_attn_paged4_fwd(b.dev["q"], b.cache4, o, da.make_paged4_params(b.cache4, *b.index(), q=b.dev["q"]))
+        return [*back, o]
+
+    alone = []
+    for b in batches:
+        alone.append(run(b))
+        torch.cuda.synchronize()
+        b.to_device()
+    torch.cuda.synchronize()
+    streams, both = [torch.cuda.Stream() for _ in batches], []
+    for b, stream in zip(batches, streams):
+        with torch.cuda.stream(stream):
+            both.append(run(b))
+    torch.cuda.synchronize()
+    for one, other in zip(alone, both):
+        assert all(torch.equal(x, y) for x, y in zip(one, other))
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("new", [1, 40])
