@@ -17,6 +17,10 @@ namespace da {
 namespace {
 
 constexpr int kRW = 4;   // waves over the 128 rows of a unit
+// A reference is rounded, and so is the way from one to the next (half a step of the larger of both): a row's weights are off by a power of two that its sum
+// divides out. With references of up to 2^28 the exponent is 24 at most (the way 16, the next reference 8); from 2^32 on weights become infinite, or nothing,
+// also those at an ordinary reference that follows.
+constexpr float kFar = 0x1p28f;
 
 // Where the 16-byte pieces of a row of 64 keys lie in LDS: neither the writes (eight lanes at a time: a piece of every quarter of two rows) nor the reads of K (the
 // same piece of eight rows) and the transposing ones of V (two pairs of pieces of four rows) meet in a bank. (Counted at d = 128: none. At d = 64 conflicts take 9 % of a
@@ -218,6 +222,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
       f32x16 oacc[NMB];
       float nref, l_run, e_run;   // negated reference (exp2 domain), sums over this lane's half of the keys
       float trigger;              // below zero until the row has met a score above -infinity: its first one becomes the reference
+      bool far = false;           // a row of the wave has left a reference beyond kFar
       const int ka = lq * ROWB + (k_piece<D>(lq, hh) << 4);
       const int row_l = 4 * hh + ((lane & 15) >> 2);
       const int va = row_l * ROWB + (v_piece<D>(row_l, (lane >> 4 & 1) << 1 | (lane & 3) >> 1) << 4) + 8 * (lane & 1);
@@ -293,6 +298,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
         float es = exp_tile(sc, pop);
         float rs = row_sum(pop);
         if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
+          far |= __builtin_amdgcn_ballot_w64(!(__builtin_fabsf(nref) <= kFar)) != 0;
           const float mt = tile_max(sc);
           const bool first = trigger < 0.0f && mt > -INFINITY;
           if (first) trigger = kSumTrigger;
@@ -396,10 +402,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged4_rows_kernel(const Paged4
       }
       if (HALVES == 2 && n_tiles < n_most) lds_barrier();   // (the other half's last tile)
       // Taken again as few rows: a unit with sums that are no numbers where some rows do not see all keys of a tile (an infinity or a NaN among its values
-      // reaches their sums, 0 times it; few rows look at the values), and one with scores so large that the rounding of a reference moves its weights
-      // out of a float's range.
+      // reaches their sums, 0 times it; few rows look at the values), and one that has had a reference beyond kFar, its last or an earlier one.
       {
-        float odd = __builtin_fabsf(nref) <= 0x1p28f ? 0.0f : 1.0f;
+        float odd = !far && __builtin_fabsf(nref) <= kFar ? 0.0f : 1.0f;
         if (n_seen > all_see) {
 #pragma unroll
           for (int mb = 0; mb < NMB; ++mb)
