@@ -431,6 +431,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
       f32x16 oacc[NMB];
       float nref, l_run, e_run;   // negated reference (exp2 domain), sums over this lane's half of the keys
       float trigger;              // below zero until the row has met a score above -infinity: its first one becomes the reference
+      bool far = false;           // a row of the wave has left a reference beyond kFar
 
       auto qk = [&](int par, f32x16 (&sacc)[MB]) {
         const char* at = k_buf(par);
@@ -497,6 +498,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
         float es = exp_tile(sc, pop);
         float rs = row_sum(pop);
         if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
+          far |= __builtin_amdgcn_ballot_w64(!(__builtin_fabsf(nref) <= kFar)) != 0;
           const float mt = tile_max(sc);
           const bool first = trigger < 0.0f && mt > -INFINITY;
           if (first) trigger = kSumTrigger;
@@ -609,14 +611,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
         body(no, no, it, it & 1, s0, s1);
       }
       if (HALVES == 2 && n_tiles < n_most) __syncthreads();   // (the other half's last tile)
-      // Where some rows do not see all keys of a tile, an infinity or a NaN among its values reaches their sums (0 times it). Sums that are no
-      // numbers have the unit's rows taken again as few rows, 32 at a time, which looks at the values of such tiles.
-      if (n_seen > all_see) {
-        float odd = 0.0f;
+      // Taken again as few rows, 32 at a time: a unit with sums that are no numbers where some rows do not see all keys of a tile (an infinity or a NaN among
+      // its values reaches their sums, 0 times it; few rows look at the values), and one that has had a reference beyond kFar, its last or an earlier one.
+      {
+        float odd = !far && __builtin_fabsf(nref) <= kFar ? 0.0f : 1.0f;
+        if (n_seen > all_see) {
 #pragma unroll
-        for (int mb = 0; mb < NMB; ++mb)
+          for (int mb = 0; mb < NMB; ++mb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(oacc[mb][i], 0.0f, odd);
+            for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(oacc[mb][i], 0.0f, odd);
+        }
         if (__syncthreads_or(odd != 0.0f)) {   // (NaN is)
           few = true;
           continue;

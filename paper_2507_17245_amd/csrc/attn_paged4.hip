@@ -17,10 +17,6 @@ namespace da {
 namespace {
 
 constexpr int kRW = 4;   // waves over the 128 rows of a unit
-// A reference is rounded, and so is the way from one to the next (half a step of the larger of both): a row's weights are off by a power of two that its sum
-// divides out. With references of up to 2^28 the exponent is 24 at most (the way 16, the next reference 8); from 2^32 on weights become infinite, or nothing,
-// also those at an ordinary reference that follows.
-constexpr float kFar = 0x1p28f;
 
 // Where the 16-byte pieces of a row of 64 keys lie in LDS: neither the writes (eight lanes at a time: a piece of every quarter of two rows) nor the reads of K (the
 // same piece of eight rows) and the transposing ones of V (two pairs of pieces of four rows) meet in a bank. (Counted at d = 128: none. At d = 64 conflicts take 9 % of a

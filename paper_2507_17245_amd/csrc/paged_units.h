@@ -223,6 +223,12 @@ __device__ inline PageWindow page_window(const int* __restrict__ table, int key,
   return w;
 }
 
+// References of units of 128 rows, where they are subtracted from scaled scores.
+// A reference is rounded, and so is the way from one to the next (half a step of the larger of both): a row's weights are off by a power of two that its sum
+// divides out. With references of up to 2^28 the exponent is 24 at most (the way 16, the next reference 8); from 2^32 on weights become infinite, or nothing,
+// also those at an ordinary reference that follows.
+constexpr float kFar = 0x1p28f;
+
 // log-sum-exp of a row from its reference (log2 units) and the sum relative to it
 __device__ inline float row_statistic(float ref, float sum) { return sum == 0.0f ? -INFINITY : 0.6931471805599453f * (ref + __builtin_log2f(sum)); }
 
