@@ -577,7 +577,7 @@ def _paged_params(shape, cache, page_table, kv_len, q_start, q, k, v, causal, so
 
 
 def _check_pages(k_pages, v_pages, params):
-    like = params.layouts["pages"]
+    like = params.layouts.get("pages")   # (none: made for a cache in 4 bits)
     if _layout(k_pages) != like or _layout(v_pages) != like:
         raise ValueError("params were made for pages of another shape, stride, dtype or device")
 
@@ -641,7 +641,7 @@ def _cache_layout(a, b, c, d):
 def _cache4(cache, params):
     """The cache as the library takes it: its tensors are those of the call, the layout is that of params."""
     k_codes, k_scales, v_codes, v_scales = cache
-    if _cache_layout(k_codes, k_scales, v_codes, v_scales) != params.layouts["cache"]:
+    if _cache_layout(k_codes, k_scales, v_codes, v_scales) != params.layouts.get("cache"):   # (none: made for pages of keys and values)
         raise ValueError("params were made for a cache of another shape, stride or device")
     return DaCache4(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), *params.strides)
 
