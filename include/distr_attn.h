@@ -317,7 +317,7 @@ typedef struct {
 /*
  * Stores the new tokens' keys and values (k, v: [n_tokens][Hkv][d] by strides) in the cache, the keys normed and rotated on the way if
  * p->rotary says so. What lies in the cache otherwise is left as it is. Places that two tokens share (a page in two
- * sequences' tables, both with new tokens on it) receive either of them.
+ * sequences' tables, both with new tokens on it) receive either of them, some channels of one beside some of the other's.
  */
 int distr_attn_cache_append(const void *k, const void *v, void *k_pages, void *v_pages, const da_paged *p);
 
@@ -350,8 +350,8 @@ typedef struct {
  * append: k and v ([n_tokens][Hkv][d] by strides) into the cache, the keys normed and rotated on the way if p->rotary says so. The scale of 32 channels
  * is the smallest from 2^-126 to 2^125 that leaves none beyond 7 times it (the largest where there is none), or 255 where one is an infinity or a
  * NaN; a channel goes to the nearest value, at the same distance from two to the one of the even code, beyond 6 to 6. Norm and
- * rotation are taken in 64 bits where 32 leave a code in doubt: the codes are those of the exact rows. Places that two tokens
- * share receive either of them, channels of one beside the other's.
+ * rotation are taken in 64 bits where 32 leave a code in doubt: the codes are those of the exact rows. In a place that two
+ * tokens share, codes come from either of them, eight channels at a time, and a scale from either: the 32 channels may hold neither token's values.
  */
 int distr_attn_cache4_append(const void *k, const void *v, const da_cache4 *cache, const da_paged *p);
 
