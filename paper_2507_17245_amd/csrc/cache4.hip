@@ -24,7 +24,9 @@ struct Batch4 {
   const int* __restrict__ kv_len;
   const int* __restrict__ q_start;
   int Hkv, n_seq, n_tokens, n_pages, page_size, max_pages;
-  int tokens;        // of a workgroup
+};
+struct Tokens4 {     // of a workgroup that reads
+  int tokens;
   uint32_t by_heads; // 2^31 / Hkv, rounded up: 2 x * by_heads >> 32 is x / Hkv for x < 2^16 (several tokens to a workgroup, so Hkv < 2^15)
 };
 
@@ -47,9 +49,9 @@ struct Places4 {
   }
 };
 // Row `pair` of the workgroup's: its token there and its head.
-__device__ inline void row_of(const Batch4& b, unsigned pair, int& token, int& head) {
-  token = b.tokens == 1 ? 0 : (int)__umulhi(2 * pair, b.by_heads);
-  head = (int)pair - token * b.Hkv;
+__device__ inline void row_of(const Tokens4& w, int Hkv, unsigned pair, int& token, int& head) {
+  token = w.tokens == 1 ? 0 : (int)__umulhi(2 * pair, w.by_heads);
+  head = (int)pair - token * Hkv;
 }
 
 template <int LPR>
@@ -192,8 +194,8 @@ __global__ __launch_bounds__(kThreads4) void cache4_append_kernel(const E* __res
       for (int j = 0; j < 16; ++j) y[j] = y[j] * rms * w[j];
     }
     // What y may be off by. A channel without rotation: 15 roundings of 2^-24 (the squares' sum, of 20, counts half). A rotated one, a c - b s: those and two
-    // more, of |a c| + |b s| <= sqrt((a^2 + b^2) (c^2 + s^2)), the length of the pair that comes out, and no more than |y_a| + |y_b|. Twice that, for what
-    // is itself rounded here.
+    // more, of |a c| + |b s| <= sqrt((a^2 + b^2) (c^2 + s^2)), the length of the pair that comes out, and no more than |y_a| + |y_b|. `part` is 32 of them,
+    // not 17, for what is itself rounded here.
     if (at.turn) {
       rotate<ROPE, 1>(y, angles);
       if (!there) {
@@ -272,20 +274,20 @@ __global__ __launch_bounds__(kThreads4) void cache4_append_kernel(const E* __res
 }
 
 template <typename E, int D, bool ONCE>
-__global__ __launch_bounds__(kThreads4) void cache4_read_kernel(E* __restrict__ k, E* __restrict__ v, const Cache4 cache, const Batch4 b, int64_t k_token,
-                                                               int64_t k_head, int64_t v_token, int64_t v_head) {
+__global__ __launch_bounds__(kThreads4) void cache4_read_kernel(E* __restrict__ k, E* __restrict__ v, const Cache4 cache, const Batch4 b, const Tokens4 w,
+                                                               int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head) {
   typedef Values16<E> Values;   // 16 bytes
   constexpr int CH = Values::CHANNELS, LPR = D / CH, STEP = kThreads4 / LPR, FLIGHT = 4;   // rows of a lane on their way at once
   __shared__ Places4 places;
-  const int c = threadIdx.x % LPR * CH, row = threadIdx.x / LPR, first = blockIdx.x * b.tokens;
-  const unsigned rows = (unsigned)min(b.tokens, b.n_tokens - first) * (unsigned)b.Hkv;
+  const int c = threadIdx.x % LPR * CH, row = threadIdx.x / LPR, first = blockIdx.x * w.tokens;
+  const unsigned rows = (unsigned)min(w.tokens, b.n_tokens - first) * (unsigned)b.Hkv;
   places.find(cache, b, first);
   for (unsigned base = row; base < rows; base += FLIGHT * STEP) {
     typename Values::Codes kc[FLIGHT], vc[FLIGHT];
     int ks[FLIGHT], vs[FLIGHT], t[FLIGHT], head[FLIGHT];
 #pragma unroll
     for (int i = 0; i < FLIGHT; ++i) {
-      row_of(b, min(base + i * STEP, rows - 1), t[i], head[i]);
+      row_of(w, b.Hkv, min(base + i * STEP, rows - 1), t[i], head[i]);
       const int64_t codes = places.code[t[i]] + head[i] * cache.code_head + c / 2, scale = places.scale[t[i]] + head[i] * cache.scale_head + c / 32;
       kc[i] = *(const typename Values::Codes*)(cache.k_codes + codes);
       vc[i] = *(const typename Values::Codes*)(cache.v_codes + codes);
@@ -305,15 +307,16 @@ Cache4 cache_of(const da_cache4& c) {
   return Cache4{(uint8_t*)c.k_codes, (uint8_t*)c.k_scales, (uint8_t*)c.v_codes, (uint8_t*)c.v_scales,
                 c.code_stride[0], c.code_stride[1], c.code_stride[2], c.scale_stride[0], c.scale_stride[1], c.scale_stride[2]};
 }
-// lanes: of a row. Workgroups of `rounds` rounds over their rows where there are tokens for more than fill the chip, and at least a token each.
-Batch4 batch_of(const da_paged& p, int lanes, int rounds) {
-  const long long rows = (long long)p.n_tokens * p.Hkv, round = kThreads4 / lanes;
-  const long long want = std::max(1LL, std::min(rounds * round, rows / (4 * kComputeUnits)));   // rows of a workgroup
-  const int tokens = (int)std::max(1LL, std::min({want / p.Hkv, (long long)kMostTokens4, 65535LL / p.Hkv}));
-  return Batch4{p.page_table, p.kv_len, p.q_start, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages, tokens,
-                (uint32_t)(((1u << 31) + (unsigned)p.Hkv - 1) / (unsigned)p.Hkv)};
+Batch4 batch_of(const da_paged& p) {
+  return Batch4{p.page_table, p.kv_len, p.q_start, p.Hkv, p.n_seq, p.n_tokens, p.n_pages, p.page_size, p.max_pages};
 }
-unsigned grid_of(const da_paged& p, const Batch4& b) { return (unsigned)((p.n_tokens + b.tokens - 1) / b.tokens); }
+// lanes: of a row. Workgroups of eight rounds over their rows where there are tokens for more than fill the chip, and at least a token each.
+Tokens4 tokens_of(const da_paged& p, int lanes) {
+  const long long rows = (long long)p.n_tokens * p.Hkv, round = kThreads4 / lanes;
+  const long long want = std::max(1LL, std::min(8 * round, rows / (4 * kComputeUnits)));   // rows of a workgroup
+  const int tokens = (int)std::max(1LL, std::min({want / p.Hkv, (long long)kMostTokens4, 65535LL / p.Hkv}));
+  return Tokens4{tokens, (uint32_t)(((1u << 31) + (unsigned)p.Hkv - 1) / (unsigned)p.Hkv)};
+}
 
 template <typename E, int D, int ROPE>
 void append(const void* k, const void* v, const da_cache4& cache, const da_paged& p, hipStream_t stream) {
@@ -323,16 +326,16 @@ void append(const void* k, const void* v, const da_cache4& cache, const da_paged
   // What is read is not needed again. us, kept in the caches | past them: 28 MB of k and v 23.3 | 24.4, 74 MB 52 | 46 (with their reads); floats: no difference.
   constexpr bool kCan = sizeof(E) == 2;
   const bool once = kCan && (long long)p.n_tokens * p.Hkv * D * 2 * (long long)sizeof(E) > kPastCaches / 2;
-  hipLaunchKernelGGL((once ? cache4_append_kernel<E, D, ROPE, kCan> : cache4_append_kernel<E, D, ROPE, false>), dim3(grid), dim3(kThreads4), 0, stream, (const E*)k, (const E*)v, cache_of(cache), batch_of(p, D / 16, 1),
+  hipLaunchKernelGGL((once ? cache4_append_kernel<E, D, ROPE, kCan> : cache4_append_kernel<E, D, ROPE, false>), dim3(grid), dim3(kThreads4), 0, stream, (const E*)k, (const E*)v, cache_of(cache), batch_of(p),
                      p.positions, p.rotary.k_weight, r, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
 }
 template <typename E, int D>
 void read(void* k, void* v, const da_cache4& cache, const da_paged& p, hipStream_t stream) {
-  const Batch4 b = batch_of(p, D / Values16<E>::CHANNELS, 8);
+  const Tokens4 w = tokens_of(p, D / Values16<E>::CHANNELS);
   // us, kept in the caches | past them: 40 MB of k and v 16.7 | 16.0, 268 MB 69 | 43.5, floats, 127 MB 39 | 25.6 (the smaller ones may be found there by who reads them next)
   const bool once = (long long)p.n_tokens * p.Hkv * D * 2 * (long long)sizeof(E) > kPastCaches / 2;
-  hipLaunchKernelGGL((once ? cache4_read_kernel<E, D, true> : cache4_read_kernel<E, D, false>), dim3(grid_of(p, b)), dim3(kThreads4), 0, stream, (E*)k, (E*)v,
-                     cache_of(cache), b, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
+  hipLaunchKernelGGL((once ? cache4_read_kernel<E, D, true> : cache4_read_kernel<E, D, false>), dim3((unsigned)((p.n_tokens + w.tokens - 1) / w.tokens)), dim3(kThreads4), 0, stream, (E*)k, (E*)v,
+                     cache_of(cache), batch_of(p), w, p.k_stride[0], p.k_stride[1], p.v_stride[0], p.v_stride[1]);
 }
 
 }  // namespace
