@@ -497,7 +497,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void paged_kernel(
         bf16x8 pop[TT];
         float es = exp_tile(sc, pop);
         float rs = row_sum(pop);
-        if (__builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0) {
+        // (d = 64: out of the loop's way, 2048 tokens on 16384 285 | 281 us with the look at the reference below; d = 128 472.5 | 474)
+        const bool lift = __builtin_amdgcn_ballot_w64(!(rs <= trigger)) != 0;
+        if (D == 64 ? __builtin_expect(lift, 0) : lift) {
           far |= __builtin_amdgcn_ballot_w64(!(__builtin_fabsf(nref) <= kFar)) != 0;
           const float mt = tile_max(sc);
           const bool first = trigger < 0.0f && mt > -INFINITY;
