@@ -614,7 +614,7 @@ def make_paged4_params(cache, page_table, kv_len, q_start, q=None, k=None, v=Non
     """Parameters of distr_attn_cache4_append and distr_attn_cache4_read (k, v given) and distr_attn_paged4_fwd (q given) for a batch of
     sequences in one cache held in 4 bits: cache = (k_codes, k_scales, v_codes, v_scales), uint8, codes [pages, Hkv, page size, d / 2] with channel
     2 j in the low bits of byte j, scales [pages, Hkv, page size, d / 32]: 2^(byte - 127) for 32 channels. Any strides with contiguous
-    rows, the same for keys and values. The rest as in make_paged_params; workspace of distr_attn_paged4_workspace_bytes."""
+    rows, the same for keys and values. page_table: no wider than the batch can need, its width decides how the attention is dealt out. The rest as in make_paged_params; workspace of distr_attn_paged4_workspace_bytes."""
     import torch
     k_codes, k_scales, v_codes, v_scales = cache
     for a, b, what in ((k_codes, v_codes, "codes"), (k_scales, v_scales, "scales")):

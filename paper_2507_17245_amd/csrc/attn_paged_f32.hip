@@ -2,9 +2,9 @@
 // work split: paged_f32.h.
 //
 // Bound: the float products, 1/16 of the bf16 rate. A lane's operands are 16-byte loads (V at d = 64: 8).
-// Measured, us: three chunks of up to 48 on up to 700, H8 d64 17.1 (latency: 13, and the combine kernel's 4.2); 100 tokens on 2000, H16 Hkv4 d128 53;
-// 16 chunks of 40 on up to 2000, H8 d64 61 (28 % of the products' rate: each unit reads the keys again, K one tile ahead); 64 single tokens of up to
-// 8192, H32 Hkv8 d64 339 (3.7 TB/s).
+// Measured, us: three chunks of up to 48 on up to 700, H8 d64 17.7 (latency: 13, and the combine kernel's 4.2); 100 tokens on 2000, H16 Hkv4 d128 51;
+// 16 chunks of 40 on up to 2000, H8 d64 63 (27 % of the products' rate: each unit reads the keys again, K one tile ahead); 64 single tokens of up to
+// 8192, H32 Hkv8 d64 335 (3.7 TB/s). The kernel as a template for both caches takes 1 % more at d = 64 and the same at d = 128.
 #include "paged_f32.h"
 
 namespace da {
